@@ -250,6 +250,172 @@ int ngpu_lm_fused_greedy_decode(const ngpu_lm *lm, const float *d_asr, int64_t B
                                 int32_t *d_states, int32_t *d_prev, int32_t *d_labels, int32_t *d_label_states,
                                 void *hip_stream);
 
+/* ------------------------------------------------------------------------
+ * Speculative decoding with the n-gram model as the drafter.  One round over a
+ * batch of sequences: ngpu_lm_draft proposes K tokens a sequence, the network
+ * runs once over them, appending its keys and values to a paged cache
+ * (ngpu_lm_kv_append) that its attention reads (ngpu_lm_attend), and
+ * ngpu_lm_verify keeps a prefix of the draft and adds one token, so that the
+ * tokens are distributed as the network's own.
+ *
+ * Random numbers are inputs.  A token is drawn from weights w >= 0 with unit
+ * exponential noise e as the argmax of w / e (the lowest token of several),
+ * which picks v with probability w[v] / sum(w).  A NaN counts as the lowest
+ * value.
+ * ------------------------------------------------------------------------ */
+
+/* Most drafted tokens a sequence and round. */
+#define NGPU_LM_MAX_DRAFT 63
+/* Least temperature other than 0 (greedy). */
+#define NGPU_LM_MIN_TEMPERATURE 1e-6f
+/* Most sequences (ngpu_lm_verify, ngpu_lm_kv_append, ngpu_lm_attend) per call. */
+#define NGPU_LM_MAX_SEQUENCES (1 << 20)
+
+enum ngpu_dtype { NGPU_F32 = 0, NGPU_F16 = 1, NGPU_BF16 = 2 };
+
+/* Draft K tokens (1..NGPU_LM_MAX_DRAFT) for each of B sequences from the n-gram
+ * model alone: with x = lm / temperature over the V tokens,
+ *   log p = x - max(x) - log sum exp(x - max(x)),
+ *   token = argmax_v exp(x[v] - max(x)) / e[v],   state <- next[token],
+ * K times.  temperature 0: token = argmax_v lm[v], the lowest of several.
+ * d_states [B]: the states the sequences are in; not changed.
+ * d_last [B] or NULL: a token each sequence takes before the draft starts (the
+ *   one that the verification before added), -1 for none.
+ * d_noise: unit exponential noise, V values at d_noise + b * noise_stride_b +
+ *   k * noise_stride_k (elements); unused (may be NULL) at temperature 0.
+ * d_tokens [B, K]; d_draft_states [B, K + 1]: the state before the draft, then the
+ *   one after each of its tokens; d_logprobs [B, K, V]: log p, the rows that
+ *   ngpu_lm_verify takes, or NULL; must be NULL at temperature 0, where the
+ *   draft has all its mass on one token.
+ * A state outside [0, num_states) or a last token outside [-1, V) gives -1
+ * tokens and states and NaN rows and is counted for ngpu_lm_check_states. */
+int ngpu_lm_draft(const ngpu_lm *lm, const int32_t *d_states, const int32_t *d_last, int64_t B, int32_t K,
+                  float temperature, const float *d_noise, int64_t noise_stride_b, int64_t noise_stride_k,
+                  int32_t *d_tokens, int32_t *d_draft_states, float *d_logprobs, void *hip_stream);
+
+/* Verification of drafted tokens.  Strides are in elements; the last dimension
+ * of logits, log-probabilities and noise has unit stride. */
+typedef struct {
+    int64_t B;                     /* sequences */
+    int32_t K;                     /* drafted tokens a sequence, 0..NGPU_LM_MAX_DRAFT */
+    int64_t V;                     /* vocabulary, 1..2^31 - 1 */
+    int32_t dtype;                 /* of the logits, ngpu_dtype */
+    const void *logits;            /* [B, K + 1, V]: row k scores the token at place k */
+    int64_t logits_stride_b, logits_stride_k;
+    const int32_t *tokens;         /* [B, K] drafted tokens; one outside [0, V) ends its sequence's draft */
+    const int32_t *lengths;        /* [B] drafted tokens that count, clamped to [0, K], or NULL for K */
+    const float *logprobs;         /* [B, K, V] natural-log probabilities the draft was drawn with, or NULL: each
+                                    * token had probability 1 (greedy drafts) */
+    int64_t logprobs_stride_b, logprobs_stride_k;
+    const float *uniforms;         /* [B, K] uniform numbers in [0, 1) */
+    const float *noise;            /* [B, V] unit exponential noise for the token that is added */
+    int64_t noise_stride_b;
+    float temperature;             /* of the network's softmax; 0: greedy, and logprobs, uniforms and noise are unused */
+    const int32_t *draft_states;   /* [B, K + 1] as ngpu_lm_draft gives them, or NULL */
+    int32_t *out_tokens;           /* [B, K + 1]: the kept tokens, the added one, then -1 */
+    int32_t *accepted;             /* [B] kept tokens a sequence, 0..K */
+    int32_t *states;               /* [B] draft_states at the kept tokens' end (the added token is not taken yet:
+                                    * it is the next draft's last token), or NULL */
+} ngpu_verify_t;
+
+/* Device memory a verification needs, 16-byte aligned, not initialised; free
+ * again when the call's work has run. */
+size_t ngpu_lm_verify_workspace(int64_t B, int32_t K, int64_t V);
+
+/* With p = softmax(logits / temperature) and q = exp(logprobs) (or 1 at the drafted
+ * token): the token x at place k is kept while every one before it is and
+ *   uniforms[k] * q[k][x] < p[k][x].
+ * At the first place a whose token is not kept, the added token is drawn from
+ * max(p[a] - q[a], 0) with the noise, at the draft's end (and where that leaves
+ * nothing) from p[a].  temperature 0: x is kept while it is the row's argmax (the
+ * lowest of several), and the added token is the argmax of row a.
+ * A NaN logit counts as -inf; +inf logits share the row's whole mass; a row with
+ * nothing above -inf gives every token p = 0, so nothing is kept there and
+ * token 0 is added.  B = 0 is a no-op. */
+int ngpu_lm_verify(const ngpu_verify_t *args, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* A paged cache of keys and values: pages of page_size tokens, each with `heads`
+ * heads of `dim` elements (unit stride).  Strides in elements. */
+typedef struct {
+    int32_t dtype;                 /* NGPU_F16 or NGPU_BF16 */
+    int32_t heads, dim;            /* dim: 1..NGPU_LM_MAX_HEAD_DIM */
+    int32_t page_size;             /* tokens */
+    int64_t num_pages;
+    void *k, *v;
+    int64_t k_stride_page, k_stride_token, k_stride_head;
+    int64_t v_stride_page, v_stride_token, v_stride_head;
+} ngpu_kv_cache_t;
+#define NGPU_LM_MAX_HEAD_DIM 256
+
+enum ngpu_rope_layout {
+    NGPU_ROPE_HALF = 0,            /* pairs (i, i + rotary / 2) */
+    NGPU_ROPE_INTERLEAVED = 1      /* pairs (2 i, 2 i + 1) */
+};
+
+/* New keys and values of S sequences, T tokens each (padded), for the cache. */
+typedef struct {
+    int64_t S, T;
+    const void *k, *v;             /* [S, T, heads, dim], the cache's type, unit stride in the last dimension */
+    int64_t k_stride_seq, k_stride_token, k_stride_head;
+    int64_t v_stride_seq, v_stride_token, v_stride_head;
+    const void *q;                 /* [S, T, q_heads, dim] queries to rotate too, or NULL */
+    int32_t q_heads;
+    int64_t q_stride_seq, q_stride_token, q_stride_head;
+    void *q_out;                   /* [S, T, q_heads, dim] contiguous; must not overlap q */
+    const int32_t *pages;          /* [S, pages_width] page tables, row stride pages_stride */
+    int64_t pages_width, pages_stride;
+    const int32_t *start;          /* [S] place of each sequence's first new token among its own tokens */
+    const int32_t *lengths;        /* [S] new tokens that count, clamped to [0, T], or NULL for T */
+    int32_t rotary;                /* rotated leading dimensions: even, 0..dim; 0: no rotation */
+    int32_t layout;                /* ngpu_rope_layout */
+    const int32_t *positions;      /* [S, T] row of the tables for each token, or NULL: start + t */
+    const float *cos, *sin;        /* [positions_count, rotary / 2] contiguous */
+    int64_t positions_count;
+} ngpu_kv_append_t;
+
+/* Token t of sequence s goes to place start[s] + t of its own tokens, that is to
+ * entry (place mod page_size) of page pages[s][place / page_size], with its key's
+ * (and query's) pairs (a, b) turned to (a cos - b sin, b cos + a sin) in fp32
+ * and rounded once.  A token that does not count, or whose place lies outside
+ * the table or on a page outside [0, num_pages), is not stored; its query is
+ * rotated all the same where it counts, and rows of q_out that do not count are
+ * zero.  A position outside [0, positions_count) gives NaN keys and queries.
+ * Places must not repeat within a call (two sequences on one page entry). */
+int ngpu_lm_kv_append(const ngpu_kv_cache_t *cache, const ngpu_kv_append_t *args, void *hip_stream);
+
+/* Attention of S sequences with T query tokens each over the cache.  The
+ * sequences come in G groups of S / G: those of one group share a prefix of
+ * cached tokens, and each has tokens of its own after it. */
+typedef struct {
+    int64_t S, T;
+    int32_t q_heads;               /* a multiple of the cache's heads; consecutive ones share a cache head */
+    const void *q;                 /* [S, T, q_heads, dim], the cache's type, unit stride in the last dimension */
+    int64_t q_stride_seq, q_stride_token, q_stride_head;
+    const int32_t *q_lengths;      /* [S] query tokens that count, clamped to [0, T], or NULL for T */
+    int64_t G;                     /* groups (divides S), 0: no shared prefix */
+    const int32_t *prefix_pages;   /* [G, prefix_width] page tables of the prefixes */
+    int64_t prefix_width, prefix_stride;
+    const int32_t *prefix_lengths; /* [G] tokens, clamped to what the table holds */
+    const int32_t *pages;          /* [S, pages_width] page tables of the own tokens, or NULL: none */
+    int64_t pages_width, pages_stride;
+    const int32_t *lengths;        /* [S] own tokens, the query tokens among them (the last ones), clamped alike */
+    float scale;                   /* of the scores */
+    void *out;                     /* [S, T, q_heads, dim] contiguous */
+    float *lse;                    /* [S, T, q_heads] log of the softmax's sum, or NULL */
+} ngpu_attend_t;
+
+/* Device memory an attention needs, 16-byte aligned, not initialised. */
+size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args);
+
+/* Query t < q_lengths[s] attends to every token of its group's prefix and to the
+ * own tokens j < lengths[s] - q_lengths[s] + t + 1:
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,
+ * the sums in fp32.  Keys on a page outside [0, num_pages) do not take part, nor
+ * does anything else that a query does not attend to, whatever it holds.  A row
+ * without any key, and one that does not count, is zero with lse = -inf. */
+int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void *d_workspace,
+                   size_t workspace_bytes, void *hip_stream);
+
 /* Synchronises hip_stream, then reports (and clears) how many out-of-range
  * input states the queries enqueued since the last check met.  Returns
  * NGPU_E_BAD_STATE when the count is non-zero. */

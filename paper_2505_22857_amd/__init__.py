@@ -40,6 +40,8 @@ EXPORTED = [
     "ngpu_lm_fused_topk", "ngpu_lm_start_state", "ngpu_lm_final_weights",
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
+    "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
+    "ngpu_lm_attend",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
 ]
 
@@ -91,6 +93,7 @@ def load_library(path: str = LIB_PATH):
     lib.ngpu_lm_start_state.argtypes = [vp, ctypes.POINTER(i64)]
     lib.ngpu_lm_final_weights.argtypes = [vp, vp, i64, vp, vp]
     lib.ngpu_lm_fused_topk.argtypes = [vp, vp, i64, i64, ctypes.c_float, i32, vp, vp, vp, vp, vp]
+    lib.ngpu_lm_draft.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, i64, i64, vp, vp, vp, vp]
     lib.ngpu_lm_check_states.argtypes = [vp, vp, ctypes.POINTER(i64)]
     lib.ngpu_lm_sync_check.argtypes = [vp, vp]
     lib.ngpu_lm_query_bytes.argtypes = [vp, vp, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
@@ -103,7 +106,8 @@ def load_library(path: str = LIB_PATH):
     lib.ngpu_lm_last_error.argtypes = []
     lib.ngpu_lm_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
-        if name not in ("ngpu_lm_free", "ngpu_lm_device_bytes", "ngpu_lm_last_error", "ngpu_arpa_free"):
+        if name not in ("ngpu_lm_free", "ngpu_lm_device_bytes", "ngpu_lm_last_error", "ngpu_arpa_free",
+                        "ngpu_lm_verify_workspace", "ngpu_lm_attend_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -411,6 +415,35 @@ class NgpuLM:
             _stream_handle(stream)))
         return labels
 
+    def draft(self, states, k: int, noise=None, temperature: float = 1.0, last=None, stream=None):
+        """Draft ``k`` tokens for each of device int32 ``states`` [B] from the n-gram model alone.
+
+        Each token is drawn from softmax(scores / ``temperature``) with ``noise`` [B, k, V] float32, unit
+        exponential: the argmax of weight / noise.  ``temperature`` 0: the best token, no noise.  ``last``
+        [B] int32: a token each sequence takes first (-1: none), as ``verify`` added it.
+
+        Returns (tokens [B, k] int32, states before the draft and after each token [B, k + 1] int32,
+        log-probabilities [B, k, V] float32, None at temperature 0)."""
+        import torch
+        from .serving import MAX_DRAFT, _need, _on
+        B, V, k, temperature = states.numel(), self.vocab_size, int(k), float(temperature)
+        dev, sample = states.device, temperature != 0.0
+        if not 1 <= k <= MAX_DRAFT:
+            raise ValueError(f"k must lie in [1, {MAX_DRAFT}]")
+        if sample and noise is None:
+            raise ValueError("sampling needs noise")
+        ps = _dptr(states, torch.int32, "states")
+        pl = _need(last, "last", dev, torch.int32, (B,))
+        pn = _need(noise, "noise", dev, torch.float32, (B, k, V), rows=True) if sample else None
+        with _on(dev, stream) as handle:
+            tokens = torch.empty((B, k), dtype=torch.int32, device=dev)
+            after = torch.empty((B, k + 1), dtype=torch.int32, device=dev)
+            rows = torch.empty((B, k, V), dtype=torch.float32, device=dev) if sample else None
+            _check(self._lib.ngpu_lm_draft(self._h, ps, pl, B, k, temperature, pn, noise.stride(0) if sample else 0,
+                                           noise.stride(1) if sample else 0, tokens.data_ptr(), after.data_ptr(),
+                                           rows.data_ptr() if sample else None, handle))
+        return tokens, after, rows
+
     def check_states(self, stream=None) -> int:
         n = ctypes.c_int64()
         rc = self._lib.ngpu_lm_check_states(self._h, _stream_handle(stream), ctypes.byref(n))
@@ -437,6 +470,10 @@ class NgpuLM:
         return int(hbm.value), int(tot.value)
 
 
-__all__ = ["NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED", "NGPU_BUILD_BOS_EOS",
+from .serving import (MAX_DRAFT, MAX_HEAD_DIM, NGPU_BF16, NGPU_F16, NGPU_F32, NGPU_ROPE_HALF,  # noqa: E402
+                      NGPU_ROPE_INTERLEAVED, attend, kv_append, rope_table, verify)
+
+__all__ = ["verify", "kv_append", "attend", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
+           "NGPU_BF16", "NGPU_ROPE_HALF", "NGPU_ROPE_INTERLEAVED", "NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED", "NGPU_BUILD_BOS_EOS",
            "NGPU_BUILD_REPAIR_CLOSURE",
            "NGPU_FUSION_PLAIN", "NGPU_FUSION_CTC", "NGPU_FUSION_TRANSDUCER", "NGPU_FUSION_AED"]

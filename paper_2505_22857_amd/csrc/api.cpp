@@ -21,6 +21,9 @@ hipError_t launch_final_weights(const DevTrie &t, const int32_t *states, int64_t
 hipError_t launch_fused_topk(const DevTrie &t, const float *asr, int64_t B, int64_t ld, float lambda, int k,
                              const int32_t *states, int32_t *tokens, float *scores, int32_t *next,
                              hipStream_t stream);
+hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *last, int64_t B, int K,
+                        float temperature, const float *noise, int64_t noise_b, int64_t noise_k, int32_t *tokens,
+                        int32_t *draft_states, float *logprobs, hipStream_t stream);
 }  // namespace ngpu
 
 namespace {
@@ -278,6 +281,31 @@ int ngpu_lm_fused_greedy_decode(const ngpu_lm *lm, const float *d_asr, int64_t B
     hipError_t e = ngpu::launch_fused_decode(t, d_asr, B, T, stride_b, stride_t, d_lengths, mode, lambda, d_states,
                                              d_prev, d_labels, d_label_states, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return hip_fail(e, "fused decode launch");
+    return ok();
+}
+
+int ngpu_lm_draft(const ngpu_lm *lm, const int32_t *d_states, const int32_t *d_last, int64_t B, int32_t K,
+                  float temperature, const float *d_noise, int64_t noise_stride_b, int64_t noise_stride_k,
+                  int32_t *d_tokens, int32_t *d_draft_states, float *d_logprobs, void *hip_stream) {
+    if (!lm) return fail(NGPU_E_INVALID_ARG, "null handle");
+    if (const int rc = ready(lm)) return rc;
+    if (B < 0 || B > kMaxBatch) return fail(NGPU_E_INVALID_ARG, "B = %lld outside [0, %lld]", (long long)B,
+                                            (long long)kMaxBatch);
+    if (K < 1 || K > NGPU_LM_MAX_DRAFT)
+        return fail(NGPU_E_INVALID_ARG, "K = %d outside [1, %d]", K, NGPU_LM_MAX_DRAFT);
+    if (temperature != 0.0f && !(std::isfinite(temperature) && temperature >= NGPU_LM_MIN_TEMPERATURE))
+        return fail(NGPU_E_INVALID_ARG, "temperature must be 0 or finite and at least %g", NGPU_LM_MIN_TEMPERATURE);
+    if (temperature == 0.0f && d_logprobs)
+        return fail(NGPU_E_INVALID_ARG, "a greedy draft (temperature 0) has no log-probabilities");
+    if (temperature != 0.0f && ((K > 1 && noise_stride_k < 0) || (B > 1 && noise_stride_b < 0)))
+        return fail(NGPU_E_INVALID_ARG, "negative strides");
+    if (B == 0) return ok();
+    if (!d_states || !d_tokens || !d_draft_states || (temperature != 0.0f && !d_noise))
+        return fail(NGPU_E_INVALID_ARG, "null device pointer");
+    hipError_t e = ngpu::launch_draft(dev_view(lm), d_states, d_last, B, K, temperature, d_noise, noise_stride_b,
+                                      noise_stride_k, d_tokens, d_draft_states, d_logprobs,
+                                      static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return hip_fail(e, "draft launch");
     return ok();
 }
 

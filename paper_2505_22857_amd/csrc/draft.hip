@@ -1,0 +1,254 @@
+// Drafting from the n-gram model: K tokens for each sequence in one launch, one
+// workgroup a sequence, its tokens dealt to W wavefronts (group.h).
+//
+// A step scores the vocabulary as the query does, x[v] = lm[v], and draws a
+// token: with m = max x and w[v] = exp((x[v] - m) / temperature), the argmax of
+// w[v] / e[v] over unit exponential noise e is v with probability w[v] / sum w.
+// Its log-probability row is (x[v] - m) / temperature - log sum w, all in fp32.
+// The wavefronts take m, sum w and the best ratio over their own tokens and
+// meet once a step: the ratios and sums are then rescaled by exp of the
+// difference of the maxima, as the parts of a split softmax are joined.
+//
+// A step is a chain of dependent accesses (chain record, dense row and arcs,
+// exchange, next record), so small batches are bound by latency; the noise rows
+// do not depend on the chain and are loaded a step ahead.  Large ones are bound
+// by reading the noise and writing the rows (8 bytes a token).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <type_traits>
+
+#include "group.h"
+
+namespace ngpu {
+
+// The inverse of float_key.
+__device__ __forceinline__ float key_float(unsigned k) {
+    return __int_as_float(int(k ^ (~unsigned(int(k) >> 31) | 0x80000000u)));
+}
+
+// Sum over W values that repeat every W lanes: pairs, then pairs of pairs, so
+// every lane adds the same numbers in the same order.
+template <int W>
+__device__ __forceinline__ float sum_over_waves(float x) {
+    auto moved = [](float v, auto ctrl) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    if (W >= 2) x += moved(x, std::integral_constant<int, 0xB1>{});    // lane ^ 1
+    if (W >= 4) x += moved(x, std::integral_constant<int, 0x4E>{});    // lane ^ 2
+    if (W >= 8) x += moved(x, std::integral_constant<int, 0x141>{});   // other half of 8
+    if (W >= 16) x += moved(x, std::integral_constant<int, 0x140>{});  // other half of 16
+    return x;
+}
+
+// Sum over the wavefront, in a fixed order, uniform in every lane.
+__device__ __forceinline__ float wave_sum(float x) {
+    x = sum_over_waves<16>(x);   // of each row of 16 lanes
+    float r = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWave; i += 16) r += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
+    return r;
+}
+
+struct Draft {
+    DevTrie t;
+    const int32_t *states, *last;
+    const float *noise;
+    int64_t noise_b, noise_k;
+    int K;
+    float inv_temperature;
+    int32_t *tokens, *draft_states;
+    float *logprobs;
+};
+
+template <int W, int NT, bool FULL, bool SAMPLE>
+__global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
+    extern __shared__ i32x4 lds4[];
+    const DevTrie &t = d.t;
+    const int64_t b = blockIdx.x;
+    const int V = t.vocab_size, K = d.K;
+    Meet *meet = reinterpret_cast<Meet *>(lds4);
+    const Group<W, NT, FULL> g(V, reinterpret_cast<i32x2 *>(meet + 1));
+    const int wave = g.wave, lane = g.lane;
+    int32_t *tokens = d.tokens + b * K, *states = d.draft_states + b * (K + 1);
+    float *rows = SAMPLE && d.logprobs ? d.logprobs + b * K * V : nullptr;
+
+    int s = __builtin_amdgcn_readfirstlane(d.states[b]);
+    const int last = d.last ? __builtin_amdgcn_readfirstlane(d.last[b]) : -1;
+    if (s < 0 || s >= t.num_states || last < -1 || last >= V) {
+        if (wave == 0 && lane == 0) atomicAdd(&t.status[0], 1);
+        for (int k = threadIdx.x; k <= K; k += W * kWave) {
+            if (k < K) tokens[k] = -1;
+            states[k] = -1;
+        }
+        if (rows)
+            for (int64_t i = threadIdx.x; i < int64_t(K) * V; i += W * kWave) rows[i] = __builtin_nanf("");
+        return;
+    }
+    const RecordIndex ri = record_index(t, lane);
+    Words<NT> noise, noise_next, dw, dt;
+    const float *noise_row = SAMPLE ? d.noise + b * d.noise_b : nullptr;
+    if (SAMPLE) g.load_row(noise_row, noise);
+    int4 rec = load_record(ri, s, lane);
+    g.clear_slots();
+    bool dirty = false;
+    int turn = 0;   // of the meeting point's two buffers
+
+    if (last >= 0) {   // the state after `last`, whose wavefront finds it
+        const ChainHead h = head_of(rec);
+        dirty = g.put_levels(t, rec, h);
+        int to = 0;
+        const int at = last - g.t0;
+        const bool mine = at >= 0 && at < g.own;
+        if (mine) {
+            const int put = g.slots[at].y;
+            to = (put != 0 ? put : t.dense_to[int64_t(h.dense_row) * V + last]) & kStateMask;
+        }
+        if (W > 1) {
+            if (mine && lane == 0) meet->b[turn][0] = to;
+            lds_barrier();
+            to = meet->b[turn][0];
+            turn ^= 1;
+        }
+        s = __builtin_amdgcn_readfirstlane(to);
+        rec = load_record(ri, s, lane);
+        if (dirty) g.clear_slots();
+        dirty = false;
+    }
+    if (threadIdx.x == 0) states[0] = s;
+
+    for (int k = 0; k < K; ++k) {
+        if (SAMPLE && k + 1 < K) {
+            noise_row += d.noise_k;
+            g.load_row(noise_row, noise_next);
+        }
+        const ChainHead h = head_of(rec);
+        g.load_dense(t, unsigned(h.dense_row), dw, dt);
+        dirty |= g.put_levels(t, rec, h);
+        float x[NT], r[NT], bx;
+        int nx[NT], bi;
+        g.lm_values(h, dw, dt, dirty, x, nx);
+        float m = -__builtin_inff(), total = 0.0f;   // of this wavefront's tokens
+        if (!FULL) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) x[i] = kWave * i + lane < g.own ? x[i] : -__builtin_inff();
+        }
+        if (SAMPLE) {
+            float lm = x[0];
+#pragma unroll
+            for (int i = 1; i < NT; ++i) lm = __builtin_fmaxf(lm, x[i]);
+            // a wavefront without tokens takes the lowest finite value: its terms are exp(-inf) = 0
+            m = __builtin_fmaxf(key_float(wave_max_u32(float_key(lm))), -3.4e38f);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const float w = expf((x[i] - m) * d.inv_temperature);
+                total += w;
+                // the noise of tokens past V reads as 0: 0 * inf is NaN and loses
+                r[i] = w * __builtin_amdgcn_rcpf(noise.f(i));
+            }
+            total = wave_sum(total);
+            if (!FULL) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) r[i] = kWave * i + lane < g.own ? r[i] : -__builtin_inff();
+            }
+            g.lane_best(r, bx, bi);
+        } else {
+            g.lane_best(x, bx, bi);
+        }
+        int to = nx[0];
+#pragma unroll
+        for (int i = 1; i < NT; ++i) to = bi == kWave * i ? nx[i] : to;
+        to &= kStateMask;
+        unsigned key = float_key(bx);
+        int token = g.t0 + bi + lane;
+        const int who = winner_lane(key, token);
+        if (W > 1) {
+            if (lane == who) {
+                const i32x4 e = {SAMPLE ? __float_as_int(bx) : int(key), token, to, __float_as_int(m)};
+                meet->a[turn][wave] = e;
+                meet->b[turn][wave] = __float_as_int(total);
+            }
+            lds_barrier();
+            const i32x4 e = meet->a[turn][lane & (W - 1)];
+            key = unsigned(e.x);
+            if (SAMPLE) {
+                const float part = __int_as_float(meet->b[turn][lane & (W - 1)]);
+                const float mw = __int_as_float(e.w);
+                m = key_float(max_over_waves<W>(float_key(mw)));
+                const float f = expf((mw - m) * d.inv_temperature);
+                total = sum_over_waves<W>(part * f);
+                // a wavefront without tokens keeps its -inf; inf * 0 (no noise, no weight) is NaN and loses
+                const float best = __int_as_float(e.x);
+                key = float_key(best > 0.0f ? or_lowest(best * f) : best);
+            }
+            turn ^= 1;
+            const int w = winner_entry<W>(key, e.y);
+            token = __builtin_amdgcn_readlane(e.y, w);
+            to = __builtin_amdgcn_readlane(e.z, w);
+        } else {
+            token = __builtin_amdgcn_readlane(token, who);
+            to = __builtin_amdgcn_readlane(to, who);
+        }
+        s = to;
+        if (k + 1 < K) rec = load_record(ri, s, lane);
+        if (dirty) g.clear_slots();
+        dirty = false;
+        if (rows) {
+            const float log_total = logf(total);
+            float *row = rows + int64_t(k) * V + g.t0;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                if (FULL || kWave * i + lane < g.own)
+                    row[kWave * i + lane] = (x[i] - m) * d.inv_temperature - log_total;
+        }
+        if (threadIdx.x == 0) {
+            tokens[k] = token;
+            states[k + 1] = s;
+        }
+        if (SAMPLE) noise = noise_next;
+    }
+}
+
+template <int W, int NT, bool FULL, bool SAMPLE>
+static hipError_t launch_group(Draft d, int64_t B, hipStream_t stream) {
+    // a grid holds at most 2^32 - 1 work-items: larger batches go in several launches
+    constexpr int64_t kMost = int64_t(UINT32_MAX) / (W * kWave);
+    const size_t lds = sizeof(Meet) + size_t(W) * kWave * NT * sizeof(i32x2);
+    for (int64_t b0 = 0; b0 < B; b0 += kMost) {
+        Draft p = d;
+        p.states += b0;
+        if (p.last) p.last += b0;
+        if (SAMPLE) p.noise += b0 * d.noise_b;
+        p.tokens += b0 * d.K;
+        p.draft_states += b0 * (d.K + 1);
+        if (p.logprobs) p.logprobs += b0 * d.K * d.t.vocab_size;
+        hipLaunchKernelGGL((draft_kernel<W, NT, FULL, SAMPLE>), dim3(unsigned(B - b0 < kMost ? B - b0 : kMost)),
+                           dim3(W * kWave), lds, stream, p);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <int W, int NT>
+static hipError_t launch_group(const Draft &d, int64_t B, hipStream_t stream) {
+    const bool full = d.t.vocab_size == W * kWave * NT;
+    if (d.noise)
+        return full ? launch_group<W, NT, true, true>(d, B, stream) : launch_group<W, NT, false, true>(d, B, stream);
+    return full ? launch_group<W, NT, true, false>(d, B, stream) : launch_group<W, NT, false, false>(d, B, stream);
+}
+
+hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *last, int64_t B, int K,
+                        float temperature, const float *noise, int64_t noise_b, int64_t noise_k, int32_t *tokens,
+                        int32_t *draft_states, float *logprobs, hipStream_t stream) {
+    const bool sample = temperature > 0.0f;
+    const Draft d{t, states, last, sample ? noise : nullptr, noise_b, noise_k, K, sample ? 1.0f / temperature : 0.0f,
+                  tokens, draft_states, sample ? logprobs : nullptr};
+    const int V = t.vocab_size;
+    if (V <= 256) return launch_group<1, 4>(d, B, stream);
+    if (V <= 512) return launch_group<1, 8>(d, B, stream);
+    if (V <= 1024) return launch_group<4, 4>(d, B, stream);
+    if (V <= 2048) return launch_group<8, 4>(d, B, stream);
+    if (V <= 4096) return launch_group<8, 8>(d, B, stream);
+    return launch_group<16, 8>(d, B, stream);
+}
+
+}  // namespace ngpu

@@ -1,0 +1,266 @@
+"""Appending to the paged cache against its definition in 64 bits.
+
+A rotated element is a cos - b sin in fp32 (three roundings, at most 2^-22 of
+|a| + |b|), rounded once to the type: half an ulp, at most 2^-8 of its size for
+bfloat16 (8 bits) and 2^-11 (11 bits; 2^-25 below the normal range) for half.  Copied
+elements and everything that is not written have to be equal.
+"""
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import paper_2505_22857_amd as ng  # noqa: E402
+import serving_reference as ref  # noqa: E402
+
+F16, BF16 = torch.float16, torch.bfloat16
+UNIT = {F16: 2.0 ** -11, BF16: 2.0 ** -8}
+HALF, INTER = ng.NGPU_ROPE_HALF, ng.NGPU_ROPE_INTERLEAVED
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+
+
+def randn(rng, dtype, *shape):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).cuda().to(dtype)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def host(x):
+    return x.double().cpu().numpy()
+
+
+def check(S=3, T=4, H=2, Hq=4, D=64, rotary=64, layout=HALF, page=8, dtype=BF16, start=None, lengths=None,
+          positions=None, tables=None, query=True, qkv=None, caches=None, rows=64, seed=0):
+    rng = np.random.default_rng(seed)
+    width = 6
+    print(f"[case] append S={S} T={T} H={H}/{Hq} D={D} R={rotary} {layout} page={page} {dtype}", flush=True)
+    k, v = randn(rng, dtype, S, T, H, D), randn(rng, dtype, S, T, H, D)
+    q = randn(rng, dtype, S, T, Hq, D) if query else None
+    if qkv is not None:
+        q, k, v = qkv(q, k, v)
+    P = S * width + 2
+    kc, vc = (caches or (lambda *s: (randn(rng, dtype, *s), randn(rng, dtype, *s))))(P, page, H, D)
+    tables = rng.permutation(P)[:S * width].reshape(S, width) if tables is None else np.asarray(tables)
+    start = rng.integers(0, max(1, width * page - T), S) if start is None else np.asarray(start)
+    cos, sin = ng.rope_table(rows, rotary) if rotary else (None, None)
+    pos = start[:, None] + np.arange(T) if positions is None else np.asarray(positions)
+    want_k, want_v = host(kc), host(vc)
+    slack_k = np.zeros_like(want_k)
+    want_q, slack_q = (np.zeros(q.shape), np.zeros(q.shape)) if query else (None, None)
+    hk, hv, hq = host(k), host(v), host(q) if query else None
+    u = UNIT[dtype]
+
+    def turned(x, p):
+        """The rotated heads and what they may be off by."""
+        y, slack = x.copy(), np.zeros_like(x)
+        if rotary == 0:
+            return y, slack
+        if not 0 <= p < rows:
+            y[..., :rotary] = np.nan
+            return y, slack
+        c, s = host(cos)[p], host(sin)[p]
+        y = ref.rotate(x, c, s, layout)
+        size = 2 * np.abs(x).max()   # no less than |a| + |b| of any pair
+        slack[..., :rotary] = (u * np.abs(y) + 2.0 ** -22 * size + 2.0 ** -25)[..., :rotary]
+        return y, slack
+
+    for s in range(S):
+        for t in range(T if lengths is None else min(max(lengths[s], 0), T)):
+            if query:
+                want_q[s, t], slack_q[s, t] = turned(hq[s, t], pos[s, t])
+            place = int(start[s]) + t
+            if not 0 <= place < tables.shape[1] * page or not 0 <= tables[s, place // page] < P:
+                continue
+            at = tables[s, place // page], place % page
+            want_k[at], slack_k[at] = turned(hk[s, t], pos[s, t])
+            want_v[at] = hv[s, t]
+    kw = {} if rotary == 0 else dict(cos=cos, sin=sin, layout=layout,
+                                     positions=None if positions is None else ints(pos))
+    out = ng.kv_append(k, v, kc, vc, ints(tables), ints(start), q=q, lengths=None if lengths is None else ints(lengths),
+                       **kw)
+    assert np.array_equal(host(vc), want_v)
+
+    def near(got, want, slack):
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        with np.errstate(invalid="ignore"):
+            assert not (np.abs(got - want) > slack).any()
+
+    near(host(kc), want_k, slack_k)
+    if query:
+        near(host(out), want_q, slack_q)
+    else:
+        assert out is None
+
+
+@pytest.mark.parametrize("D,rotary", [(64, 64), (64, 32), (128, 128), (128, 64), (80, 80), (80, 32), (96, 48), (256, 256),
+                                      (256, 32), (2, 2), (10, 6), (24, 24), (33, 32), (1, 0), (72, 8), (128, 16),
+                                      (64, 0), (40, 24)])
+@pytest.mark.parametrize("layout", [HALF, INTER])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_dimensions(D, rotary, layout, dtype):
+    check(D=D, rotary=rotary, layout=layout, dtype=dtype, seed=D + rotary)
+    check(D=D, rotary=rotary, layout=layout, dtype=dtype, S=1, T=1, H=1, Hq=1, page=1, seed=D)
+
+
+@pytest.mark.parametrize("H,Hq", [(1, 1), (1, 8), (3, 9), (8, 32), (5, 5)])
+@pytest.mark.parametrize("T", [1, 2, 7, 33])
+def test_heads_and_tokens(H, Hq, T):
+    check(H=H, Hq=Hq, T=T, page=16, D=128, rotary=64, seed=T)
+    check(H=H, Hq=Hq, T=T, page=7, query=False, seed=T)
+
+
+def test_lengths_places_and_pages():
+    """Tokens that do not count, places past the table or below it, pages outside the cache."""
+    check(S=6, T=5, lengths=[0, 1, 5, -2, 99, 3])
+    check(S=5, T=5, start=[44, 47, 48, -3, 2 ** 31 - 3], rows=64)
+    tables = np.random.default_rng(1).permutation(32)[:30].reshape(5, 6)
+    tables[0, 0], tables[1, 1], tables[2, 2], tables[3, :] = -1, 32, 2 ** 31 - 1, -(2 ** 31)
+    check(S=5, T=20, tables=tables, start=[0, 3, 9, 2, 20])
+    check(S=2, T=3, tables=np.zeros((2, 0), np.int64), start=[0, 1])
+
+
+@pytest.mark.parametrize("layout", [HALF, INTER])
+def test_positions(layout):
+    """Positions of their own (after a prefix, repeated), the last row, and rows outside the table: NaN."""
+    check(positions=[[9, 9, 0, 63], [1, 2, 3, 4], [60, 61, 62, 63]], layout=layout)
+    check(positions=[[-1, 5, 64, 2 ** 31 - 1], [0, 1, 2, -5], [7, 7, 7, 7]], layout=layout)
+    check(start=[61, 0, 30], page=16, layout=layout, rows=64)
+
+
+@pytest.mark.parametrize("D,rotary,off", [(64, 64, 0), (128, 64, 8), (64, 64, 1), (128, 32, 4), (80, 48, 3)])
+@pytest.mark.parametrize("layout", [HALF, INTER])
+def test_strides(D, rotary, off, layout):
+    """Heads split from one projection, at any offset; token-major inputs; caches of any layout."""
+    def split(q, k, v):
+        S, T, Hq, H = *q.shape[:3], k.shape[2]
+        wide = torch.zeros(S, T, (Hq + 2 * H) * D + off + 3, dtype=q.dtype, device="cuda")
+        part = wide[..., off:off + (Hq + 2 * H) * D]
+        views = [p.unflatten(-1, (-1, D)) for p in part.split((Hq * D, H * D, H * D), -1)]
+        for view, x in zip(views, (q, k, v)):
+            view.copy_(x)
+        return views
+
+    def heads_first(P, page, H, D):
+        return [torch.randn(P, H, page, D, device="cuda").to(BF16).transpose(1, 2) for _ in range(2)]
+
+    def together(P, page, H, D):
+        return list(torch.randn(P, page, H, 2 * D + off, device="cuda").to(BF16)[..., off:].split(D, -1))
+
+    check(D=D, rotary=rotary, layout=layout, qkv=split)
+    check(D=D, rotary=rotary, layout=layout, qkv=split, caches=heads_first)
+    check(D=D, rotary=rotary, layout=layout, caches=together)
+    check(D=D, rotary=rotary, layout=layout,
+          qkv=lambda q, k, v: [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v)])
+    check(D=D, rotary=rotary, layout=layout, qkv=lambda q, k, v: [x[:, :, :1].expand(x.shape) for x in (q, k, v)])
+
+
+def test_values_that_are_not_finite():
+    for layout in (HALF, INTER):
+        k = torch.ones(1, 2, 1, 64, dtype=F16, device="cuda")
+        k[0, 0, 0, 3], k[0, 1, 0, 40] = float("nan"), float("inf")
+        kc, vc = (torch.zeros(1, 4, 1, 64, dtype=F16, device="cuda") for _ in range(2))
+        cos, sin = ng.rope_table(8, 32)
+        ng.kv_append(k, k, kc, vc, ints([[0]]), ints([1]), cos=cos, sin=sin, layout=layout)
+        bad = torch.isnan(kc[0, 1, 0]).nonzero()[:, 0].tolist()
+        assert bad == ([3, 19] if layout == HALF else [2, 3])
+        assert kc[0, 2, 0, 40] == float("inf") and torch.isfinite(kc[0, 2, 0, :40]).all()
+        assert torch.equal(vc[0, 1:3, 0].nan_to_num(7, 8), k[0, :, 0].nan_to_num(7, 8))
+
+
+def test_offsets_past_32_bits():
+    """A cache whose pages lie past 2^31 elements."""
+    pages, page, H, D = 3, 16, 2, 64
+    stride = (1 << 30) + 128
+    kc, vc = (torch.empty(2 * stride + page * H * D, dtype=F16, device="cuda").as_strided(
+        (pages, page, H, D), (stride, H * D, D, 1)) for _ in range(2))
+    kc.zero_(), vc.zero_()
+    k, v = (torch.randn(1, 20, H, D, device="cuda").half() for _ in range(2))
+    ng.kv_append(k, v, kc, vc, ints([[0, 2]]), ints([10]))
+    assert torch.equal(kc[0, 10:], k[0, :6]) and torch.equal(kc[2, :14], k[0, 6:])
+    assert torch.equal(vc[0, 10:], v[0, :6]) and torch.equal(vc[2, :14], v[0, 6:])
+    assert not kc[1].any() and not kc[2, 14:].any()
+
+
+def test_other_stream_and_graph():
+    kc, vc = (torch.zeros(8, 16, 2, 64, dtype=F16, device="cuda") for _ in range(2))
+    k, v, q = (torch.randn(2, 3, 2, 64, device="cuda").half() for _ in range(3))
+    cos, sin = ng.rope_table(64, 64)
+    args = dict(pages=ints([[0, 1], [2, 3]]), start=ints([14, 5]), cos=cos, sin=sin, q=q)
+    want = ng.kv_append(k, v, kc, vc, **args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = ng.kv_append(k, v, kc, vc, **args, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = ng.kv_append(k, v, kc, vc, **args)
+    for i in range(4):
+        q.mul_(-0.5)
+        k.add_(1)
+        kc.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        mine = kc.clone()
+        kc.zero_()
+        assert torch.equal(held, ng.kv_append(k, v, kc, vc, **args)) and torch.equal(mine, kc) and kc.any(), i
+
+
+def test_long_prompt():
+    check(S=2, T=300, H=4, Hq=8, D=128, rotary=128, page=64, start=[0, 17], rows=400, lengths=[300, 211])
+
+
+def test_rope_table():
+    cos, sin = ng.rope_table(5, 4, base=100.0, scale=2.0, device="cpu")
+    angle = np.arange(5)[:, None] / 2.0 * np.array([1.0, 0.1])
+    assert np.array_equal(cos.numpy(), np.cos(angle).astype(np.float32))
+    assert np.array_equal(sin.numpy(), np.sin(angle).astype(np.float32))
+    cos, _ = ng.rope_table(3, 4, frequencies=[0.5, 0.25], device="cpu")
+    assert np.array_equal(cos.numpy(), np.cos(np.arange(3)[:, None] * [0.5, 0.25]).astype(np.float32))
+    for bad in (dict(rotary=3), dict(rotary=-2), dict(rotary=4, frequencies=[1.0])):
+        with pytest.raises(ValueError):
+            ng.rope_table(4, device="cpu", **bad)
+
+
+def test_refusals():
+    kc, vc = (torch.zeros(4, 8, 2, 16, dtype=F16, device="cuda") for _ in range(2))
+    k = torch.zeros(2, 3, 2, 16, dtype=F16, device="cuda")
+    pages, start = ints([[0, 1], [2, 3]]), ints([0, 0])
+    cos, sin = ng.rope_table(16, 16)
+    ok = dict(k=k, v=k, k_cache=kc, v_cache=vc, pages=pages, start=start, cos=cos, sin=sin, q=k)
+    ng.kv_append(**ok)
+
+    def bad(error, **kw):
+        with pytest.raises(error):
+            ng.kv_append(**{**ok, **kw})
+
+    bad(TypeError, k=k.float())
+    bad(TypeError, v=k.cpu())
+    bad(ValueError, v=k[:, :2])
+    bad(ValueError, k=k[0])
+    bad(TypeError, k_cache=kc.float())
+    bad(ValueError, v_cache=vc[:3])
+    bad(TypeError, v_cache=vc.to(BF16))
+    bad(TypeError, k=k.transpose(2, 3).contiguous().transpose(2, 3))
+    bad(TypeError, pages=pages.long())
+    bad(ValueError, pages=pages[:1])
+    bad(ValueError, start=start[:1])
+    bad(ValueError, lengths=start[:1])
+    bad(ValueError, positions=start)
+    bad(ValueError, sin=None)
+    bad(ValueError, sin=sin[:, :4])
+    bad(TypeError, cos=cos.double(), sin=sin.double())
+    bad(ValueError, q=k[..., :8])
+    bad(ng.NgpuError, layout=2)
+    wide = torch.zeros(16, 9, device="cuda")
+    bad(ng.NgpuError, cos=wide, sin=wide)   # more dimensions than a head has
+    assert ng.kv_append(**{**ok, "k": k[:, :0], "v": k[:, :0], "q": k[:, :0]}).shape == (2, 0, 2, 16)
