@@ -1,32 +1,13 @@
-// Attention over a paged cache with a prefix that a group of sequences shares.
+// Attention over a paged cache with a prefix that a group of sequences shares:
+// the kernels' choice and launches, the kernel for dimensions and strides that
+// the matrix kernel (attend_tile.h) does not take, and the join of a row's parts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
-#include "cache.h"
-#include "walk.h"
+#include "attend_tile.h"
 
 namespace ngpu {
-
-struct Attend {
-    ngpu_kv_cache_t c;
-    ngpu_attend_t a;
-};
-
-__device__ __forceinline__ int64_t query_length(const ngpu_attend_t &a, int64_t s) {
-    return a.q_lengths ? min(max(int64_t(a.q_lengths[s]), int64_t(0)), a.T) : a.T;
-}
-__device__ __forceinline__ PageTable prefix_of(const Attend &p, int64_t s) {
-    if (p.a.G == 0) return {nullptr, 0};
-    const int64_t g = s / (p.a.S / p.a.G);
-    const int64_t n = max(int64_t(p.a.prefix_lengths[g]), int64_t(0));
-    return {p.a.prefix_pages + g * p.a.prefix_stride, min(n, p.a.prefix_width * p.c.page_size)};
-}
-__device__ __forceinline__ PageTable own_of(const Attend &p, int64_t s) {
-    if (!p.a.pages) return {nullptr, 0};
-    const int64_t n = max(int64_t(p.a.lengths[s]), int64_t(0));
-    return {p.a.pages + s * p.a.pages_stride, min(n, p.a.pages_width * p.c.page_size)};
-}
 
 constexpr int kRowWaves = 4;
 constexpr int kMostDims = NGPU_LM_MAX_HEAD_DIM / kWave;   // dimensions a lane holds
@@ -79,9 +60,14 @@ __global__ __launch_bounds__(kRowWaves * kWave) void attend_row_kernel(Attend p,
         }
     };
     if (t < nq) {
-        const PageTable prefix = prefix_of(p, s), own = own_of(p, s);
-        attend(prefix, prefix.count);
-        attend(own, min(own.count, own.count - nq + t + 1));
+        if (a.G > 0) {
+            const PageTable prefix = prefix_table(p, s / (a.S / a.G));
+            attend(prefix, prefix.count);
+        }
+        if (a.pages) {
+            const PageTable own = own_table(p, s);
+            attend(own, min(own.count, own.count - nq + t + 1));
+        }
     }
     __shared__ float part[kRowWaves][2], sums[kRowWaves][NGPU_LM_MAX_HEAD_DIM];
     if (lane == 0) part[wave][0] = m, part[wave][1] = sum;
@@ -102,7 +88,7 @@ __global__ __launch_bounds__(kRowWaves * kWave) void attend_row_kernel(Attend p,
 }
 
 template <class T>
-static hipError_t launch(const Attend &p, hipStream_t stream) {
+static hipError_t launch_rows(const Attend &p, hipStream_t stream) {
     constexpr int64_t kMost = int64_t(UINT32_MAX) / (kRowWaves * kWave);
     const int64_t rows = p.a.S * p.a.T * p.a.q_heads;
     for (int64_t r0 = 0; r0 < rows; r0 += kMost) {
@@ -113,11 +99,175 @@ static hipError_t launch(const Attend &p, hipStream_t stream) {
     return hipSuccess;
 }
 
-size_t attend_workspace(const ngpu_kv_cache_t &, const ngpu_attend_t &) { return 0; }
+// A row's parts joined: each thread takes 4 dimensions of one row.
+constexpr int kJoinThreads = 256;
+template <class T>
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(Attend p, AttendPlan plan, int64_t rows, int lanes,
+                                                                   int64_t row0) {
+    const ngpu_attend_t &a = p.a;
+    const int D = p.c.dim, d = int(threadIdx.x) % lanes * 4;
+    const int64_t row = row0 + int64_t(blockIdx.x) * (kJoinThreads / lanes) + int(threadIdx.x) / lanes;
+    if (row >= rows || d >= D) return;
+    float top = -__builtin_inff(), sum = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t token = row / a.q_heads;
+    if (token % a.T < query_length(a, token / a.T)) {
+        for (int i = 0; i < plan.parts; ++i) top = __builtin_fmaxf(top, plan.stats[i * rows + row].x);
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+        for (int i = 0; i < plan.parts; ++i) {
+            const float2 s = plan.stats[i * rows + row];
+            if (s.y == 0.0f) continue;   // no key in this part (a NaN sum goes on)
+            const float f = s.x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s.x - base);
+            sum += s.y * f;
+            o += *reinterpret_cast<const f32x4 *>(plan.sums + (i * rows + row) * D + d) * f;
+        }
+    }
+    const bool any = sum != 0.0f;
+    if (a.lse && d == 0)
+        a.lse[row] = any ? (top == -__builtin_inff() ? sum : top * 0.69314718056f + logf(sum)) : -__builtin_inff();
+    const float f = 1.0f / sum;
+    s16x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = any ? short(from_float<T>(o[i] * f).bits) : short(0);
+    *reinterpret_cast<s16x4 *>(static_cast<T *>(a.out) + row * D + d) = y;
+}
 
-hipError_t launch_attend(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, void *, hipStream_t stream) {
+namespace {
+
+constexpr int kCus = 256;   // of an MI355X
+
+// Which kernel takes a call, and how it is cut.
+struct Choice {
+    bool tiles;              // the matrix kernel takes it
+    int steps;               // 32-dimension steps of a head: 2, 3, 4, 8
+    int prefix_tiles, own_tiles;      // 16-row tiles a wavefront
+    int prefix_waves, own_waves;      // wavefronts along rows: 1, 2, 4
+    AttendPlan plan;
+};
+
+// The matrix kernel loads 16 bytes of 8 elements at a time and keeps a row of
+// the cache as a 32-bit number of them.
+bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
+    const int64_t strides[] = {c.k_stride_page, c.k_stride_token, c.k_stride_head,
+                               c.v_stride_page, c.v_stride_token, c.v_stride_head};
+    for (const int64_t s : strides)
+        if (s % 8 != 0) return false;
+    constexpr int64_t kMost = int64_t(1) << 31;   // 16-byte units: pages and tokens each stay below half the range
+    const int64_t pages = std::max<int64_t>(c.num_pages, 1);
+    return c.dim % 8 == 0 && reinterpret_cast<uintptr_t>(c.k) % 16 == 0 && reinterpret_cast<uintptr_t>(c.v) % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && c.k_stride_page / 8 <= kMost / pages &&
+           c.v_stride_page / 8 <= kMost / pages && c.k_stride_token / 8 <= kMost / c.page_size &&
+           c.v_stride_token / 8 <= kMost / c.page_size && a.T <= (1 << 24);
+}
+
+void cut_rows(int64_t rows, int steps, int &tiles, int &waves, int &blocks) {
+    const int most = steps > 4 ? 2 : 3;
+    tiles = rows <= 16 ? 1 : 2;
+    waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : 4);
+    if (rows > 128 && most == 3) tiles = 3;
+    blocks = int((rows + 16 * tiles * waves - 1) / (16 * tiles * waves));
+}
+
+Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace) {
+    Choice r{};
+    r.tiles = takes_tiles(c, a);
+    if (!r.tiles) return r;
+    r.steps = c.dim <= 64 ? 2 : (c.dim <= 96 ? 3 : (c.dim <= 128 ? 4 : 8));
+    const int64_t rep = a.q_heads / c.heads;
+    auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int &tiles, int &waves) {
+        Cut u{problems, 0, 0};
+        cut_rows(rows, r.steps, tiles, waves, u.blocks);
+        const int64_t tile = waves == 1 && r.steps <= 4 ? 128 : 64;
+        const int64_t have = problems * u.blocks, wanted = waves == 4 ? 2 * kCus : kCus;
+        const int64_t most = std::max<int64_t>(1, (most_keys + 2 * tile - 1) / (2 * tile));
+        u.splits = int(std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, wanted / have)));
+        return u;
+    };
+    if (a.G > 0)
+        r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size, r.prefix_tiles,
+                            r.prefix_waves);
+    if (a.pages) r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, r.own_tiles, r.own_waves);
+    r.plan.parts = r.plan.prefix.splits + r.plan.own.splits;
+    const int64_t rows = a.S * a.T * a.q_heads;
+    r.plan.sums = reinterpret_cast<float *>(workspace);
+    r.plan.stats = reinterpret_cast<float2 *>(workspace + size_t(r.plan.parts) * size_t(rows) * c.dim * 4);
+    return r;
+}
+
+template <class T, int DK, int RT, int WR, int WK>
+hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int64_t w1, hipStream_t stream) {
+    using A = AttendTile<T, DK, RT, WR, WK>;
+    constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
+    static const hipError_t ready = hipFuncSetAttribute(
+        reinterpret_cast<const void *>(&attend_tile_kernel<T, DK, RT, WR, WK>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, A::kLds);
+    if (ready != hipSuccess) return ready;
+    for (; w0 < w1; w0 += kMost) {
+        hipLaunchKernelGGL((attend_tile_kernel<T, DK, RT, WR, WK>), dim3(unsigned(std::min(kMost, w1 - w0))),
+                           dim3(64 * WR * WK), A::kLds, stream, p, plan, w0);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <class T, int DK>
+hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int tiles, int waves, int64_t w0, int64_t w1,
+                       hipStream_t stream) {
+    constexpr int kSplit = DK <= 4 ? 4 : 2;   // wavefronts along keys: two stages of their tiles fill the LDS
+    if (waves == 1)
+        return tiles == 1 ? launch_tile<T, DK, 1, 1, kSplit>(p, plan, w0, w1, stream)
+                          : launch_tile<T, DK, 2, 1, kSplit>(p, plan, w0, w1, stream);
+    if (waves == 2) return launch_tile<T, DK, 2, 2, 2>(p, plan, w0, w1, stream);
+    if constexpr (DK <= 4)
+        if (tiles == 3) return launch_tile<T, DK, 3, 4, 1>(p, plan, w0, w1, stream);
+    return launch_tile<T, DK, 2, 4, 1>(p, plan, w0, w1, stream);
+}
+template <class T>
+hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, int64_t w0, int64_t w1,
+                       hipStream_t stream) {
+    switch (r.steps) {
+        case 2: return launch_tile<T, 2>(p, r.plan, tiles, waves, w0, w1, stream);
+        case 3: return launch_tile<T, 3>(p, r.plan, tiles, waves, w0, w1, stream);
+        case 4: return launch_tile<T, 4>(p, r.plan, tiles, waves, w0, w1, stream);
+        default: return launch_tile<T, 8>(p, r.plan, tiles, waves, w0, w1, stream);
+    }
+}
+
+template <class T>
+hipError_t launch(const Attend &p, void *workspace, hipStream_t stream) {
+    const ngpu_attend_t &a = p.a;
+    const Choice r = choose(p.c, a, static_cast<char *>(workspace));
+    if (!r.tiles) return launch_rows<T>(p, stream);
+    const int64_t prefix = r.plan.prefix.works(), all = prefix + r.plan.own.works();
+    if (prefix > 0)
+        if (const hipError_t e = launch_tile<T>(p, r, r.prefix_tiles, r.prefix_waves, 0, prefix, stream);
+            e != hipSuccess)
+            return e;
+    if (all > prefix)
+        if (const hipError_t e = launch_tile<T>(p, r, r.own_tiles, r.own_waves, prefix, all, stream); e != hipSuccess)
+            return e;
+    if (r.plan.parts == 1) return hipSuccess;
+    int lanes = 2;   // threads a row
+    while (4 * lanes < p.c.dim) lanes *= 2;
+    const int64_t rows = a.S * a.T * a.q_heads, per = kJoinThreads / lanes, kMost = int64_t(1) << 23;
+    for (int64_t r0 = 0; r0 < rows; r0 += kMost * per) {
+        const int64_t groups = std::min(kMost, (rows - r0 + per - 1) / per);
+        hipLaunchKernelGGL((attend_join_kernel<T>), dim3(unsigned(groups)), dim3(kJoinThreads), 0, stream, p, r.plan,
+                           rows, lanes, r0);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t attend_workspace(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
+    const Choice r = choose(c, a, nullptr);
+    return r.tiles && r.plan.parts > 1 ? size_t(r.plan.parts) * size_t(a.S * a.T * a.q_heads) * (size_t(c.dim) * 4 + 8) : 0;
+}
+
+hipError_t launch_attend(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, void *workspace, hipStream_t stream) {
     const Attend p{c, a};
-    return c.dtype == NGPU_F16 ? launch<F16>(p, stream) : launch<Bf16>(p, stream);
+    return c.dtype == NGPU_F16 ? launch<F16>(p, workspace, stream) : launch<Bf16>(p, workspace, stream);
 }
 
 }  // namespace ngpu
