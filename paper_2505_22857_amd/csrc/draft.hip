@@ -15,48 +15,18 @@
 // by reading the noise and writing the rows (8 bytes a token).
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-#include <type_traits>
-
-#include "group.h"
+#include "reduce.h"
 
 namespace ngpu {
 
-// The inverse of float_key.
-__device__ __forceinline__ float key_float(unsigned k) {
-    return __int_as_float(int(k ^ (~unsigned(int(k) >> 31) | 0x80000000u)));
-}
-
-// Sum over W values that repeat every W lanes: pairs, then pairs of pairs, so
-// every lane adds the same numbers in the same order.
-template <int W>
-__device__ __forceinline__ float sum_over_waves(float x) {
-    auto moved = [](float v, auto ctrl) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
-    };
-    if (W >= 2) x += moved(x, std::integral_constant<int, 0xB1>{});    // lane ^ 1
-    if (W >= 4) x += moved(x, std::integral_constant<int, 0x4E>{});    // lane ^ 2
-    if (W >= 8) x += moved(x, std::integral_constant<int, 0x141>{});   // other half of 8
-    if (W >= 16) x += moved(x, std::integral_constant<int, 0x140>{});  // other half of 16
-    return x;
-}
-
-// Sum over the wavefront, in a fixed order, uniform in every lane.
-__device__ __forceinline__ float wave_sum(float x) {
-    x = sum_over_waves<16>(x);   // of each row of 16 lanes
-    float r = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kWave; i += 16) r += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
-    return r;
-}
-
 struct Draft {
     DevTrie t;
+    int uni_base;   // dense row of the state entered by token w: uni_base + w, or -1: the row's head says it
     const int32_t *states, *last;
     const float *noise;
     int64_t noise_b, noise_k;
     int K;
-    float inv_temperature;
+    float to_log2;   // log2 e / temperature
     int32_t *tokens, *draft_states;
     float *logprobs;
 };
@@ -93,6 +63,14 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
     g.clear_slots();
     bool dirty = false;
     int turn = 0;   // of the meeting point's two buffers
+    // The record of the state entered by `token` and, where the token alone names it, the dense row.
+    auto enter = [&](int token) {
+        rec = load_record(ri, s, lane);
+        if (dirty) g.clear_slots();
+        dirty = false;
+        g.load_dense(t, d.uni_base >= 0 ? unsigned(d.uni_base + token) : unsigned(__builtin_amdgcn_readlane(rec.x, 0)), dw,
+                     dt);
+    };
 
     if (last >= 0) {   // the state after `last`, whose wavefront finds it
         const ChainHead h = head_of(rec);
@@ -111,9 +89,9 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
             turn ^= 1;
         }
         s = __builtin_amdgcn_readfirstlane(to);
-        rec = load_record(ri, s, lane);
-        if (dirty) g.clear_slots();
-        dirty = false;
+        enter(last);
+    } else {
+        g.load_dense(t, unsigned(__builtin_amdgcn_readlane(rec.x, 0)), dw, dt);
     }
     if (threadIdx.x == 0) states[0] = s;
 
@@ -123,7 +101,6 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
             g.load_row(noise_row, noise_next);
         }
         const ChainHead h = head_of(rec);
-        g.load_dense(t, unsigned(h.dense_row), dw, dt);
         dirty |= g.put_levels(t, rec, h);
         float x[NT], r[NT], bx;
         int nx[NT], bi;
@@ -138,10 +115,10 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
 #pragma unroll
             for (int i = 1; i < NT; ++i) lm = __builtin_fmaxf(lm, x[i]);
             // a wavefront without tokens takes the lowest finite value: its terms are exp(-inf) = 0
-            m = __builtin_fmaxf(key_float(wave_max_u32(float_key(lm))), -3.4e38f);
+            m = __builtin_fmaxf(wave_max(lm), -3.4e38f);
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                const float w = expf((x[i] - m) * d.inv_temperature);
+                const float w = __builtin_amdgcn_exp2f((x[i] - m) * d.to_log2);
                 total += w;
                 // the noise of tokens past V reads as 0: 0 * inf is NaN and loses
                 r[i] = w * __builtin_amdgcn_rcpf(noise.f(i));
@@ -175,7 +152,7 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
                 const float part = __int_as_float(meet->b[turn][lane & (W - 1)]);
                 const float mw = __int_as_float(e.w);
                 m = key_float(max_over_waves<W>(float_key(mw)));
-                const float f = expf((mw - m) * d.inv_temperature);
+                const float f = __builtin_amdgcn_exp2f((mw - m) * d.to_log2);
                 total = sum_over_waves<W>(part * f);
                 // a wavefront without tokens keeps its -inf; inf * 0 (no noise, no weight) is NaN and loses
                 const float best = __int_as_float(e.x);
@@ -190,16 +167,14 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
             to = __builtin_amdgcn_readlane(to, who);
         }
         s = to;
-        if (k + 1 < K) rec = load_record(ri, s, lane);
-        if (dirty) g.clear_slots();
-        dirty = false;
+        if (k + 1 < K) enter(token);
         if (rows) {
-            const float log_total = logf(total);
+            const float log_total = __builtin_amdgcn_logf(total), ln2 = 0.693147180559945f;   // (v_log_f32 is log2)
             float *row = rows + int64_t(k) * V + g.t0;
 #pragma unroll
             for (int i = 0; i < NT; ++i)
                 if (FULL || kWave * i + lane < g.own)
-                    row[kWave * i + lane] = (x[i] - m) * d.inv_temperature - log_total;
+                    row[kWave * i + lane] = ((x[i] - m) * d.to_log2 - log_total) * ln2;
         }
         if (threadIdx.x == 0) {
             tokens[k] = token;
@@ -240,7 +215,10 @@ hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *
                         float temperature, const float *noise, int64_t noise_b, int64_t noise_k, int32_t *tokens,
                         int32_t *draft_states, float *logprobs, hipStream_t stream) {
     const bool sample = temperature > 0.0f;
-    const Draft d{t, states, last, sample ? noise : nullptr, noise_b, noise_k, K, sample ? 1.0f / temperature : 0.0f,
+    // as the whole decode: order-1 states are numbered by token when every token has a unigram
+    const int n1 = (t.max_order > 2 ? t.first[2] : t.num_states) - 1;
+    const int uni = t.max_order > 1 && n1 == t.vocab_size + (t.final_w ? 1 : 0) ? 1 : -1;
+    const Draft d{t, uni, states, last, sample ? noise : nullptr, noise_b, noise_k, K, sample ? 1.44269504088896f / temperature : 0.0f,
                   tokens, draft_states, sample ? logprobs : nullptr};
     const int V = t.vocab_size;
     if (V <= 256) return launch_group<1, 4>(d, B, stream);
