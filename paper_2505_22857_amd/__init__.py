@@ -137,6 +137,9 @@ def _load_fast():
         lib = load_library()
         mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                    (lib.ngpu_lm_advance, lib.ngpu_lm_fused_greedy_step, lib.ngpu_lm_fused_topk)))
+        mod.bind_serving(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                           (lib.ngpu_lm_draft, lib.ngpu_lm_verify_workspace, lib.ngpu_lm_verify, lib.ngpu_lm_kv_append,
+                            lib.ngpu_lm_attend_workspace, lib.ngpu_lm_attend)))
         _fast = mod
     return _fast
 
@@ -424,6 +427,12 @@ class NgpuLM:
 
         Returns (tokens [B, k] int32, states before the draft and after each token [B, k + 1] int32,
         log-probabilities [B, k, V] float32, None at temperature 0)."""
+        if stream is None and self._fast is not None:
+            r = self._fast.draft(self._h.value, self.vocab_size, states, k, noise, float(temperature), last)
+            if r is not None:   # None: not the ordinary call, handled (or refused) below
+                if r.__class__ is int:
+                    _check(r)
+                return r
         import torch
         from .serving import MAX_DRAFT, _need, _on
         B, V, k, temperature = states.numel(), self.vocab_size, int(k), float(temperature)

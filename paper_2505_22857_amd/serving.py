@@ -14,7 +14,7 @@ import contextlib
 import ctypes
 import math
 
-from . import _check, _stream_handle, _torch_mod, load_library
+from . import _check, _fast_or_none, _stream_handle, _torch_mod, load_library
 
 NGPU_F32, NGPU_F16, NGPU_BF16 = 0, 1, 2
 NGPU_ROPE_HALF, NGPU_ROPE_INTERLEAVED = 0, 1
@@ -74,6 +74,17 @@ def _library():
     return _lib
 
 
+_native_module = None
+
+
+def _native():
+    """The native per-call module, False where it cannot be used (said once)."""
+    global _native_module
+    if _native_module is None:
+        _native_module = _fast_or_none() or False
+    return _native_module
+
+
 def _type_code(dtype):
     torch = _torch_mod()
     return {torch.float32: NGPU_F32, torch.float16: NGPU_F16, torch.bfloat16: NGPU_BF16}.get(dtype)
@@ -129,6 +140,13 @@ def verify(logits, tokens, logprobs=None, uniforms=None, noise=None, temperature
     Returns (tokens [B, K + 1] int32: the kept ones, the added one, then -1; kept tokens [B] int32; the
     n-gram state [B] int32 after the kept tokens, None without ``draft_states``).  The added token is the
     next draft's ``last``."""
+    native = _native()
+    if stream is None and native:
+        r = native.verify(logits, tokens, logprobs, uniforms, noise, float(temperature), lengths, draft_states)
+        if r is not None:   # None: not the ordinary call, handled (or refused) below
+            if r.__class__ is int:
+                _check(r)
+            return r
     torch = _torch_mod()
     dev = _device_of(logits, "logits")
     if logits.dim() != 3 or logits.shape[1] < 1:
@@ -196,6 +214,13 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
     ``sin`` [positions, rotary / 2] (``rope_table``) the first ``rotary`` dimensions of the keys, and of
     ``q`` [S, T, q heads, dim], are rotated by row ``positions[s, t]`` (without it: the token's place).
     Returns the rotated queries (zero where a token does not count), None without ``q``."""
+    native = _native()
+    if stream is None and native:
+        r = native.kv_append(k, v, k_cache, v_cache, pages, start, positions, cos, sin, layout, q, lengths)
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r if q is not None else None
     torch = _torch_mod()
     dev, cache = _cache(k_cache, v_cache)
     if k.dim() != 4:
@@ -242,6 +267,14 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
 
     Returns [S, T, q heads, dim] (zero where a row sees no key or does not count), and with
     ``return_lse`` the log of each row's softmax sum [S, T, q heads] float32 (-inf there)."""
+    native = _native()
+    if stream is None and native and not return_lse:
+        r = native.attend(q, k_cache, v_cache, pages, lengths, prefix_pages, prefix_lengths, q_lengths,
+                          scale if scale is None else float(scale))
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r
     torch = _torch_mod()
     dev, cache = _cache(k_cache, v_cache)
     if q.dim() != 4:
