@@ -112,14 +112,31 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(Attend p, Att
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     const int64_t token = row / a.q_heads;
     if (token % a.T < query_length(a, token / a.T)) {
-        for (int i = 0; i < plan.parts; ++i) top = __builtin_fmaxf(top, plan.stats[i * rows + row].x);
+        // eight parts at a time, so that their loads are in flight together; past the last: the last again, for nothing
+        constexpr int kBatch = 8;
+        const int n = plan.parts;
+        for (int i = 0; i < n; i += kBatch) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) top = __builtin_fmaxf(top, plan.stats[min(i + u, n - 1) * rows + row].x);
+        }
         const float base = top == -__builtin_inff() ? 0.0f : top;
-        for (int i = 0; i < plan.parts; ++i) {
-            const float2 s = plan.stats[i * rows + row];
-            if (s.y == 0.0f) continue;   // no key in this part (a NaN sum goes on)
-            const float f = s.x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s.x - base);
-            sum += s.y * f;
-            o += *reinterpret_cast<const f32x4 *>(plan.sums + (i * rows + row) * D + d) * f;
+        for (int i = 0; i < n; i += kBatch) {
+            float2 s[kBatch];
+            f32x4 x[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                s[u] = plan.stats[min(i + u, n - 1) * rows + row];
+                x[u] = *reinterpret_cast<const f32x4 *>(plan.sums + (min(i + u, n - 1) * rows + row) * D + d);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                // a part without a key (sum 0) has written no sums; a NaN sum goes on
+                const bool any = i + u < n && s[u].y != 0.0f;
+                const float f = s[u].x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s[u].x - base);
+                sum += any ? s[u].y * f : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += any ? x[u][e] * f : 0.0f;
+            }
         }
     }
     const bool any = sum != 0.0f;
@@ -157,14 +174,12 @@ bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
     return c.dim % 8 == 0 && reinterpret_cast<uintptr_t>(c.k) % 16 == 0 && reinterpret_cast<uintptr_t>(c.v) % 16 == 0 &&
            reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && c.k_stride_page / 8 <= kMost / pages &&
            c.v_stride_page / 8 <= kMost / pages && c.k_stride_token / 8 <= kMost / c.page_size &&
-           c.v_stride_token / 8 <= kMost / c.page_size && a.T <= (1 << 24);
+           c.v_stride_token / 8 <= kMost / c.page_size && a.S * a.T * a.q_heads < kMost / 256;
 }
 
 void cut_rows(int64_t rows, int steps, int &tiles, int &waves, int &blocks) {
-    const int most = steps > 4 ? 2 : 3;
-    tiles = rows <= 16 ? 1 : 2;
+    tiles = rows <= 16 || (rows > 64 && steps > 4) ? 1 : 2;
     waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : 4);
-    if (rows > 128 && most == 3) tiles = 3;
     blocks = int((rows + 16 * tiles * waves - 1) / (16 * tiles * waves));
 }
 
@@ -204,7 +219,7 @@ hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int6
     if (ready != hipSuccess) return ready;
     for (; w0 < w1; w0 += kMost) {
         hipLaunchKernelGGL((attend_tile_kernel<T, DK, RT, WR, WK>), dim3(unsigned(std::min(kMost, w1 - w0))),
-                           dim3(64 * WR * WK), A::kLds, stream, p, plan, w0);
+                           dim3(64 * WR * WK), A::kLds, stream, p, plan, unsigned(w0));
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -217,9 +232,7 @@ hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int tiles, int w
         return tiles == 1 ? launch_tile<T, DK, 1, 1, kSplit>(p, plan, w0, w1, stream)
                           : launch_tile<T, DK, 2, 1, kSplit>(p, plan, w0, w1, stream);
     if (waves == 2) return launch_tile<T, DK, 2, 2, 2>(p, plan, w0, w1, stream);
-    if constexpr (DK <= 4)
-        if (tiles == 3) return launch_tile<T, DK, 3, 4, 1>(p, plan, w0, w1, stream);
-    return launch_tile<T, DK, 2, 4, 1>(p, plan, w0, w1, stream);
+    return launch_tile<T, DK, (DK <= 4 ? 2 : 1), 4, 1>(p, plan, w0, w1, stream);
 }
 template <class T>
 hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, int64_t w0, int64_t w1,
@@ -233,18 +246,8 @@ hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, i
 }
 
 template <class T>
-hipError_t launch(const Attend &p, void *workspace, hipStream_t stream) {
+hipError_t join(const Attend &p, const Choice &r, hipStream_t stream) {
     const ngpu_attend_t &a = p.a;
-    const Choice r = choose(p.c, a, static_cast<char *>(workspace));
-    if (!r.tiles) return launch_rows<T>(p, stream);
-    const int64_t prefix = r.plan.prefix.works(), all = prefix + r.plan.own.works();
-    if (prefix > 0)
-        if (const hipError_t e = launch_tile<T>(p, r, r.prefix_tiles, r.prefix_waves, 0, prefix, stream);
-            e != hipSuccess)
-            return e;
-    if (all > prefix)
-        if (const hipError_t e = launch_tile<T>(p, r, r.own_tiles, r.own_waves, prefix, all, stream); e != hipSuccess)
-            return e;
     if (r.plan.parts == 1) return hipSuccess;
     int lanes = 2;   // threads a row
     while (4 * lanes < p.c.dim) lanes *= 2;
@@ -256,6 +259,28 @@ hipError_t launch(const Attend &p, void *workspace, hipStream_t stream) {
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <class T>
+hipError_t launch(const Attend &p, void *workspace, hipStream_t stream) {
+    const ngpu_attend_t &a = p.a;
+    const Choice r = choose(p.c, a, static_cast<char *>(workspace));
+    if (!r.tiles) return launch_rows<T>(p, stream);
+    const int64_t prefix = r.plan.prefix.works(), all = prefix + r.plan.own.works();
+    if (prefix > 0 && all > prefix && r.prefix_waves == 1 && r.own_waves == 1) {   // both in one launch
+        if (const hipError_t e = launch_tile<T>(p, r, std::max(r.prefix_tiles, r.own_tiles), 1, 0, all, stream);
+            e != hipSuccess)
+            return e;
+        return join<T>(p, r, stream);
+    }
+    if (prefix > 0)
+        if (const hipError_t e = launch_tile<T>(p, r, r.prefix_tiles, r.prefix_waves, 0, prefix, stream);
+            e != hipSuccess)
+            return e;
+    if (all > prefix)
+        if (const hipError_t e = launch_tile<T>(p, r, r.own_tiles, r.own_waves, prefix, all, stream); e != hipSuccess)
+            return e;
+    return join<T>(p, r, stream);
 }
 
 }  // namespace

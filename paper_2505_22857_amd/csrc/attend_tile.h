@@ -78,6 +78,11 @@ struct Matrix<Bf16> {
         typedef __bf16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ s16x8 round(const float (&x)[8]) {
+        typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+        typedef float f8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(s16x8, __builtin_convertvector(f8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, v8));
+    }
 };
 template <>
 struct Matrix<F16> {
@@ -86,18 +91,25 @@ struct Matrix<F16> {
         typedef _Float16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ s16x8 round(const float (&x)[8]) {
+        typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+        typedef float f8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(s16x8, __builtin_convertvector(f8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, v8));
+    }
 };
 
 // Maximum over the four lanes that hold a row (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_max(float x) {
-    auto both = [](float v, auto r) { return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])); };
-    x = both(x, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    return both(x, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    auto both = [](auto r) { return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])); };
+    x = both(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return both(__builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
 }
-__device__ __forceinline__ float row_sum4(float x) {
-    auto both = [](float v, auto r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); };
-    x = both(x, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    return both(x, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+
+// The sum of the four, alike in each.
+__device__ __forceinline__ float row_sum(float x) {
+    auto both = [](auto r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); };
+    x = both(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return both(__builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
 }
 
 // Waits for everything this wavefront has loaded (registers and LDS).
@@ -110,6 +122,11 @@ __device__ __forceinline__ void wait_loads_all() {
 // nothing else in these kernels uses: a clobber would only be warned about.)
 __device__ __forceinline__ void load_to_lds(const void *p, unsigned at) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
+}
+
+// The same from a uniform address and a lane's offset.
+__device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned at) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
 }
 
 // DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR, WK:
@@ -138,9 +155,12 @@ struct AttendTile {
     }
 };
 
+// Registers are held to what two workgroups of four wavefronts a CU leave each where that spills nothing.
 template <class T, int DK, int RT, int WR, int WK>
-__global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, AttendPlan plan, int64_t work0) {
+__global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
+                                                                                   unsigned work0) {
     using A = AttendTile<T, DK, RT, WR, WK>;
+    using M = Matrix<T>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ unsigned masks[2][4];   // per stage, the keys of each loading wavefront that exist (WR > 1)
     const unsigned lds0 = unsigned(reinterpret_cast<uintptr_t>((LdsPtr<char>)lds));
@@ -151,34 +171,49 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
 
     // Workgroups go to the 8 XCDs in turn; those of one problem follow each
     // other on one XCD, whose L2 then serves the row blocks' common keys.
-    int64_t w = work0 + (gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x);
-    const bool own = w >= plan.prefix.works();
+    unsigned w = work0 + (gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x);
+    const bool own = w >= unsigned(plan.prefix.works());
     const Cut &cut = own ? plan.own : plan.prefix;
-    if (own) w -= plan.prefix.works();
-    const int block = int(w % cut.blocks), split = int(w / cut.blocks % cut.splits);
-    const int64_t problem = w / cut.blocks / cut.splits;
-    const int h = int(problem % H);
-    const int64_t g = problem / H;
-    const int64_t beam = own ? 1 : a.S / a.G, s0 = g * beam;
-    const int64_t rows = beam * T_ * rep;
+    if (own) w -= unsigned(plan.prefix.works());
+    const int block = int(w % unsigned(cut.blocks));
+    w /= unsigned(cut.blocks);
+    const int split = int(w % unsigned(cut.splits));
+    w /= unsigned(cut.splits);
+    const int h = int(w % unsigned(H)), g = int(w / unsigned(H));
+    const int beam = own ? 1 : int(a.S / a.G), s0 = g * beam;
+    const unsigned rows = unsigned(beam) * T_ * rep;   // (all rows of a call are below 2^31)
     const PageTable table = own ? own_table(p, s0) : prefix_table(p, g);
     const int count = int(table.count);
+
+    // this split's keys
+    const int tiles = (count + A::kKeys - 1) / A::kKeys, per = (tiles + cut.splits - 1) / cut.splits;
+    const int tile0 = min(tiles, split * per), tile1 = min(tiles, tile0 + per);
+
+    // A lane's key of a tile: its row of the cache in 16-byte units.
+    const unsigned page_size = unsigned(p.c.page_size);
+    const int my_key = wave * A::kLoad + lane % A::kLoad;
+    auto page_of = [&](int tile) {
+        const int j = tile * A::kKeys + my_key;
+        return tile < tile1 && j < count ? table.pages[unsigned(j) / page_size] : -1;
+    };
+    int page = page_of(tile0), next_page = page_of(tile0 + 1);
 
     // this wavefront's query rows: operand registers, and the keys each row sees
     s16x8 q[RT][DK];
     int limit[RT];
-    int64_t out_row[RT];   // -1: no row
-    bool counts[RT];       // a query token that counts
-    const int64_t row0 = int64_t(block) * A::kRows + wr * 16 * RT;
+    int out_row[RT];   // -1: no row
+    bool counts[RT];   // a query token that counts
     const bool aligned = (reinterpret_cast<uintptr_t>(a.q) % 16 == 0) && a.q_stride_seq % 8 == 0 &&
                          a.q_stride_token % 8 == 0 && a.q_stride_head % 8 == 0;
+    const short flip = a.scale < 0.0f ? short(0x8000) : short(0);   // the scores' sign, so that the factor is not negative
     int least = count;   // keys that every row of the workgroup's sequences sees
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int64_t row = row0 + 16 * r + col;
+        const unsigned row = unsigned(block) * A::kRows + (wr * RT + r) * 16 + col;
         const bool is = row < rows;
-        const int64_t i = is ? row : 0, s = s0 + i / (int64_t(T_) * rep);
-        const int t = int(i / rep % T_), head = h * rep + int(i % rep);
+        const unsigned i = is ? row : 0, token = i / unsigned(rep);
+        const int s = s0 + int(token / unsigned(T_)), t = int(token % unsigned(T_));
+        const int head = h * rep + int(i - token * unsigned(rep));
         out_row[r] = is ? (s * T_ + t) * a.q_heads + head : -1;
         const int nq = int(query_length(a, s));
         counts[r] = t < nq;
@@ -200,39 +235,52 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
                     for (int e = 0; e < 8; ++e) x[e] = short(src[d + e].bits);
                 }
             }
-            q[r][k] = x;
+            q[r][k] = x ^ flip;
         }
     }
     least = __builtin_amdgcn_readfirstlane(least);
 
-    // this split's keys
-    const int tiles = (count + A::kKeys - 1) / A::kKeys, per = (tiles + cut.splits - 1) / cut.splits;
-    const int tile0 = min(tiles, split * per), tile1 = min(tiles, tile0 + per);
-
-    // A lane's key of a tile: its row of the cache in 16-byte units, all ones where there is none.
-    const unsigned page_size = unsigned(p.c.page_size);
-    const int my_key = wave * A::kLoad + lane % A::kLoad;
-    auto page_of = [&](int tile) {
-        const int j = tile * A::kKeys + my_key;
-        return tile < tile1 && j < count ? table.pages[unsigned(j) / page_size] : -1;
-    };
     const uint64_t k_page = uint64_t(p.c.k_stride_page) / 8, v_page = uint64_t(p.c.v_stride_page) / 8;
     const unsigned k_token = unsigned(p.c.k_stride_token / 8), v_token = unsigned(p.c.v_stride_token / 8);
     const char *k_head = static_cast<const char *>(p.c.k) + int64_t(h) * p.c.k_stride_head * 2;
     const char *v_head = static_cast<const char *>(p.c.v) + int64_t(h) * p.c.v_stride_head * 2;
     const int piece = lane % A::kPieces, in_load = lane / A::kPieces;
-    const int pieces = D / 8;
+    // Where a wavefront's keys lie in one page and a row has no missing
+    // dimensions, a lane's offsets are the same for every tile.
+    const bool in_page = page_size % A::kLoad == 0 && D == 32 * DK && k_token < (1u << 21) && v_token < (1u << 21);
+    unsigned k_off[A::kLoads], v_off[A::kLoads];
+#pragma unroll
+    for (int u = 0; u < A::kLoads; ++u) {
+        const int row = u * A::kPerLoad + in_load, full = wave * A::kLoad + row;
+        k_off[u] = (unsigned(row) * k_token + unsigned(piece ^ A::key_swizzle(full))) * 16;
+        v_off[u] = (unsigned(row) * v_token + unsigned(piece ^ A::value_swizzle(full))) * 16;
+    }
     unsigned valid = 0;   // keys that exist among those this wavefront loaded last
-    auto fetch = [&](int tile, int stage, int page) {
-        const int j = tile * A::kKeys + my_key;
+    auto fetch = [&](int tile, int stage) {
         const bool is = page >= 0 && page < p.c.num_pages;   // (-1 past the end)
-        const unsigned entry = unsigned(j) % page_size;
-        const unsigned k_at = is ? unsigned(uint64_t(unsigned(page)) * k_page) + entry * k_token : 0u;
-        const unsigned v_at = is ? unsigned(uint64_t(unsigned(page)) * v_page) + entry * v_token : 0u;
         const unsigned long long mask = __ballot(is);
-        valid = unsigned(mask) & (A::kLoad == 32 ? 0xffffffffu : 0xffffu);
+        constexpr unsigned kAll = A::kLoad == 32 ? 0xffffffffu : 0xffffu;
+        valid = unsigned(mask) & kAll;
         if (WR > 1 && lane == 0) masks[stage][wave] = valid;
-        const unsigned at = lds0 + unsigned(stage * A::kStage + wave * A::kLoad * A::kPitch);
+        const unsigned at = __builtin_amdgcn_readfirstlane(lds0 + unsigned(stage * A::kStage + wave * A::kLoad * A::kPitch));
+        const unsigned entry = unsigned(tile * A::kKeys + my_key) % page_size;
+        if (in_page && valid == kAll) {
+            const unsigned e0 = __builtin_amdgcn_readfirstlane(entry), p0 = __builtin_amdgcn_readfirstlane(page);
+            const char *kb = k_head + (p0 * k_page + e0 * uint64_t(k_token)) * 16;
+            const char *vb = v_head + (p0 * v_page + e0 * uint64_t(v_token)) * 16;
+#pragma unroll
+            for (int u = 0; u < A::kLoads; ++u) {
+                const int full = wave * A::kLoad + u * A::kPerLoad + in_load;
+                if (4 * DK == A::kPieces || (piece ^ A::key_swizzle(full)) < 4 * DK)
+                    load_to_lds(kb, k_off[u], at + u * kWave * 16);
+                if (4 * DK == A::kPieces || (piece ^ A::value_swizzle(full)) < 4 * DK)
+                    load_to_lds(vb, v_off[u], at + A::kKeys * A::kPitch + u * kWave * 16);
+            }
+            return;
+        }
+        const unsigned k_at = is ? unsigned(unsigned(page) * k_page) + entry * k_token : 0u;
+        const unsigned v_at = is ? unsigned(unsigned(page) * v_page) + entry * v_token : 0u;
+        const int pieces = D / 8;
 #pragma unroll
         for (int u = 0; u < A::kLoads; ++u) {
             const int row = u * A::kPerLoad + in_load;   // of this wavefront's keys
@@ -249,8 +297,18 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
         }
     };
 
+    // this lane's places in a tile of its key group: the operand rows of K and the blocks of V
+    unsigned k_at[DK], v_at[A::kTiles];
+#pragma unroll
+    for (int k = 0; k < DK; ++k) k_at[k] = unsigned(col * A::kPitch + 16 * ((4 * k + quad) ^ A::key_swizzle(col)));
+#pragma unroll
+    for (int d = 0; d < A::kTiles; ++d) {
+        const int row = 4 * quad + col / 4;
+        v_at[d] = unsigned(row * A::kPitch + 16 * ((2 * d + (col % 4) / 2) ^ A::value_swizzle(row)) + 8 * (col & 1));
+    }
+
     f32x4 o[RT][A::kTiles];
-    float m[RT], sum[RT];
+    float m[RT], sum[RT];   // sum: of the weights of this lane's keys, before they are rounded
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         m[r] = -__builtin_inff();
@@ -258,13 +316,9 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
 #pragma unroll
         for (int d = 0; d < A::kTiles; ++d) o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const float to_log2 = a.scale * 1.44269504088896f;
+    const float to_log2 = __builtin_fabsf(a.scale) * 1.44269504088896f;
 
-    int next_page = -1;
-    if (tile0 < tile1) {
-        fetch(tile0, 0, page_of(tile0));
-        next_page = page_of(tile0 + 1);
-    }
+    if (tile0 < tile1) fetch(tile0, 0);
     for (int tile = tile0; tile < tile1; ++tile) {
         const int stage = (tile - tile0) & 1;
         const unsigned mine = valid;
@@ -273,176 +327,174 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
         else
             wait_loads();
         if (tile + 1 < tile1) {
-            fetch(tile + 1, stage ^ 1, next_page);
+            page = next_page;
             next_page = page_of(tile + 2);
+            fetch(tile + 1, stage ^ 1);
         }
         const char *keys = lds + stage * A::kStage + wk * 32 * A::kChunks * A::kPitch;
         const char *values = keys + A::kKeys * A::kPitch;
+        const int key0 = tile * A::kKeys + wk * A::kChunks * 32;
+        // which of the keys exist
+        unsigned exists[A::kChunks];
+        bool partial = own && key0 + 32 * A::kChunks > least;   // some rows do not see some of them
+        const bool some_rows = partial;
 #pragma unroll
         for (int c = 0; c < A::kChunks; ++c) {
-            const int key0 = tile * A::kKeys + (wk * A::kChunks + c) * 32;
-            unsigned exists = mine;
+            exists[c] = mine;
             if (WR > 1) {
                 const int first = (wk * A::kChunks + c) * 32 / A::kLoad;
-                exists = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
+                exists[c] = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
             }
-            exists = __builtin_amdgcn_readfirstlane(exists);
-            if (exists == 0) continue;
-            // scores
-            f32x4 x[RT][2];
+            exists[c] = __builtin_amdgcn_readfirstlane(exists[c]);
+            partial |= exists[c] != 0xffffffffu;
+        }
+
+        f32x4 x[RT][2 * A::kChunks];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) x[r][0] = x[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < DK; ++k)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = c * 32 + u * 16 + col;   // of this key group
-                const int full = wk * 32 * A::kChunks + row;
+            for (int u = 0; u < 2 * A::kChunks; ++u) {
+                const s16x8 kx = *reinterpret_cast<const s16x8 *>(keys + u * 16 * A::kPitch + k_at[k]);
 #pragma unroll
-                for (int k = 0; k < DK; ++k) {
-                    const s16x8 kx = *reinterpret_cast<const s16x8 *>(
-                        keys + row * A::kPitch + 16 * ((4 * k + quad) ^ A::key_swizzle(full)));
+                for (int r = 0; r < RT; ++r)
+                    x[r][u] = M::mul(kx, q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][u]);
+            }
+        s16x8 weights[RT][A::kChunks];
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) x[r][u] = Matrix<T>::mul(kx, q[r][k], x[r][u]);
+        for (int r = 0; r < RT; ++r) {
+            if (partial) {
+#pragma unroll
+                for (int e = 0; e < 8 * A::kChunks; ++e) {
+                    const int key = 16 * (e / 4 % 2) + 4 * quad + e % 4;
+                    const bool sees = ((exists[e / 8] >> key) & 1u) && key0 + e / 8 * 32 + key < limit[r];
+                    x[r][e / 4][e % 4] = sees ? x[r][e / 4][e % 4] : -__builtin_inff();
                 }
             }
-            const bool partial = exists != 0xffffffffu || (own && key0 + 32 > least);   // uniform
-            s16x8 weights[RT];
+            float top = x[r][0][0];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                float y[8];
+            for (int e = 1; e < 8 * A::kChunks; ++e) top = __builtin_fmaxf(top, x[r][e / 4][e % 4]);
+            top *= to_log2;
+            if (__ballot(top > m[r] + 8.0f)) {   // (also while m is -inf)
+                const float now = __builtin_fmaxf(m[r], row_max(top));
+                const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
+                m[r] = now;
+                sum[r] *= f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = x[r][e / 4][e % 4] * to_log2;
-                if (partial) {
+                for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
+            }
+            const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
+#pragma unroll
+            for (int c = 0; c < A::kChunks; ++c) {
+                float z[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4], to_log2, -base));
+                if (partial) {   // (a score of -inf times a factor of 0 is NaN)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int key = 16 * (e / 4) + 4 * quad + e % 4;
-                        const bool sees = ((exists >> key) & 1u) && key0 + key < limit[r];
-                        y[e] = sees ? y[e] : -__builtin_inff();
+                        z[e] = ((exists[c] >> key) & 1u) && key0 + c * 32 + key < limit[r] ? z[e] : 0.0f;
                     }
                 }
-                float top = y[0];
 #pragma unroll
-                for (int e = 1; e < 8; ++e) top = __builtin_fmaxf(top, y[e]);
-                top = row_max(top);
-                if (__ballot(top > m[r] + 8.0f)) {   // (also while m is -inf)
-                    const float now = __builtin_fmaxf(m[r], top);
-                    const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
-                    m[r] = now;
-                    sum[r] *= f;
-#pragma unroll
-                    for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
-                }
-                const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
-                float part = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float z = __builtin_amdgcn_exp2f(y[e] - base);
-                    part += z;
-                    weights[r][e] = short(from_float<T>(z).bits);
-                }
-                sum[r] += part;
+                for (int e = 0; e < 8; ++e) sum[r] += z[e];
+                weights[r][c] = M::round(z);
             }
-            // values
-            const bool some_rows = own && key0 + 32 > least;   // a key that only some rows see
+        }
+#pragma unroll
+        for (int c = 0; c < A::kChunks; ++c) {
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d) {
                 s16x8 vx;
-                bool odd = false;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int row = c * 32 + u * 16 + 4 * quad + col / 4;
-                    const int full = wk * 32 * A::kChunks + row;
-                    const char *at = values + row * A::kPitch + 16 * ((2 * d + ((col & 3) >> 1)) ^ A::value_swizzle(full)) +
-                                     8 * (col & 1);
-                    const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr<s16x4>)(const_cast<char *>(at)));
+                    const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (LdsPtr<s16x4>)(const_cast<char *>(values + (c * 32 + u * 16) * A::kPitch + v_at[d])));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) vx[4 * u + e] = part[e];
                 }
                 if (some_rows) {
                     // A value that is not finite must not reach the rows that do not see its key (0 * inf): it
                     // is left out here and added below to the rows that do.
+                    bool odd = false;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const bool bad = (vx[e] & Matrix<T>::kExponent) == Matrix<T>::kExponent;
+                        const bool bad = (vx[e] & M::kExponent) == M::kExponent;
                         odd |= bad;
                         vx[e] = bad ? short(0) : vx[e];
                     }
-                }
+                    if (__ballot(odd)) {
+                        for (int key = 0; key < 32; ++key) {
+                            const int row = c * 32 + key;
 #pragma unroll
-                for (int r = 0; r < RT; ++r) o[r][d] = Matrix<T>::mul(vx, weights[r], o[r][d]);
-                if (some_rows && __ballot(odd)) {
-                    for (int key = 0; key < 32; ++key) {
-                        const int row = c * 32 + key, full = wk * 32 * A::kChunks + row;
+                            for (int i = 0; i < 4; ++i) {
+                                const int dim = 16 * d + 4 * quad + i;
+                                const T v = *reinterpret_cast<const T *>(
+                                    values + row * A::kPitch + 16 * ((dim / 8) ^ A::value_swizzle(row)) + 2 * (dim % 8));
+                                const bool bad = (short(v.bits) & M::kExponent) == M::kExponent;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int dim = 16 * d + 4 * quad + i;
-                            const T v = *reinterpret_cast<const T *>(
-                                values + row * A::kPitch + 16 * ((dim / 8) ^ A::value_swizzle(full)) + 2 * (dim % 8));
-                            const bool bad = (short(v.bits) & Matrix<T>::kExponent) == Matrix<T>::kExponent;
+                                for (int r = 0; r < RT; ++r) {
+                                    int z = 0;   // the row's weight of this key
 #pragma unroll
-                            for (int r = 0; r < RT; ++r) {
-                                int z = 0;   // the row's weight of this key
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) z = key / 16 * 4 + key % 4 == e ? weights[r][e] : z;
-                                z = __shfl(z, key % 16 / 4 * 16 + col);
-                                if (bad && key0 + key < limit[r])
-                                    o[r][d][i] += to_float(T{uint16_t(z)}) * to_float(v);
+                                    for (int e = 0; e < 8; ++e) z = key / 16 * 4 + key % 4 == e ? weights[r][c][e] : z;
+                                    z = __shfl(z, key % 16 / 4 * 16 + col);
+                                    if (bad && key0 + row < limit[r])
+                                        o[r][d][i] += to_float(T{uint16_t(z)}) * to_float(v);
+                                }
                             }
                         }
                     }
                 }
+#pragma unroll
+                for (int r = 0; r < RT; ++r) o[r][d] = M::mul(vx, weights[r][c], o[r][d]);
             }
         }
     }
 
-#pragma unroll
-    for (int r = 0; r < RT; ++r) sum[r] = row_sum4(sum[r]);
-
     // The wavefronts that share rows join their parts.
+    float total[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) total[r] = row_sum(sum[r]);
     if (WK > 1) {
         wait_loads_all();   // nothing reads or loads a tile any more
-        float *box = reinterpret_cast<float *>(lds);             // [WR][RT * 16][kDims], one key group's turn
-        __shared__ float join[2][WK][WR * RT * 16];
+        float *box = reinterpret_cast<float *>(lds);
+        __shared__ float2 join[WK][WR * RT * 16];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
-            if (quad == 0) {
-                join[0][wk][(wr * RT + r) * 16 + col] = m[r];
-                join[1][wk][(wr * RT + r) * 16 + col] = sum[r];
-            }
+            if (quad == 0) join[wk][(wr * RT + r) * 16 + col] = make_float2(m[r], total[r]);
         __syncthreads();
+        constexpr int kGroup = WR * RT * A::kTiles * 256;   // floats of one key group
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int at = (wr * RT + r) * 16 + col;
-            float top = join[0][0][at], total = 0.0f;
+            float top = join[0][at].x, all = 0.0f;
 #pragma unroll
-            for (int k = 1; k < WK; ++k) top = __builtin_fmaxf(top, join[0][k][at]);
+            for (int k = 1; k < WK; ++k) top = __builtin_fmaxf(top, join[k][at].x);
             const float base = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-            for (int k = 0; k < WK; ++k) total += join[1][k][at] * __builtin_amdgcn_exp2f(join[0][k][at] - base);
+            for (int k = 0; k < WK; ++k) all += join[k][at].y * __builtin_amdgcn_exp2f(join[k][at].x - base);
             const float f = __builtin_amdgcn_exp2f(m[r] - base);
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
             m[r] = top;
-            sum[r] = total;
+            total[r] = all;
+            if (wk != 0) {
+#pragma unroll
+                for (int d = 0; d < A::kTiles; ++d)
+                    *reinterpret_cast<f32x4 *>(box + wk * kGroup + ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4) =
+                        o[r][d];
+            }
         }
-        // key group 0 collects: the others write, group after group of dimensions is summed by all
-        constexpr int kGroup = WR * RT * 16 * A::kDims;   // floats of one key group
+        __syncthreads();
+        if (wk != 0) return;
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d)
-                *reinterpret_cast<f32x4 *>(box + wk * kGroup + ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4) = o[r][d];
-        __syncthreads();
-        if (wk == 0) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int d = 0; d < A::kTiles; ++d)
-#pragma unroll
-                    for (int k = 1; k < WK; ++k)
-                        o[r][d] += *reinterpret_cast<const f32x4 *>(
-                            box + k * kGroup + ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4);
-        }
-        if (wk != 0) return;
+                for (int k = 1; k < WK; ++k)
+                    o[r][d] += *reinterpret_cast<const f32x4 *>(box + k * kGroup +
+                                                                ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4);
     }
 
     const int64_t all_rows = a.S * a.T * a.q_heads;
@@ -451,19 +503,19 @@ __global__ __launch_bounds__(64 * WR * WK) void attend_tile_kernel(Attend p, Att
     for (int r = 0; r < RT; ++r) {
         if (out_row[r] < 0) continue;
         if (plan.parts > 1) {
-            if (quad == 0) plan.stats[part * all_rows + out_row[r]] = make_float2(m[r], sum[r]);
-            if (sum[r] == 0.0f) continue;
+            if (quad == 0) plan.stats[part * all_rows + out_row[r]] = make_float2(m[r], total[r]);
+            if (total[r] == 0.0f) continue;
             float *dst = plan.sums + (part * all_rows + out_row[r]) * D;
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d)
                 if (const int at = 16 * d + 4 * quad; at < D) *reinterpret_cast<f32x4 *>(dst + at) = o[r][d];
         } else {
-            const bool any = counts[r] && sum[r] != 0.0f;   // (a NaN sum too)
+            const bool any = counts[r] && total[r] != 0.0f;   // (a NaN sum too)
             if (a.lse && quad == 0)
-                a.lse[out_row[r]] = any ? (m[r] == -__builtin_inff() ? sum[r] : m[r] * 0.69314718056f + logf(sum[r]))
+                a.lse[out_row[r]] = any ? (m[r] == -__builtin_inff() ? total[r] : m[r] * 0.69314718056f + logf(total[r]))
                                         : -__builtin_inff();
-            T *dst = static_cast<T *>(a.out) + out_row[r] * D;
-            const float f = 1.0f / sum[r];
+            T *dst = static_cast<T *>(a.out) + int64_t(out_row[r]) * D;
+            const float f = 1.0f / total[r];
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d) {
                 if (const int at = 16 * d + 4 * quad; at < D) {
