@@ -99,46 +99,67 @@ static hipError_t launch_rows(const Attend &p, hipStream_t stream) {
     return hipSuccess;
 }
 
-// A row's parts joined: each thread takes 4 dimensions of one row.
+// A row's parts joined: `lanes` threads take 4 dimensions each, and `groups` such
+// sets of threads every groups-th part, eight parts at a time so that their
+// loads are in flight together; the sets then meet in LDS.
 constexpr int kJoinThreads = 256;
 template <class T>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(Attend p, AttendPlan plan, int64_t rows, int lanes,
-                                                                   int64_t row0) {
+                                                                   int groups, int64_t row0) {
+    constexpr int kBatch = 8;
     const ngpu_attend_t &a = p.a;
-    const int D = p.c.dim, d = int(threadIdx.x) % lanes * 4;
-    const int64_t row = row0 + int64_t(blockIdx.x) * (kJoinThreads / lanes) + int(threadIdx.x) / lanes;
-    if (row >= rows || d >= D) return;
+    const int D = p.c.dim, d = int(threadIdx.x) % lanes * 4, group = int(threadIdx.x) / lanes % groups;
+    const int64_t row = row0 + int64_t(blockIdx.x) * (kJoinThreads / (lanes * groups)) + int(threadIdx.x) / (lanes * groups);
+    const int64_t token = row / a.q_heads;
+    const bool counts = row < rows && token % a.T < query_length(a, token / a.T);
     float top = -__builtin_inff(), sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t token = row / a.q_heads;
-    if (token % a.T < query_length(a, token / a.T)) {
-        // eight parts at a time, so that their loads are in flight together; past the last: the last again, for nothing
-        constexpr int kBatch = 8;
-        const int n = plan.parts;
-        for (int i = 0; i < n; i += kBatch) {
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) top = __builtin_fmaxf(top, plan.stats[min(i + u, n - 1) * rows + row].x);
-        }
-        const float base = top == -__builtin_inff() ? 0.0f : top;
-        for (int i = 0; i < n; i += kBatch) {
+    auto factor = [](float m, float base) { return m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - base); };
+    if (counts && d < D) {
+        for (int i = group; i < plan.parts; i += groups * kBatch) {
             float2 s[kBatch];
             f32x4 x[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                s[u] = plan.stats[min(i + u, n - 1) * rows + row];
-                x[u] = *reinterpret_cast<const f32x4 *>(plan.sums + (min(i + u, n - 1) * rows + row) * D + d);
+            for (int u = 0; u < kBatch; ++u) {   // past the last part: the last again, for nothing
+                const int64_t at = min(i + u * groups, plan.parts - 1) * rows + row;
+                s[u] = plan.stats[at];
+                x[u] = *reinterpret_cast<const f32x4 *>(plan.sums + at * D + d);
             }
+            const float before = top;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) top = i + u * groups < plan.parts ? __builtin_fmaxf(top, s[u].x) : top;
+            const float base = top == -__builtin_inff() ? 0.0f : top, f0 = factor(before, base);
+            sum *= f0;
+            o *= f0;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 // a part without a key (sum 0) has written no sums; a NaN sum goes on
-                const bool any = i + u < n && s[u].y != 0.0f;
-                const float f = s[u].x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s[u].x - base);
+                const bool any = i + u * groups < plan.parts && s[u].y != 0.0f;
+                const float f = factor(s[u].x, base);
                 sum += any ? s[u].y * f : 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] += any ? x[u][e] * f : 0.0f;
             }
         }
     }
+    if (groups > 1) {
+        __shared__ f32x4 sums[kJoinThreads];
+        __shared__ float2 stats[kJoinThreads];
+        sums[threadIdx.x] = o;
+        stats[threadIdx.x] = make_float2(top, sum);
+        __syncthreads();
+        if (group != 0) return;
+        for (int g = 1; g < groups; ++g) {
+            const int at = int(threadIdx.x) + g * lanes;
+            const float2 s = stats[at];
+            const float now = __builtin_fmaxf(top, s.x), base = now == -__builtin_inff() ? 0.0f : now;
+            const float f0 = factor(top, base), f1 = factor(s.x, base);
+            sum = sum * f0 + s.y * f1;
+            o = o * f0 + sums[at] * f1;
+            top = now;
+        }
+    }
+    if (row >= rows || d >= D) return;
     const bool any = sum != 0.0f;
     if (a.lse && d == 0)
         a.lse[row] = any ? (top == -__builtin_inff() ? sum : top * 0.69314718056f + logf(sum)) : -__builtin_inff();
@@ -192,8 +213,7 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int &tiles, int &waves) {
         Cut u{problems, 0, 0};
         cut_rows(rows, r.steps, tiles, waves, u.blocks);
-        const int64_t tile = waves == 1 && r.steps <= 4 ? 128 : 64;
-        const int64_t have = problems * u.blocks, wanted = waves == 4 ? 2 * kCus : kCus;
+        const int64_t tile = waves == 4 ? 64 : 32, have = problems * u.blocks, wanted = 2 * kCus;
         const int64_t most = std::max<int64_t>(1, (most_keys + 2 * tile - 1) / (2 * tile));
         u.splits = int(std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, wanted / have)));
         return u;
@@ -209,17 +229,17 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     return r;
 }
 
-template <class T, int DK, int RT, int WR, int WK>
+template <class T, int DK, int RT, int WR>
 hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int64_t w1, hipStream_t stream) {
-    using A = AttendTile<T, DK, RT, WR, WK>;
+    using A = AttendTile<T, DK, RT, WR>;
     constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
     static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void *>(&attend_tile_kernel<T, DK, RT, WR, WK>),
+        reinterpret_cast<const void *>(&attend_tile_kernel<T, DK, RT, WR>),
         hipFuncAttributeMaxDynamicSharedMemorySize, A::kLds);
     if (ready != hipSuccess) return ready;
     for (; w0 < w1; w0 += kMost) {
-        hipLaunchKernelGGL((attend_tile_kernel<T, DK, RT, WR, WK>), dim3(unsigned(std::min(kMost, w1 - w0))),
-                           dim3(64 * WR * WK), A::kLds, stream, p, plan, unsigned(w0));
+        hipLaunchKernelGGL((attend_tile_kernel<T, DK, RT, WR>), dim3(unsigned(std::min(kMost, w1 - w0))),
+                           dim3(64 * WR), A::kLds, stream, p, plan, unsigned(w0));
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -227,12 +247,11 @@ hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int6
 template <class T, int DK>
 hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int tiles, int waves, int64_t w0, int64_t w1,
                        hipStream_t stream) {
-    constexpr int kSplit = DK <= 4 ? 4 : 2;   // wavefronts along keys: two stages of their tiles fill the LDS
     if (waves == 1)
-        return tiles == 1 ? launch_tile<T, DK, 1, 1, kSplit>(p, plan, w0, w1, stream)
-                          : launch_tile<T, DK, 2, 1, kSplit>(p, plan, w0, w1, stream);
-    if (waves == 2) return launch_tile<T, DK, 2, 2, 2>(p, plan, w0, w1, stream);
-    return launch_tile<T, DK, (DK <= 4 ? 2 : 1), 4, 1>(p, plan, w0, w1, stream);
+        return tiles == 1 ? launch_tile<T, DK, 1, 1>(p, plan, w0, w1, stream)
+                          : launch_tile<T, DK, 2, 1>(p, plan, w0, w1, stream);
+    if (waves == 2) return launch_tile<T, DK, 2, 2>(p, plan, w0, w1, stream);
+    return launch_tile<T, DK, (DK <= 4 ? 2 : 1), 4>(p, plan, w0, w1, stream);
 }
 template <class T>
 hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, int64_t w0, int64_t w1,
@@ -251,11 +270,13 @@ hipError_t join(const Attend &p, const Choice &r, hipStream_t stream) {
     if (r.plan.parts == 1) return hipSuccess;
     int lanes = 2;   // threads a row
     while (4 * lanes < p.c.dim) lanes *= 2;
-    const int64_t rows = a.S * a.T * a.q_heads, per = kJoinThreads / lanes, kMost = int64_t(1) << 23;
+    int groups = 1;   // sets of them, eight parts each
+    while (8 * groups < r.plan.parts && 2 * groups * lanes <= kJoinThreads) groups *= 2;
+    const int64_t rows = a.S * a.T * a.q_heads, per = kJoinThreads / (lanes * groups), kMost = int64_t(1) << 23;
     for (int64_t r0 = 0; r0 < rows; r0 += kMost * per) {
-        const int64_t groups = std::min(kMost, (rows - r0 + per - 1) / per);
-        hipLaunchKernelGGL((attend_join_kernel<T>), dim3(unsigned(groups)), dim3(kJoinThreads), 0, stream, p, r.plan,
-                           rows, lanes, r0);
+        const int64_t grid = std::min(kMost, (rows - r0 + per - 1) / per);
+        hipLaunchKernelGGL((attend_join_kernel<T>), dim3(unsigned(grid)), dim3(kJoinThreads), 0, stream, p, r.plan,
+                           rows, lanes, groups, r0);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;

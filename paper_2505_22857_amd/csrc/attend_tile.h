@@ -120,23 +120,30 @@ __device__ __forceinline__ void wait_loads_all() {
 // 16 bytes a lane from memory to LDS at `at` + 16 lane (uniform `at`).  As asm, since
 // the compiler would wait for it before any later LDS load.  (m0 is a reserved register, which
 // nothing else in these kernels uses: a clobber would only be warned about.)
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void *p, unsigned at) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
+    if (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(p) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
 }
 
 // The same from a uniform address and a lane's offset.
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned at) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+    if (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(at), "v"(offset), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
 }
 
-// DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR, WK:
-// wavefronts along rows and along keys.
-template <class T, int DK, int RT, int WR, int WK>
+// DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR:
+// wavefronts, each with rows of its own, that share the tiles of keys.
+template <class T, int DK, int RT, int WR>
 struct AttendTile {
-    static constexpr int kWaves = WR * WK;
-    static constexpr int kChunks = WK > 1 ? 1 : 2;              // of 32 keys, a wavefront and tile
-    static constexpr int kKeys = 32 * kChunks * WK;             // a tile
-    static constexpr int kLoad = kKeys / kWaves;                // keys a wavefront loads
+    static constexpr int kChunks = WR > 2 ? 2 : 1;              // of 32 keys, a tile
+    static constexpr int kKeys = 32 * kChunks;                  // a tile
+    static constexpr int kLoad = kKeys / WR;                // keys a wavefront loads
     static constexpr int kRows = 16 * RT * WR;                  // a workgroup
     static constexpr int kPitch = DK <= 2 ? 128 : (DK <= 4 ? 256 : 512);   // bytes of a row in LDS
     static constexpr int kPieces = kPitch / 16;                 // 16-byte chunks of it
@@ -144,9 +151,8 @@ struct AttendTile {
     static constexpr int kLds = 2 * kStage;
     static constexpr int kPerLoad = kWave / kPieces;            // rows a load instruction brings
     static constexpr int kLoads = kLoad / kPerLoad;
+    static constexpr bool kOnce = WR == 1;                      // no other workgroup reads these keys
     static constexpr int kTiles = 2 * DK;                       // of 16 dimensions
-    static constexpr int kDims = 32 * DK;
-    static_assert(WK == 1 || kWaves * 16 * RT * kDims * 4 <= kLds, "the wavefronts' sums meet in the tiles' LDS");
     static_assert(kLoad == 16 || kLoad == 32, "a wavefront's lanes hold its keys' pages");
 
     static __device__ __forceinline__ int key_swizzle(int row) { return kPieces == 8 ? (row >> 1) & 7 : row & 15; }
@@ -156,30 +162,38 @@ struct AttendTile {
 };
 
 // Registers are held to what two workgroups of four wavefronts a CU leave each where that spills nothing.
-template <class T, int DK, int RT, int WR, int WK>
-__global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
+template <class T, int DK, int RT, int WR>
+__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
                                                                                    unsigned work0) {
-    using A = AttendTile<T, DK, RT, WR, WK>;
+    using A = AttendTile<T, DK, RT, WR>;
     using M = Matrix<T>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ unsigned masks[2][4];   // per stage, the keys of each loading wavefront that exist (WR > 1)
+    unsigned (*masks)[4] = nullptr;   // per stage, the keys of each loading wavefront that exist
+    if constexpr (WR > 1) {
+        __shared__ unsigned shared_masks[2][4];
+        masks = shared_masks;
+    }
     const unsigned lds0 = unsigned(reinterpret_cast<uintptr_t>((LdsPtr<char>)lds));
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int wk = wave / WR, wr = wave % WR, col = lane % 16, quad = lane / 16;
+    const int col = lane % 16, quad = lane / 16;
     const ngpu_attend_t &a = p.a;
     const int H = p.c.heads, rep = a.q_heads / H, D = p.c.dim, T_ = int(a.T);
 
-    // Workgroups go to the 8 XCDs in turn; those of one problem follow each
-    // other on one XCD, whose L2 then serves the row blocks' common keys.
-    unsigned w = work0 + (gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x);
-    const bool own = w >= unsigned(plan.prefix.works());
+    // Workgroups go to the 8 XCDs in turn.  Each XCD takes a run of the prefixes'
+    // works, which share keys (row blocks) or rows of pages (heads) in its L2.
+    const unsigned prefix_works = unsigned(plan.prefix.works());
+    unsigned w = work0 + blockIdx.x;
+    const bool own = w >= prefix_works;
     const Cut &cut = own ? plan.own : plan.prefix;
-    if (own) w -= unsigned(plan.prefix.works());
+    if (own)
+        w -= prefix_works;
+    else
+        w = w % 8 * (prefix_works / 8) + min(w % 8, prefix_works % 8) + w / 8;
     const int block = int(w % unsigned(cut.blocks));
     w /= unsigned(cut.blocks);
-    const int split = int(w % unsigned(cut.splits));
-    w /= unsigned(cut.splits);
-    const int h = int(w % unsigned(H)), g = int(w / unsigned(H));
+    const int h = int(w % unsigned(H));
+    w /= unsigned(H);
+    const int split = int(w % unsigned(cut.splits)), g = int(w / unsigned(cut.splits));
     const int beam = own ? 1 : int(a.S / a.G), s0 = g * beam;
     const unsigned rows = unsigned(beam) * T_ * rep;   // (all rows of a call are below 2^31)
     const PageTable table = own ? own_table(p, s0) : prefix_table(p, g);
@@ -209,7 +223,7 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
     int least = count;   // keys that every row of the workgroup's sequences sees
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const unsigned row = unsigned(block) * A::kRows + (wr * RT + r) * 16 + col;
+        const unsigned row = unsigned(block) * A::kRows + (wave * RT + r) * 16 + col;
         const bool is = row < rows;
         const unsigned i = is ? row : 0, token = i / unsigned(rep);
         const int s = s0 + int(token / unsigned(T_)), t = int(token % unsigned(T_));
@@ -272,9 +286,9 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
             for (int u = 0; u < A::kLoads; ++u) {
                 const int full = wave * A::kLoad + u * A::kPerLoad + in_load;
                 if (4 * DK == A::kPieces || (piece ^ A::key_swizzle(full)) < 4 * DK)
-                    load_to_lds(kb, k_off[u], at + u * kWave * 16);
+                    load_to_lds<A::kOnce>(kb, k_off[u], at + u * kWave * 16);
                 if (4 * DK == A::kPieces || (piece ^ A::value_swizzle(full)) < 4 * DK)
-                    load_to_lds(vb, v_off[u], at + A::kKeys * A::kPitch + u * kWave * 16);
+                    load_to_lds<A::kOnce>(vb, v_off[u], at + A::kKeys * A::kPitch + u * kWave * 16);
             }
             return;
         }
@@ -292,12 +306,12 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
                                                   : reinterpret_cast<const char *>(kNoData);
             const char *vs = there && vp < pieces ? v_head + (uint64_t(v_row) + unsigned(vp)) * 16
                                                   : reinterpret_cast<const char *>(kNoData);
-            load_to_lds(ks, at + u * kWave * 16);
-            load_to_lds(vs, at + A::kKeys * A::kPitch + u * kWave * 16);
+            load_to_lds<A::kOnce>(ks, at + u * kWave * 16);
+            load_to_lds<A::kOnce>(vs, at + A::kKeys * A::kPitch + u * kWave * 16);
         }
     };
 
-    // this lane's places in a tile of its key group: the operand rows of K and the blocks of V
+    // this lane's places in a tile: the operand rows of K and the blocks of V
     unsigned k_at[DK], v_at[A::kTiles];
 #pragma unroll
     for (int k = 0; k < DK; ++k) k_at[k] = unsigned(col * A::kPitch + 16 * ((4 * k + quad) ^ A::key_swizzle(col)));
@@ -331,9 +345,9 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
             next_page = page_of(tile + 2);
             fetch(tile + 1, stage ^ 1);
         }
-        const char *keys = lds + stage * A::kStage + wk * 32 * A::kChunks * A::kPitch;
+        const char *keys = lds + stage * A::kStage;
         const char *values = keys + A::kKeys * A::kPitch;
-        const int key0 = tile * A::kKeys + wk * A::kChunks * 32;
+        const int key0 = tile * A::kKeys;
         // which of the keys exist
         unsigned exists[A::kChunks];
         bool partial = own && key0 + 32 * A::kChunks > least;   // some rows do not see some of them
@@ -342,7 +356,7 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
         for (int c = 0; c < A::kChunks; ++c) {
             exists[c] = mine;
             if (WR > 1) {
-                const int first = (wk * A::kChunks + c) * 32 / A::kLoad;
+                const int first = c * 32 / A::kLoad;
                 exists[c] = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
             }
             exists[c] = __builtin_amdgcn_readfirstlane(exists[c]);
@@ -451,52 +465,9 @@ __global__ __launch_bounds__(64 * WR * WK, DK <= 4 ? 2 : 1) void attend_tile_ker
         }
     }
 
-    // The wavefronts that share rows join their parts.
     float total[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) total[r] = row_sum(sum[r]);
-    if (WK > 1) {
-        wait_loads_all();   // nothing reads or loads a tile any more
-        float *box = reinterpret_cast<float *>(lds);
-        __shared__ float2 join[WK][WR * RT * 16];
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-            if (quad == 0) join[wk][(wr * RT + r) * 16 + col] = make_float2(m[r], total[r]);
-        __syncthreads();
-        constexpr int kGroup = WR * RT * A::kTiles * 256;   // floats of one key group
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int at = (wr * RT + r) * 16 + col;
-            float top = join[0][at].x, all = 0.0f;
-#pragma unroll
-            for (int k = 1; k < WK; ++k) top = __builtin_fmaxf(top, join[k][at].x);
-            const float base = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-            for (int k = 0; k < WK; ++k) all += join[k][at].y * __builtin_amdgcn_exp2f(join[k][at].x - base);
-            const float f = __builtin_amdgcn_exp2f(m[r] - base);
-#pragma unroll
-            for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
-            m[r] = top;
-            total[r] = all;
-            if (wk != 0) {
-#pragma unroll
-                for (int d = 0; d < A::kTiles; ++d)
-                    *reinterpret_cast<f32x4 *>(box + wk * kGroup + ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4) =
-                        o[r][d];
-            }
-        }
-        __syncthreads();
-        if (wk != 0) return;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int d = 0; d < A::kTiles; ++d)
-#pragma unroll
-                for (int k = 1; k < WK; ++k)
-                    o[r][d] += *reinterpret_cast<const f32x4 *>(box + k * kGroup +
-                                                                ((wr * RT + r) * A::kTiles + d) * 256 + lane * 4);
-    }
-
     const int64_t all_rows = a.S * a.T * a.q_heads;
     const int part = (own ? plan.prefix.splits : 0) + split;
 #pragma unroll
