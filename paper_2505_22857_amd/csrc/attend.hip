@@ -9,82 +9,49 @@
 
 namespace ngpu {
 
-constexpr int kRowWaves = 4;
-constexpr int kMostDims = NGPU_LM_MAX_HEAD_DIM / kWave;   // dimensions a lane holds
-
-__device__ __forceinline__ float lanes_sum(float x) {
-    for (int d = kWave / 2; d > 0; d /= 2) x += __shfl_xor(x, d);
-    return x;
-}
-
 // One workgroup per row (sequence, query token, head); its wavefronts take every
-// fourth key, a lane every 64th dimension, and keep a running maximum and sum.
+// fourth key and keep sums of their own, which meet in LDS.
+constexpr int kRowWaves = 4;
 template <class T>
 __global__ __launch_bounds__(kRowWaves * kWave) void attend_row_kernel(Attend p, int64_t row0) {
     const ngpu_attend_t &a = p.a;
     const int64_t row = row0 + blockIdx.x, s = row / a.q_heads / a.T, t = row / a.q_heads % a.T;
-    const int head = int(row % a.q_heads), kv = head / (a.q_heads / p.c.heads), D = p.c.dim;
+    const int head = int(row % a.q_heads), kv = head / (a.q_heads / p.c.heads);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    T *out = static_cast<T *>(a.out) + row * D;
     const int64_t nq = query_length(a, s);
-    float q[kMostDims], o[kMostDims], m = -__builtin_inff(), sum = 0.0f;
-    const T *src = static_cast<const T *>(a.q) + s * a.q_stride_seq + t * a.q_stride_token + head * a.q_stride_head;
-    for (int i = 0; i < kMostDims; ++i) {
-        const int d = lane + kWave * i;
-        q[i] = d < D ? to_float(src[d]) : 0.0f;
-        o[i] = 0.0f;
-    }
-    auto attend = [&](const PageTable &table, int64_t seen) {
-        for (int64_t j = wave; j < seen; j += kRowWaves) {
-            int64_t entry;
-            const int64_t page = table.page(p.c, j, entry);
-            if (page < 0) continue;
-            const T *k = static_cast<const T *>(p.c.k) + page * p.c.k_stride_page + entry * p.c.k_stride_token +
-                         kv * p.c.k_stride_head;
-            const T *v = static_cast<const T *>(p.c.v) + page * p.c.v_stride_page + entry * p.c.v_stride_token +
-                         kv * p.c.v_stride_head;
-            float x = 0.0f;
-            for (int i = 0; i < kMostDims; ++i)
-                if (const int d = lane + kWave * i; d < D) x = __builtin_fmaf(q[i], to_float(k[d]), x);
-            x = lanes_sum(x) * a.scale;
-            if (!(x <= m)) {   // a NaN score makes the row NaN
-                const float f = expf(m - x);
-                sum *= f;
-                for (int i = 0; i < kMostDims; ++i) o[i] *= f;
-                m = x;
-            }
-            const float w = x == -__builtin_inff() ? 0.0f : expf(x - m);
-            sum += w;
-            for (int i = 0; i < kMostDims; ++i)
-                if (const int d = lane + kWave * i; d < D) o[i] = __builtin_fmaf(w, to_float(v[d]), o[i]);
-        }
-    };
+    RowPart<T> r;
+    r.load(p, s, t, head, lane);
     if (t < nq) {
         if (a.G > 0) {
             const PageTable prefix = prefix_table(p, s / (a.S / a.G));
-            attend(prefix, prefix.count);
+            for (int64_t j = wave; j < prefix.count; j += kRowWaves) r.take(p, prefix, j, kv, lane);
         }
         if (a.pages) {
             const PageTable own = own_table(p, s);
-            attend(own, min(own.count, own.count - nq + t + 1));
+            for (int64_t j = wave; j < min(own.count, own.count - nq + t + 1); j += kRowWaves) r.take(p, own, j, kv, lane);
         }
     }
-    __shared__ float part[kRowWaves][2], sums[kRowWaves][NGPU_LM_MAX_HEAD_DIM];
-    if (lane == 0) part[wave][0] = m, part[wave][1] = sum;
-    for (int i = 0; i < kMostDims; ++i) sums[wave][lane + kWave * i] = o[i];
+    __shared__ float2 stats[kRowWaves];
+    __shared__ float sums[kRowWaves][NGPU_LM_MAX_HEAD_DIM];
+    if (lane == 0) stats[wave] = make_float2(r.m, r.sum);
+#pragma unroll
+    for (int i = 0; i < r.kDims; ++i) sums[wave][lane + kWave * i] = r.o[i];
     __syncthreads();
-    float mm = part[0][0], total = 0.0f, f[kRowWaves];
-    for (int w = 1; w < kRowWaves; ++w) mm = part[w][0] > mm ? part[w][0] : mm;
-    for (int w = 0; w < kRowWaves; ++w) {
-        f[w] = part[w][0] == -__builtin_inff() ? 0.0f : expf(part[w][0] - mm);
-        total += part[w][1] * f[w];
+    if (wave != 0) return;
+    float top = stats[0].x, total = 0.0f, f[kRowWaves];
+    for (int w = 1; w < kRowWaves; ++w) top = stats[w].x > top ? stats[w].x : top;
+    for (int w = 0; w < kRowWaves; ++w) {   // (a part without a key: sum 0, whatever the factor)
+        f[w] = stats[w].x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(stats[w].x - top);
+        total += stats[w].y * f[w];
     }
-    for (int d = threadIdx.x; d < D; d += kRowWaves * kWave) {
-        float x = 0.0f;
-        for (int w = 0; w < kRowWaves; ++w) x += sums[w][d] * f[w];
-        out[d] = from_float<T>(mm == -__builtin_inff() ? 0.0f : x / total);
+    r.m = top;
+    r.sum = total;
+#pragma unroll
+    for (int i = 0; i < r.kDims; ++i) {
+        r.o[i] = 0.0f;
+        for (int w = 0; w < kRowWaves; ++w) r.o[i] += sums[w][lane + kWave * i] * f[w];
     }
-    if (a.lse && threadIdx.x == 0) a.lse[row] = mm == -__builtin_inff() ? mm : mm + logf(total);
+    r.finish(p, row, lane, t < nq);
 }
 
 template <class T>
@@ -199,8 +166,8 @@ bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
 }
 
 void cut_rows(int64_t rows, int steps, int &tiles, int &waves, int &blocks) {
-    tiles = rows <= 16 || (rows > 64 && steps > 4) ? 1 : 2;
-    waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : 4);
+    tiles = rows <= 16 || steps > 4 ? 1 : 2;
+    waves = rows <= 16 * tiles ? 1 : (rows <= 32 * tiles ? 2 : 4);
     blocks = int((rows + 16 * tiles * waves - 1) / (16 * tiles * waves));
 }
 
@@ -210,18 +177,28 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     if (!r.tiles) return r;
     r.steps = c.dim <= 64 ? 2 : (c.dim <= 96 ? 3 : (c.dim <= 128 ? 4 : 8));
     const int64_t rep = a.q_heads / c.heads;
-    auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int &tiles, int &waves) {
+    auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int64_t wanted, int &tiles, int &waves) {
         Cut u{problems, 0, 0};
         cut_rows(rows, r.steps, tiles, waves, u.blocks);
-        const int64_t tile = waves == 4 ? 64 : 32, have = problems * u.blocks, wanted = 2 * kCus;
+        const int64_t tile = waves == 4 ? 64 : 32, have = problems * u.blocks;
         const int64_t most = std::max<int64_t>(1, (most_keys + 2 * tile - 1) / (2 * tile));
         u.splits = int(std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, wanted / have)));
         return u;
     };
-    if (a.G > 0)
-        r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size, r.prefix_tiles,
-                            r.prefix_waves);
-    if (a.pages) r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, r.own_tiles, r.own_waves);
+    // Workgroups a CU: more of them only disturb each other's streams.  One prefix
+    // of 100000 tokens for 5 x 4 rows, 8 heads of 128, us: 238 / 205 / 214 / 273 with 2 / 3 /
+    // 4 / 5; heads of 64: 67 / 51 / 49 / 52; of 256 (2 fit): 48, 62 with 3.
+    const int64_t per_cu = r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2);
+    if (a.pages)
+        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, kCus, r.own_tiles, r.own_waves);
+    if (a.G > 0) {
+        const int64_t left = per_cu * kCus - r.plan.own.works();
+        r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size,
+                            std::max<int64_t>(left, 2 * kCus), r.prefix_tiles, r.prefix_waves);
+        if (r.prefix_waves == 4)
+            r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size, 2 * kCus,
+                                r.prefix_tiles, r.prefix_waves);
+    }
     r.plan.parts = r.plan.prefix.splits + r.plan.own.splits;
     const int64_t rows = a.S * a.T * a.q_heads;
     r.plan.sums = reinterpret_cast<float *>(workspace);
@@ -247,11 +224,11 @@ hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int6
 template <class T, int DK>
 hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int tiles, int waves, int64_t w0, int64_t w1,
                        hipStream_t stream) {
-    if (waves == 1)
-        return tiles == 1 ? launch_tile<T, DK, 1, 1>(p, plan, w0, w1, stream)
-                          : launch_tile<T, DK, 2, 1>(p, plan, w0, w1, stream);
-    if (waves == 2) return launch_tile<T, DK, 2, 2>(p, plan, w0, w1, stream);
-    return launch_tile<T, DK, (DK <= 4 ? 2 : 1), 4>(p, plan, w0, w1, stream);
+    constexpr int kMost = DK <= 4 ? 2 : 1;   // tiles a wavefront's registers hold
+    if (waves == 1 && tiles == 1) return launch_tile<T, DK, 1, 1>(p, plan, w0, w1, stream);
+    if (waves == 1) return launch_tile<T, DK, kMost, 1>(p, plan, w0, w1, stream);
+    if (waves == 2) return launch_tile<T, DK, kMost, 2>(p, plan, w0, w1, stream);
+    return launch_tile<T, DK, kMost, 4>(p, plan, w0, w1, stream);
 }
 template <class T>
 hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, int64_t w0, int64_t w1,

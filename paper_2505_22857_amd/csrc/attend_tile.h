@@ -24,6 +24,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "cache.h"
 #include "walk.h"
 
@@ -31,6 +33,7 @@ namespace ngpu {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
 struct Attend {
     ngpu_kv_cache_t c;
@@ -66,6 +69,59 @@ struct AttendPlan {
 // 16 bytes of zeros, which stand for keys and dimensions that do not exist.
 static __device__ __attribute__((aligned(16))) unsigned kNoData[4];
 
+// One row's running maximum (in log2) and sums, a wavefront's lanes holding every
+// 64th dimension: for what the matrix instructions do not take.
+template <class T>
+struct RowPart {
+    static constexpr int kDims = NGPU_LM_MAX_HEAD_DIM / kWave;
+    float q[kDims], o[kDims], m = -__builtin_inff(), sum = 0.0f;
+    __device__ __forceinline__ void load(const Attend &p, int64_t s, int64_t t, int head, int lane) {
+        const T *src = static_cast<const T *>(p.a.q) + s * p.a.q_stride_seq + t * p.a.q_stride_token +
+                       head * p.a.q_stride_head;
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) {
+            q[i] = lane + kWave * i < p.c.dim ? to_float(src[lane + kWave * i]) : 0.0f;
+            o[i] = 0.0f;
+        }
+    }
+    __device__ __forceinline__ void take(const Attend &p, const PageTable &table, int64_t j, int kv, int lane) {
+        int64_t entry;
+        const int64_t page = table.page(p.c, j, entry);
+        if (page < 0) return;
+        const T *k = static_cast<const T *>(p.c.k) + page * p.c.k_stride_page + entry * p.c.k_stride_token +
+                     kv * p.c.k_stride_head;
+        const T *v = static_cast<const T *>(p.c.v) + page * p.c.v_stride_page + entry * p.c.v_stride_token +
+                     kv * p.c.v_stride_head;
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kDims; ++i)
+            if (const int d = lane + kWave * i; d < p.c.dim) x = __builtin_fmaf(q[i], to_float(k[d]), x);
+        for (int d = kWave / 2; d > 0; d /= 2) x += __shfl_xor(x, d);
+        x *= p.a.scale * 1.44269504088896f;
+        if (!(x <= m)) {   // a NaN score makes the row NaN
+            const float f = __builtin_amdgcn_exp2f(m - x);
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < kDims; ++i) o[i] *= f;
+            m = x;
+        }
+        const float w = x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x - m);
+        sum += w;
+#pragma unroll
+        for (int i = 0; i < kDims; ++i)
+            if (const int d = lane + kWave * i; d < p.c.dim) o[i] = __builtin_fmaf(w, to_float(v[d]), o[i]);
+    }
+    // the finished row; `counts`: of a query token that counts
+    __device__ __forceinline__ void finish(const Attend &p, int64_t row, int lane, bool counts) const {
+        const bool any = counts && sum != 0.0f;   // (a NaN sum too)
+        if (p.a.lse && lane == 0) p.a.lse[row] = any ? m * 0.69314718056f + logf(sum) : -__builtin_inff();
+        T *dst = static_cast<T *>(p.a.out) + row * p.c.dim;
+#pragma unroll
+        for (int i = 0; i < kDims; ++i)
+            if (const int d = lane + kWave * i; d < p.c.dim) dst[d] = from_float<T>(any ? o[i] / sum : 0.0f);
+    }
+};
+
 template <class T>
 using LdsPtr = __attribute__((address_space(3))) T *;
 
@@ -73,7 +129,7 @@ template <class T>
 struct Matrix;
 template <>
 struct Matrix<Bf16> {
-    static constexpr short kExponent = 0x7f80;
+    static constexpr unsigned short kInfinity = 0x7f80;   // its bits
     static __device__ __forceinline__ f32x4 mul(s16x8 a, s16x8 b, f32x4 c) {
         typedef __bf16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -86,7 +142,7 @@ struct Matrix<Bf16> {
 };
 template <>
 struct Matrix<F16> {
-    static constexpr short kExponent = 0x7c00;
+    static constexpr unsigned short kInfinity = 0x7c00;
     static __device__ __forceinline__ f32x4 mul(s16x8 a, s16x8 b, f32x4 c) {
         typedef _Float16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -97,6 +153,11 @@ struct Matrix<F16> {
         return __builtin_bit_cast(s16x8, __builtin_convertvector(f8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, v8));
     }
 };
+
+template <class T>
+__device__ __forceinline__ LdsPtr<T> lds_at(unsigned at) {
+    return (LdsPtr<T>)(uintptr_t)at;
+}
 
 // Maximum over the four lanes that hold a row (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_max(float x) {
@@ -130,7 +191,10 @@ __device__ __forceinline__ void load_to_lds(const void *p, unsigned at) {
 
 // The same from a uniform address and a lane's offset.
 template <bool ONCE>
-__device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned at) {
+__device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, unsigned at) {
+    const uint64_t a = reinterpret_cast<uint64_t>(from);   // (the compiler may hold it in vector registers)
+    const uint64_t base = uint64_t(unsigned(__builtin_amdgcn_readfirstlane(int(a >> 32)))) << 32 |
+                          unsigned(__builtin_amdgcn_readfirstlane(int(a)));
     if (ONCE)
         asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(at), "v"(offset), "s"(base) : "memory");
     else
@@ -167,7 +231,7 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
                                                                                    unsigned work0) {
     using A = AttendTile<T, DK, RT, WR>;
     using M = Matrix<T>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(512))) char lds[];   // (a row's pieces are found by exclusive or)
     unsigned (*masks)[4] = nullptr;   // per stage, the keys of each loading wavefront that exist
     if constexpr (WR > 1) {
         __shared__ unsigned shared_masks[2][4];
@@ -215,8 +279,6 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     // this wavefront's query rows: operand registers, and the keys each row sees
     s16x8 q[RT][DK];
     int limit[RT];
-    int out_row[RT];   // -1: no row
-    bool counts[RT];   // a query token that counts
     const bool aligned = (reinterpret_cast<uintptr_t>(a.q) % 16 == 0) && a.q_stride_seq % 8 == 0 &&
                          a.q_stride_token % 8 == 0 && a.q_stride_head % 8 == 0;
     const short flip = a.scale < 0.0f ? short(0x8000) : short(0);   // the scores' sign, so that the factor is not negative
@@ -228,9 +290,7 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
         const unsigned i = is ? row : 0, token = i / unsigned(rep);
         const int s = s0 + int(token / unsigned(T_)), t = int(token % unsigned(T_));
         const int head = h * rep + int(i - token * unsigned(rep));
-        out_row[r] = is ? (s * T_ + t) * a.q_heads + head : -1;
         const int nq = int(query_length(a, s));
-        counts[r] = t < nq;
         limit[r] = count;
         if (own) {
             limit[r] = min(count, max(0, count - nq + t + 1));
@@ -262,13 +322,6 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     // Where a wavefront's keys lie in one page and a row has no missing
     // dimensions, a lane's offsets are the same for every tile.
     const bool in_page = page_size % A::kLoad == 0 && D == 32 * DK && k_token < (1u << 21) && v_token < (1u << 21);
-    unsigned k_off[A::kLoads], v_off[A::kLoads];
-#pragma unroll
-    for (int u = 0; u < A::kLoads; ++u) {
-        const int row = u * A::kPerLoad + in_load, full = wave * A::kLoad + row;
-        k_off[u] = (unsigned(row) * k_token + unsigned(piece ^ A::key_swizzle(full))) * 16;
-        v_off[u] = (unsigned(row) * v_token + unsigned(piece ^ A::value_swizzle(full))) * 16;
-    }
     unsigned valid = 0;   // keys that exist among those this wavefront loaded last
     auto fetch = [&](int tile, int stage) {
         const bool is = page >= 0 && page < p.c.num_pages;   // (-1 past the end)
@@ -282,13 +335,19 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
             const unsigned e0 = __builtin_amdgcn_readfirstlane(entry), p0 = __builtin_amdgcn_readfirstlane(page);
             const char *kb = k_head + (p0 * k_page + e0 * uint64_t(k_token)) * 16;
             const char *vb = v_head + (p0 * v_page + e0 * uint64_t(v_token)) * 16;
+            unsigned k_row = unsigned(in_load) * k_token * 16, v_row = unsigned(in_load) * v_token * 16;
+            int first = wave * A::kLoad + in_load;
+            asm volatile("" : "+v"(k_row), "+v"(v_row), "+v"(first));   // computed here, not kept in registers for it
 #pragma unroll
             for (int u = 0; u < A::kLoads; ++u) {
-                const int full = wave * A::kLoad + u * A::kPerLoad + in_load;
-                if (4 * DK == A::kPieces || (piece ^ A::key_swizzle(full)) < 4 * DK)
-                    load_to_lds<A::kOnce>(kb, k_off[u], at + u * kWave * 16);
-                if (4 * DK == A::kPieces || (piece ^ A::value_swizzle(full)) < 4 * DK)
-                    load_to_lds<A::kOnce>(vb, v_off[u], at + A::kKeys * A::kPitch + u * kWave * 16);
+                const int kp = piece ^ A::key_swizzle(first + u * A::kPerLoad);
+                const int vp = piece ^ A::value_swizzle(first + u * A::kPerLoad);
+                if (4 * DK == A::kPieces || kp < 4 * DK)
+                    load_to_lds<A::kOnce>(kb + uint64_t(u * A::kPerLoad) * k_token * 16, k_row + unsigned(kp) * 16,
+                                          at + u * kWave * 16);
+                if (4 * DK == A::kPieces || vp < 4 * DK)
+                    load_to_lds<A::kOnce>(vb + uint64_t(u * A::kPerLoad) * v_token * 16, v_row + unsigned(vp) * 16,
+                                          at + A::kKeys * A::kPitch + u * kWave * 16);
             }
             return;
         }
@@ -308,18 +367,15 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
                                                   : reinterpret_cast<const char *>(kNoData);
             load_to_lds<A::kOnce>(ks, at + u * kWave * 16);
             load_to_lds<A::kOnce>(vs, at + A::kKeys * A::kPitch + u * kWave * 16);
+            __builtin_amdgcn_sched_barrier(0);   // (addresses of all loads at once would not fit the registers)
         }
     };
 
-    // this lane's places in a tile: the operand rows of K and the blocks of V
-    unsigned k_at[DK], v_at[A::kTiles];
-#pragma unroll
-    for (int k = 0; k < DK; ++k) k_at[k] = unsigned(col * A::kPitch + 16 * ((4 * k + quad) ^ A::key_swizzle(col)));
-#pragma unroll
-    for (int d = 0; d < A::kTiles; ++d) {
-        const int row = 4 * quad + col / 4;
-        v_at[d] = unsigned(row * A::kPitch + 16 * ((2 * d + (col % 4) / 2) ^ A::value_swizzle(row)) + 8 * (col & 1));
-    }
+    // This lane's places in a tile: step 0 of its operand row of K, dimensions 0 of its blocks of V; step k
+    // is at the first XOR 64 k, dimensions 16 d at the second XOR 32 d.
+    const int v_in = 4 * quad + col / 4;
+    const unsigned k_first = unsigned(col * A::kPitch + 16 * (quad ^ A::key_swizzle(col)));
+    const unsigned v_first = unsigned(v_in * A::kPitch + 16 * (((col % 4) / 2) ^ A::value_swizzle(v_in)) + 8 * (col & 1));
 
     f32x4 o[RT][A::kTiles];
     float m[RT], sum[RT];   // sum: of the weights of this lane's keys, before they are rounded
@@ -330,7 +386,111 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
 #pragma unroll
         for (int d = 0; d < A::kTiles; ++d) o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const float to_log2 = __builtin_fabsf(a.scale) * 1.44269504088896f;
+    // (a factor of 0 would make NaN of the -inf of a key that is not seen)
+    const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.scale) * 1.44269504088896f, 1e-30f);
+
+    // A value that is not finite would reach the rows that do not see its key (0 *
+    // inf): where a tile holds such keys and values, the rows are computed one by one at the end.
+    bool one_by_one = false;
+    // 32 keys of a tile into every row's sums: those whose bit of `exists` is set.
+    auto take = [&](int stage, int chunk, int key0, unsigned exists) {
+        const unsigned tile_at = lds0 + unsigned(stage * A::kStage + chunk * 32 * A::kPitch);
+        unsigned k_at = tile_at + k_first, v_at = tile_at + A::kKeys * A::kPitch + v_first;
+        asm volatile("" : "+v"(k_at), "+v"(v_at));   // their steps are computed below, not kept in registers
+        // Operands are loaded a step ahead, and no further: hoisted loads would not fit the registers.
+        f32x4 x[RT][2];
+        s16x8 kx[2][2], vx[2];
+        auto load_keys = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) kx[k & 1][u] = *lds_at<s16x8>((k_at ^ unsigned(64 * k)) + u * 16 * A::kPitch);
+        };
+        auto load_values = [&](int d) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    lds_at<s16x4>((v_at ^ unsigned(32 * d)) + u * 16 * A::kPitch));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vx[d & 1][4 * u + e] = part[e];
+            }
+        };
+        load_keys(0);
+#pragma unroll
+        for (int k = 0; k < DK; ++k) {
+            if (k + 1 < DK)
+                load_keys(k + 1);
+            else
+                load_values(0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    x[r][u] = M::mul(kx[k & 1][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool some_rows = own && key0 + 32 > least;   // some rows do not see some of the keys
+        if (exists != 0xffffffffu || some_rows) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                // the row's view of this lane's keys: bit 16 u + i is key 16 u + 4 quad + i
+                const int below = limit[r] - key0 - 4 * quad;
+                const unsigned sees = exists >> (4 * quad) &
+                                      (below >= 32 ? 0xffffffffu : (below > 0 ? (1u << below) - 1u : 0u));
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[r][e / 4][e % 4] = sees >> (16 * (e / 4) + e % 4) & 1u ? x[r][e / 4][e % 4] : -__builtin_inff();
+            }
+            if (some_rows) {
+                u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
+                for (int i = lane; i < 2 * A::kPitch; i += kWave)
+                    most = __builtin_elementwise_max(
+                        most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) odd |= most[e] >= M::kInfinity;
+                if (__ballot(odd)) one_by_one = true;
+            }
+        }
+        float top[RT];
+        bool rises = false;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            top[r] = x[r][0][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
+            top[r] *= to_log2;
+            rises |= top[r] > m[r] + 8.0f;   // (also while m is -inf)
+        }
+        if (__ballot(rises)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float now = __builtin_fmaxf(m[r], row_max(top[r]));
+                const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
+                m[r] = now;
+                sum[r] *= f;
+#pragma unroll
+                for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
+            }
+        }
+        s16x8 weights[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
+            float z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][e / 4][e % 4], to_log2, -base));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[r] += z[e];
+            weights[r] = M::round(z);
+        }
+#pragma unroll
+        for (int d = 0; d < A::kTiles; ++d) {
+            if (d + 1 < A::kTiles) load_values(d + 1);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) o[r][d] = M::mul(vx[d & 1], weights[r], o[r][d]);
+            if (d % 2) __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 
     if (tile0 < tile1) fetch(tile0, 0);
     for (int tile = tile0; tile < tile1; ++tile) {
@@ -345,123 +505,16 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
             next_page = page_of(tile + 2);
             fetch(tile + 1, stage ^ 1);
         }
-        const char *keys = lds + stage * A::kStage;
-        const char *values = keys + A::kKeys * A::kPitch;
         const int key0 = tile * A::kKeys;
-        // which of the keys exist
-        unsigned exists[A::kChunks];
-        bool partial = own && key0 + 32 * A::kChunks > least;   // some rows do not see some of them
-        const bool some_rows = partial;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < A::kChunks; ++c) {
-            exists[c] = mine;
+            unsigned exists = mine;
             if (WR > 1) {
                 const int first = c * 32 / A::kLoad;
-                exists[c] = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
+                exists = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
             }
-            exists[c] = __builtin_amdgcn_readfirstlane(exists[c]);
-            partial |= exists[c] != 0xffffffffu;
-        }
-
-        f32x4 x[RT][2 * A::kChunks];
-#pragma unroll
-        for (int k = 0; k < DK; ++k)
-#pragma unroll
-            for (int u = 0; u < 2 * A::kChunks; ++u) {
-                const s16x8 kx = *reinterpret_cast<const s16x8 *>(keys + u * 16 * A::kPitch + k_at[k]);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    x[r][u] = M::mul(kx, q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][u]);
-            }
-        s16x8 weights[RT][A::kChunks];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (partial) {
-#pragma unroll
-                for (int e = 0; e < 8 * A::kChunks; ++e) {
-                    const int key = 16 * (e / 4 % 2) + 4 * quad + e % 4;
-                    const bool sees = ((exists[e / 8] >> key) & 1u) && key0 + e / 8 * 32 + key < limit[r];
-                    x[r][e / 4][e % 4] = sees ? x[r][e / 4][e % 4] : -__builtin_inff();
-                }
-            }
-            float top = x[r][0][0];
-#pragma unroll
-            for (int e = 1; e < 8 * A::kChunks; ++e) top = __builtin_fmaxf(top, x[r][e / 4][e % 4]);
-            top *= to_log2;
-            if (__ballot(top > m[r] + 8.0f)) {   // (also while m is -inf)
-                const float now = __builtin_fmaxf(m[r], row_max(top));
-                const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
-                m[r] = now;
-                sum[r] *= f;
-#pragma unroll
-                for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
-            }
-            const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
-#pragma unroll
-            for (int c = 0; c < A::kChunks; ++c) {
-                float z[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4], to_log2, -base));
-                if (partial) {   // (a score of -inf times a factor of 0 is NaN)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int key = 16 * (e / 4) + 4 * quad + e % 4;
-                        z[e] = ((exists[c] >> key) & 1u) && key0 + c * 32 + key < limit[r] ? z[e] : 0.0f;
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[r] += z[e];
-                weights[r][c] = M::round(z);
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < A::kChunks; ++c) {
-#pragma unroll
-            for (int d = 0; d < A::kTiles; ++d) {
-                s16x8 vx;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (LdsPtr<s16x4>)(const_cast<char *>(values + (c * 32 + u * 16) * A::kPitch + v_at[d])));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) vx[4 * u + e] = part[e];
-                }
-                if (some_rows) {
-                    // A value that is not finite must not reach the rows that do not see its key (0 * inf): it
-                    // is left out here and added below to the rows that do.
-                    bool odd = false;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool bad = (vx[e] & M::kExponent) == M::kExponent;
-                        odd |= bad;
-                        vx[e] = bad ? short(0) : vx[e];
-                    }
-                    if (__ballot(odd)) {
-                        for (int key = 0; key < 32; ++key) {
-                            const int row = c * 32 + key;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int dim = 16 * d + 4 * quad + i;
-                                const T v = *reinterpret_cast<const T *>(
-                                    values + row * A::kPitch + 16 * ((dim / 8) ^ A::value_swizzle(row)) + 2 * (dim % 8));
-                                const bool bad = (short(v.bits) & M::kExponent) == M::kExponent;
-#pragma unroll
-                                for (int r = 0; r < RT; ++r) {
-                                    int z = 0;   // the row's weight of this key
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) z = key / 16 * 4 + key % 4 == e ? weights[r][c][e] : z;
-                                    z = __shfl(z, key % 16 / 4 * 16 + col);
-                                    if (bad && key0 + row < limit[r])
-                                        o[r][d][i] += to_float(T{uint16_t(z)}) * to_float(v);
-                                }
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) o[r][d] = M::mul(vx, weights[r][c], o[r][d]);
-            }
+            exists = __builtin_amdgcn_readfirstlane(exists);
+            take(stage, c, key0 + 32 * c, exists);
         }
     }
 
@@ -470,22 +523,46 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     for (int r = 0; r < RT; ++r) total[r] = row_sum(sum[r]);
     const int64_t all_rows = a.S * a.T * a.q_heads;
     const int part = (own ? plan.prefix.splits : 0) + split;
+    if (one_by_one) {
+        for (unsigned i = 0; i < 16 * RT; ++i) {
+            const unsigned row = unsigned(block) * A::kRows + unsigned(wave) * 16 * RT + i;
+            if (row >= rows) break;
+            const int t = int(row / unsigned(rep)), head = h * rep + int(row % unsigned(rep));   // (own: one sequence)
+            const int nq = int(query_length(a, s0)), sees = max(0, min(count, count - nq + t + 1));
+            RowPart<T> r;
+            r.load(p, s0, t, head, lane);
+            for (int j = tile0 * A::kKeys; j < min(tile1 * A::kKeys, sees); ++j) r.take(p, table, j, h, lane);
+            const int64_t out = (int64_t(s0) * T_ + t) * a.q_heads + head;
+            if (plan.parts > 1) {
+                if (lane == 0) plan.stats[part * all_rows + out] = make_float2(r.m, r.sum);
+#pragma unroll
+                for (int e = 0; e < r.kDims; ++e)
+                    if (const int d = lane + kWave * e; d < D) plan.sums[(part * all_rows + out) * D + d] = r.o[e];
+            } else {
+                r.finish(p, out, lane, t < nq);
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        if (out_row[r] < 0) continue;
+        const unsigned i = unsigned(block) * A::kRows + (wave * RT + r) * 16 + col, token = i / unsigned(rep);
+        if (i >= rows) continue;
+        const int s = s0 + int(token / unsigned(T_)), t = int(token % unsigned(T_));
+        const int64_t row = int64_t(s * T_ + t) * a.q_heads + h * rep + int(i - token * unsigned(rep));
         if (plan.parts > 1) {
-            if (quad == 0) plan.stats[part * all_rows + out_row[r]] = make_float2(m[r], total[r]);
+            if (quad == 0) plan.stats[part * all_rows + row] = make_float2(m[r], total[r]);
             if (total[r] == 0.0f) continue;
-            float *dst = plan.sums + (part * all_rows + out_row[r]) * D;
+            float *dst = plan.sums + (part * all_rows + row) * D;
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d)
                 if (const int at = 16 * d + 4 * quad; at < D) *reinterpret_cast<f32x4 *>(dst + at) = o[r][d];
         } else {
-            const bool any = counts[r] && total[r] != 0.0f;   // (a NaN sum too)
+            const bool any = t < query_length(a, s) && total[r] != 0.0f;   // (a NaN sum too)
             if (a.lse && quad == 0)
-                a.lse[out_row[r]] = any ? (m[r] == -__builtin_inff() ? total[r] : m[r] * 0.69314718056f + logf(total[r]))
+                a.lse[row] = any ? (m[r] == -__builtin_inff() ? total[r] : m[r] * 0.69314718056f + logf(total[r]))
                                         : -__builtin_inff();
-            T *dst = static_cast<T *>(a.out) + int64_t(out_row[r]) * D;
+            T *dst = static_cast<T *>(a.out) + row * D;
             const float f = 1.0f / total[r];
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d) {
