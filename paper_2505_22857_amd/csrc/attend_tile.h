@@ -33,6 +33,7 @@ namespace ngpu {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
 struct Attend {
@@ -134,10 +135,9 @@ struct Matrix<Bf16> {
         typedef __bf16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
-    static __device__ __forceinline__ s16x8 round(const float (&x)[8]) {
-        typedef __bf16 v8 __attribute__((ext_vector_type(8)));
-        typedef float f8 __attribute__((ext_vector_type(8)));
-        return __builtin_bit_cast(s16x8, __builtin_convertvector(f8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, v8));
+    static __device__ __forceinline__ unsigned round(float a, float b) {
+        typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(unsigned, v2{__bf16(a), __bf16(b)});
     }
 };
 template <>
@@ -147,10 +147,9 @@ struct Matrix<F16> {
         typedef _Float16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
-    static __device__ __forceinline__ s16x8 round(const float (&x)[8]) {
-        typedef _Float16 v8 __attribute__((ext_vector_type(8)));
-        typedef float f8 __attribute__((ext_vector_type(8)));
-        return __builtin_bit_cast(s16x8, __builtin_convertvector(f8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, v8));
+    static __device__ __forceinline__ unsigned round(float a, float b) {
+        typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(unsigned, v2{_Float16(a), _Float16(b)});
     }
 };
 
@@ -392,56 +391,66 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     // A value that is not finite would reach the rows that do not see its key (0 *
     // inf): where a tile holds such keys and values, the rows are computed one by one at the end.
     bool one_by_one = false;
-    // 32 keys of a tile into every row's sums: those whose bit of `exists` is set.
-    auto take = [&](int stage, int chunk, int key0, unsigned exists) {
-        const unsigned tile_at = lds0 + unsigned(stage * A::kStage + chunk * 32 * A::kPitch);
+    // A tile's keys into every row's sums: those whose bit of `exists` is set.
+    auto take = [&](int stage, int key0, const unsigned (&exists)[A::kChunks]) {
+        constexpr int C = A::kChunks;
+        const unsigned tile_at = lds0 + unsigned(stage * A::kStage);
         unsigned k_at = tile_at + k_first, v_at = tile_at + A::kKeys * A::kPitch + v_first;
         asm volatile("" : "+v"(k_at), "+v"(v_at));   // their steps are computed below, not kept in registers
         // Operands are loaded a step ahead, and no further: hoisted loads would not fit the registers.
-        f32x4 x[RT][2];
+        f32x4 x[RT][2 * C];
         s16x8 kx[2][2], vx[2];
-        auto load_keys = [&](int k) {
+        auto load_keys = [&](int i) {   // 32 keys of step i mod DK
 #pragma unroll
-            for (int u = 0; u < 2; ++u) kx[k & 1][u] = *lds_at<s16x8>((k_at ^ unsigned(64 * k)) + u * 16 * A::kPitch);
+            for (int u = 0; u < 2; ++u)
+                kx[i & 1][u] = *lds_at<s16x8>((k_at ^ unsigned(64 * (i % DK))) + (i / DK * 2 + u) * 16 * A::kPitch);
         };
-        auto load_values = [&](int d) {
+        auto load_values = [&](int i) {   // 32 keys, dimensions 16 (i mod kTiles) on
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    lds_at<s16x4>((v_at ^ unsigned(32 * d)) + u * 16 * A::kPitch));
+                const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(
+                    (v_at ^ unsigned(32 * (i % A::kTiles))) + (i / A::kTiles * 2 + u) * 16 * A::kPitch));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) vx[d & 1][4 * u + e] = part[e];
+                for (int e = 0; e < 4; ++e) vx[i & 1][4 * u + e] = part[e];
             }
         };
         load_keys(0);
 #pragma unroll
-        for (int k = 0; k < DK; ++k) {
-            if (k + 1 < DK)
-                load_keys(k + 1);
+        for (int i = 0; i < C * DK; ++i) {
+            if (i + 1 < C * DK)
+                load_keys(i + 1);
             else
                 load_values(0);
+            const int c = i / DK, k = i % DK;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
-                    x[r][u] = M::mul(kx[k & 1][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][u]);
+                    x[r][2 * c + u] = M::mul(kx[i & 1][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        const bool some_rows = own && key0 + 32 > least;   // some rows do not see some of the keys
-        if (exists != 0xffffffffu || some_rows) {
+        const bool some_rows = own && key0 + A::kKeys > least;   // some rows do not see some of the keys
+        bool all = !some_rows;
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                // the row's view of this lane's keys: bit 16 u + i is key 16 u + 4 quad + i
-                const int below = limit[r] - key0 - 4 * quad;
-                const unsigned sees = exists >> (4 * quad) &
-                                      (below >= 32 ? 0xffffffffu : (below > 0 ? (1u << below) - 1u : 0u));
+        for (int c = 0; c < C; ++c) all = all && exists[c] == 0xffffffffu;
+        if (!all) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[r][e / 4][e % 4] = sees >> (16 * (e / 4) + e % 4) & 1u ? x[r][e / 4][e % 4] : -__builtin_inff();
-            }
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    // the row's view of this lane's keys: bit 16 u + i is key 16 u + 4 quad + i
+                    const int below = limit[r] - key0 - 32 * c - 4 * quad;
+                    const unsigned sees = exists[c] >> (4 * quad) &
+                                          (below >= 32 ? 0xffffffffu : (below > 0 ? (1u << below) - 1u : 0u));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[r][2 * c + e / 4][e % 4] = sees >> (16 * (e / 4) + e % 4) & 1u ? x[r][2 * c + e / 4][e % 4]
+                                                                                       : -__builtin_inff();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             if (some_rows) {
                 u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
-                for (int i = lane; i < 2 * A::kPitch; i += kWave)
+                for (int i = lane; i < A::kKeys * A::kPieces; i += kWave)
                     most = __builtin_elementwise_max(
                         most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
                 bool odd = false;
@@ -456,7 +465,7 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
         for (int r = 0; r < RT; ++r) {
             top[r] = x[r][0][0];
 #pragma unroll
-            for (int e = 1; e < 8; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
+            for (int e = 1; e < 8 * C; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
             top[r] *= to_log2;
             rises |= top[r] > m[r] + 8.0f;   // (also while m is -inf)
         }
@@ -471,24 +480,38 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
                 for (int d = 0; d < A::kTiles; ++d) o[r][d] *= f;
             }
         }
-        s16x8 weights[RT];
+        float base[RT];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
-            float z[8];
+        for (int r = 0; r < RT; ++r) base[r] = m[r] == -__builtin_inff() ? 0.0f : m[r];
+        u32x4 weights[RT][C];   // of chunk c: pairs of rounded ones
+        auto weigh = [&](int c, int pair) {   // the pair-th of the chunk's 4 RT
+            const int r = pair / 4, e = pair % 4 * 2;
+            const float z0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4], to_log2, -base[r]));
+            const float z1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4 + 1], to_log2, -base[r]));
+            sum[r] += z0;
+            sum[r] += z1;
+            weights[r][c][pair % 4] = M::round(z0, z1);
+        };
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][e / 4][e % 4], to_log2, -base));
+        for (int i = 0; i < 4 * RT; ++i) weigh(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+        // the next chunk's weights are computed between the matrix instructions of this one
+        constexpr int kPairs = (4 * RT + A::kTiles - 1) / A::kTiles;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[r] += z[e];
-            weights[r] = M::round(z);
-        }
+        for (int i = 0; i < C * A::kTiles; ++i) {
+            const int c = i / A::kTiles, d = i % A::kTiles;
+            if (i + 1 < C * A::kTiles) load_values(i + 1);
 #pragma unroll
-        for (int d = 0; d < A::kTiles; ++d) {
-            if (d + 1 < A::kTiles) load_values(d + 1);
+            for (int r = 0; r < RT; ++r)
+                o[r][d] = M::mul(vx[i & 1], __builtin_bit_cast(s16x8, weights[r][c]), o[r][d]);
+            if (c + 1 < C) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) o[r][d] = M::mul(vx[d & 1], weights[r], o[r][d]);
-            if (d % 2) __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < kPairs; ++j)
+                    if (d * kPairs + j < 4 * RT) weigh(c + 1, d * kPairs + j);
+                __builtin_amdgcn_sched_barrier(0);
+            } else if (d % 2) {
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
 
@@ -506,16 +529,17 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
             fetch(tile + 1, stage ^ 1);
         }
         const int key0 = tile * A::kKeys;
-#pragma unroll 1
+        unsigned exists[A::kChunks];
+#pragma unroll
         for (int c = 0; c < A::kChunks; ++c) {
-            unsigned exists = mine;
+            exists[c] = mine;
             if (WR > 1) {
                 const int first = c * 32 / A::kLoad;
-                exists = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
+                exists[c] = masks[stage][first] | (A::kLoad == 16 ? masks[stage][first + 1] << 16 : 0u);
             }
-            exists = __builtin_amdgcn_readfirstlane(exists);
-            take(stage, c, key0 + 32 * c, exists);
+            exists[c] = __builtin_amdgcn_readfirstlane(exists[c]);
         }
+        take(stage, key0, exists);
     }
 
     float total[RT];
