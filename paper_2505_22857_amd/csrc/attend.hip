@@ -81,27 +81,40 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(Attend p, Att
     const bool counts = row < rows && token % a.T < query_length(a, token / a.T);
     float top = -__builtin_inff(), sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    // the parts of this row: its group's, then its sequence's own
+    int first = 0, skip = 0;   // parts of the prefix, and of its room that its group has not
+    if (plan.prefix.problems > 0) {
+        first = plan.prefix.splits;
+        if (plan.prefix.parts > plan.prefix.splits) {
+            const int lane = threadIdx.x % kWave;
+            const int n = dealt_splits(plan.prefix, int(a.G), lane < a.G ? prefix_table(p, lane).count : 0);
+            first = __shfl(n, row < rows ? int(token / a.T / (a.S / a.G)) : 0);
+        }
+        skip = plan.prefix.parts - first;
+    }
+    const int parts = first + plan.own.splits;
     auto factor = [](float m, float base) { return m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - base); };
     if (counts && d < D) {
-        for (int i = group; i < plan.parts; i += groups * kBatch) {
+        for (int i = group; i < parts; i += groups * kBatch) {
             float2 s[kBatch];
             f32x4 x[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {   // past the last part: the last again, for nothing
-                const int64_t at = min(i + u * groups, plan.parts - 1) * rows + row;
+                const int n = min(i + u * groups, parts - 1);
+                const int64_t at = (n < first ? n : n + skip) * rows + row;
                 s[u] = plan.stats[at];
                 x[u] = *reinterpret_cast<const f32x4 *>(plan.sums + at * D + d);
             }
             const float before = top;
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) top = i + u * groups < plan.parts ? __builtin_fmaxf(top, s[u].x) : top;
+            for (int u = 0; u < kBatch; ++u) top = i + u * groups < parts ? __builtin_fmaxf(top, s[u].x) : top;
             const float base = top == -__builtin_inff() ? 0.0f : top, f0 = factor(before, base);
             sum *= f0;
             o *= f0;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 // a part without a key (sum 0) has written no sums; a NaN sum goes on
-                const bool any = i + u * groups < plan.parts && s[u].y != 0.0f;
+                const bool any = i + u * groups < parts && s[u].y != 0.0f;
                 const float f = factor(s[u].x, base);
                 sum += any ? s[u].y * f : 0.0f;
 #pragma unroll
@@ -178,11 +191,11 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     r.steps = c.dim <= 64 ? 2 : (c.dim <= 96 ? 3 : (c.dim <= 128 ? 4 : 8));
     const int64_t rep = a.q_heads / c.heads;
     auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int64_t wanted, int &tiles, int &waves) {
-        Cut u{problems, 0, 0};
+        Cut u{problems, 0, 0, 0};
         cut_rows(rows, r.steps, tiles, waves, u.blocks);
         const int64_t tile = waves == 4 ? 64 : 32, have = problems * u.blocks;
         const int64_t most = std::max<int64_t>(1, (most_keys + 2 * tile - 1) / (2 * tile));
-        u.splits = int(std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, wanted / have)));
+        u.splits = u.parts = int(std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, wanted / have)));
         return u;
     };
     // Workgroups a CU: more of them only disturb each other's streams.  One prefix
@@ -199,7 +212,9 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
             r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size, 2 * kCus,
                                 r.prefix_tiles, r.prefix_waves);
     }
-    r.plan.parts = r.plan.prefix.splits + r.plan.own.splits;
+    if (a.G > 1 && a.G <= kDealt && r.plan.prefix.splits > 1)   // a group may take more than its share
+        r.plan.prefix.parts = int(std::min<int64_t>(2 * r.plan.prefix.splits, 1 + a.G * (r.plan.prefix.splits - 1)));
+    r.plan.parts = r.plan.prefix.parts + r.plan.own.splits;
     const int64_t rows = a.S * a.T * a.q_heads;
     r.plan.sums = reinterpret_cast<float *>(workspace);
     r.plan.stats = reinterpret_cast<float2 *>(workspace + size_t(r.plan.parts) * size_t(rows) * c.dim * 4);
@@ -248,7 +263,7 @@ hipError_t join(const Attend &p, const Choice &r, hipStream_t stream) {
     int lanes = 2;   // threads a row
     while (4 * lanes < p.c.dim) lanes *= 2;
     int groups = 1;   // sets of them, eight parts each
-    while (8 * groups < r.plan.parts && 2 * groups * lanes <= kJoinThreads) groups *= 2;
+    while (8 * groups < r.plan.prefix.splits + r.plan.own.splits && 2 * groups * lanes <= kJoinThreads) groups *= 2;
     const int64_t rows = a.S * a.T * a.q_heads, per = kJoinThreads / (lanes * groups), kMost = int64_t(1) << 23;
     for (int64_t r0 = 0; r0 < rows; r0 += kMost * per) {
         const int64_t grid = std::min(kMost, (rows - r0 + per - 1) / per);

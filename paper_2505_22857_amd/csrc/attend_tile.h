@@ -58,11 +58,30 @@ __device__ __forceinline__ PageTable own_table(const Attend &p, int64_t s) {
 struct Cut {
     int64_t problems;    // groups (or sequences) times cache heads
     int blocks, splits;
+    int parts;           // most splits of a problem: splits, or more where they are dealt by length
     __host__ __device__ int64_t works() const { return problems * blocks * splits; }
 };
+
+// Most groups whose splits are dealt by their lengths: a lane holds one.
+constexpr int kDealt = kWave;
+
+// The splits of the group in this lane, of those the call has for all groups
+// together: one each, and the rest by length, so that a workgroup's share of the
+// keys hardly depends on its group.  For the whole wavefront; G <= kDealt.
+__device__ __forceinline__ int dealt_splits(const Cut &cut, int G, int64_t length) {
+    unsigned units = unsigned(length + 63) / 64;
+    unsigned total = units;
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2) total += __shfl_xor(total, d);
+    const int lane = threadIdx.x % kWave, spare = G * (cut.splits - 1);
+    const int coarse = max(0, 14 - int(__builtin_clz(total | 1)));   // so that the product fits 32 bits
+    const int share = total > 0 ? int(unsigned(spare) * (units >> coarse) / (total >> coarse)) : cut.splits - 1;
+    return lane < G ? min(1 + share, cut.parts) : 0;
+}
+
 struct AttendPlan {
     Cut prefix, own;
-    int parts;           // splits of both: partial results a row
+    int parts;           // of both: most partial results a row
     float *sums;         // [parts, rows, dim] sums of weight times v around the part's maximum
     float2 *stats;       // [parts, rows] {maximum in log2, sum of weights}
 };
@@ -256,14 +275,28 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     w /= unsigned(cut.blocks);
     const int h = int(w % unsigned(H));
     w /= unsigned(H);
-    const int split = int(w % unsigned(cut.splits)), g = int(w / unsigned(cut.splits));
+    int split = int(w % unsigned(cut.splits)), splits = cut.splits, g = int(w / unsigned(cut.splits));
+    if (!own && plan.prefix.parts > splits) {
+        const int n = dealt_splits(cut, int(a.G), lane < a.G ? prefix_table(p, lane).count : 0);
+        int end = n;   // of the splits of the groups up to this lane's
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int below = __shfl_up(end, d);   // (of all lanes: a lane that does not take part gives nothing)
+            end += lane >= d ? below : 0;
+        }
+        const int before = __builtin_popcountll(__ballot(lane < a.G && end <= int(w)));
+        if (before >= a.G) return;   // one that rounding left over
+        g = before;
+        splits = __builtin_amdgcn_readlane(n, before);
+        split = int(w) - (__builtin_amdgcn_readlane(end, before) - splits);
+    }
     const int beam = own ? 1 : int(a.S / a.G), s0 = g * beam;
     const unsigned rows = unsigned(beam) * T_ * rep;   // (all rows of a call are below 2^31)
     const PageTable table = own ? own_table(p, s0) : prefix_table(p, g);
     const int count = int(table.count);
 
     // this split's keys
-    const int tiles = (count + A::kKeys - 1) / A::kKeys, per = (tiles + cut.splits - 1) / cut.splits;
+    const int tiles = (count + A::kKeys - 1) / A::kKeys, per = (tiles + splits - 1) / splits;
     const int tile0 = min(tiles, split * per), tile1 = min(tiles, tile0 + per);
 
     // A lane's key of a tile: its row of the cache in 16-byte units.
@@ -546,7 +579,7 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
 #pragma unroll
     for (int r = 0; r < RT; ++r) total[r] = row_sum(sum[r]);
     const int64_t all_rows = a.S * a.T * a.q_heads;
-    const int part = (own ? plan.prefix.splits : 0) + split;
+    const int part = (own ? plan.prefix.parts : 0) + split;
     if (one_by_one) {
         for (unsigned i = 0; i < 16 * RT; ++i) {
             const unsigned row = unsigned(block) * A::kRows + unsigned(wave) * 16 * RT + i;
