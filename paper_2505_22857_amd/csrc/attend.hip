@@ -203,7 +203,7 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     // 4 / 5; heads of 64: 67 / 51 / 49 / 52; of 256 (2 fit): 48, 62 with 3.
     const int64_t per_cu = r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2);
     if (a.pages)
-        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, kCus, r.own_tiles, r.own_waves);
+        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, 4 * kCus, r.own_tiles, r.own_waves);
     if (a.G > 0) {
         const int64_t left = per_cu * kCus - r.plan.own.works();
         r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size,
@@ -216,6 +216,7 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
         r.plan.prefix.parts = int(std::min<int64_t>(2 * r.plan.prefix.splits, 1 + a.G * (r.plan.prefix.splits - 1)));
     r.plan.parts = r.plan.prefix.parts + r.plan.own.splits;
     const int64_t rows = a.S * a.T * a.q_heads;
+    r.plan.page_magic = c.page_size == 1 ? UINT32_MAX : unsigned((uint64_t(1) << 32) / unsigned(c.page_size));
     r.plan.sums = reinterpret_cast<float *>(workspace);
     r.plan.stats = reinterpret_cast<float2 *>(workspace + size_t(r.plan.parts) * size_t(rows) * c.dim * 4);
     return r;
