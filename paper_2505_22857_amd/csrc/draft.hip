@@ -31,10 +31,11 @@ struct Draft {
     float to_log2;   // log2 e / temperature
     int32_t *tokens, *draft_states;
     float *logprobs;
-    bool streams;   // the rows go past the caches
+    bool streams;
 };
 
-template <int W, int NT, bool FULL, bool SAMPLE>
+// STREAM: the rows go past the caches.
+template <int W, int NT, bool FULL, bool SAMPLE, bool STREAM>
 __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
     extern __shared__ i32x4 lds4[];
     const DevTrie &t = d.t;
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
         for (int i = 0; i < NT; ++i) {
             if (FULL || kWave * i + lane < g.own) {
                 const float y = ((x[i] - m) * d.to_log2 - log_total) * kLn2;
-                if (d.streams)
+                if (STREAM)
                     __builtin_nontemporal_store(y, &row[kWave * i + lane]);
                 else
                     row[kWave * i + lane] = y;
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
     if (SAMPLE) write_row(K - 1);
 }
 
-template <int W, int NT, bool FULL, bool SAMPLE>
+template <int W, int NT, bool FULL, bool SAMPLE, bool STREAM>
 static hipError_t launch_group(Draft d, int64_t B, hipStream_t stream) {
     // a grid holds at most 2^32 - 1 work-items: larger batches go in several launches
     constexpr int64_t kMost = int64_t(UINT32_MAX) / (W * kWave);
@@ -214,18 +215,22 @@ static hipError_t launch_group(Draft d, int64_t B, hipStream_t stream) {
         p.tokens += b0 * d.K;
         p.draft_states += b0 * (d.K + 1);
         if (p.logprobs) p.logprobs += b0 * d.K * d.t.vocab_size;
-        hipLaunchKernelGGL((draft_kernel<W, NT, FULL, SAMPLE>), dim3(unsigned(B - b0 < kMost ? B - b0 : kMost)),
+        hipLaunchKernelGGL((draft_kernel<W, NT, FULL, SAMPLE, STREAM>), dim3(unsigned(B - b0 < kMost ? B - b0 : kMost)),
                            dim3(W * kWave), lds, stream, p);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
+template <int W, int NT, bool FULL>
+static hipError_t launch_group(const Draft &d, int64_t B, hipStream_t stream) {
+    if (!d.noise) return launch_group<W, NT, FULL, false, false>(d, B, stream);
+    return d.streams ? launch_group<W, NT, FULL, true, true>(d, B, stream)
+                     : launch_group<W, NT, FULL, true, false>(d, B, stream);
+}
 template <int W, int NT>
 static hipError_t launch_group(const Draft &d, int64_t B, hipStream_t stream) {
-    const bool full = d.t.vocab_size == W * kWave * NT;
-    if (d.noise)
-        return full ? launch_group<W, NT, true, true>(d, B, stream) : launch_group<W, NT, false, true>(d, B, stream);
-    return full ? launch_group<W, NT, true, false>(d, B, stream) : launch_group<W, NT, false, false>(d, B, stream);
+    return d.t.vocab_size == W * kWave * NT ? launch_group<W, NT, true>(d, B, stream)
+                                            : launch_group<W, NT, false>(d, B, stream);
 }
 
 hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *last, int64_t B, int K,
