@@ -322,3 +322,51 @@ def test_refusals():
         got = ng.attend(torch.zeros(shape, dtype=F16, device="cuda"), kc, vc)
         assert got.shape == shape
     assert math.isfinite(float(ng.attend(**ok).float().sum()))
+
+
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+@pytest.mark.parametrize("page", [2, 4, 8, 16, 24, 32, 48])
+@pytest.mark.parametrize("beam", [1, 40])
+def test_pages_and_tiles(D, page, beam):
+    """Pages that hold a part of a load, one load or many, with one wavefront a tile and with four."""
+    check(G=2, beam=beam, T=2, H=1, rep=2, D=D, page=page, prefix=(333, 96), own=(40, 2, 7, 33), seed=page, dtype=F16)
+
+
+def test_more_tiles_than_lanes():
+    """More groups than a wavefront's lanes, each prefix in one piece of more than 64 tiles."""
+    prefix = np.random.default_rng(0).integers(0, 2600, 100)
+    prefix[:3] = 2600, 2049, 2048
+    check(G=100, beam=1, T=1, H=8, rep=1, D=16, page=64, prefix=prefix, own=(1, 2), seed=1)
+
+
+@pytest.mark.parametrize("G,beam", [(2, 2), (5, 3), (5, 40), (64, 1), (65, 1)])
+def test_ragged_prefixes(G, beam):
+    """Prefixes of very different lengths, empty ones among them: the splits follow the lengths."""
+    prefix = np.resize([3000, 0, 1, 64, 1500, 65], G)
+    check(G=G, beam=beam, T=1, H=2, rep=2, D=32, page=32, prefix=prefix, own=(3, 40, 1), seed=G)
+    check(G=G, beam=beam, T=1, H=2, rep=2, D=32, page=32, prefix=np.zeros(G, int) if G > 2 else (700, 0),
+          own=(3, 40, 1), seed=G)
+
+
+@pytest.mark.parametrize("T", [20, 80])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_late_values_in_long_drafts(T, bad):
+    """The same as for short ones where several wavefronts, or blocks of rows, share the own tokens."""
+    def spoil(q, kc, vc, pages, prefix_pages):
+        vc, kc = vc.clone(), kc.clone()
+        at = int(pages[0][(own[0] - 2) // 16]), (own[0] - 2) % 16
+        vc[at][0, 5:9] = bad
+        kc[at][1, 3] = bad
+        return q, kc, vc, pages, prefix_pages
+    own = np.array([T + 70, T])
+    out = check(G=1, beam=2, T=T, rep=3, prefix=(40,), own=own, page=16, D=128, change=spoil)
+    assert torch.isfinite(out[0, :T - 2]).all() and torch.isfinite(out[1]).all()
+    assert not torch.isfinite(out[0, T - 2:, :3, 5:9]).any()
+    if bad != bad:          # (an infinite key's score is -inf, a weight of zero, where the query's value is negative)
+        assert not torch.isfinite(out[0, T - 2:, 3:]).any()
+
+
+def test_one_part_is_written_directly():
+    """A single piece of own tokens and no prefix: no join; with rows that do not count."""
+    check(G=0, beam=5, T=4, own=(10, 4, 0, 63, 2), q_lengths=np.array([4, 0, 2, 3, 4]), page=64, D=128)
+    check(G=0, beam=2, T=40, rep=4, H=1, own=(40, 60), page=64, D=256, q_lengths=np.array([40, 11]))

@@ -178,3 +178,8 @@ def test_refusals():
             lm.draft(states, 2, noise=noise, temperature=t)
     tok, after, rows = lm.draft(states[:0], 2, noise=noise[:0])
     assert tok.shape == (0, 2) and after.shape == (0, 3) and rows.shape == (0, 2, 40)
+
+
+def test_rows_past_the_caches():
+    """So many rows that they are written past the caches."""
+    check(*model(2048), 700, 6, 1.0, True)
