@@ -202,14 +202,20 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     // of 100000 tokens for 5 x 4 rows, 8 heads of 128, us: 238 / 205 / 214 / 273 with 2 / 3 /
     // 4 / 5; heads of 64: 67 / 51 / 49 / 52; of 256 (2 fit): 48, 62 with 3.
     const int64_t per_cu = r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2);
-    if (a.pages)
-        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size, 4 * kCus, r.own_tiles, r.own_waves);
+    const int64_t prefix_rows = a.G > 0 ? a.S / a.G * a.T * rep : 0;
+    if (a.pages) {
+        // Beside prefixes of several wavefronts they wait for memory while those compute, and fewer parts are
+        // joined: 2 for a CU, not 4.  64 sequences of 300 tokens, 8 heads of 128, 2048 of prefix: 60 us, not 68.
+        cut_rows(prefix_rows, r.steps, r.prefix_tiles, r.prefix_waves, r.plan.prefix.blocks);
+        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size,
+                         (r.prefix_waves > 1 ? 2 : 4) * kCus, r.own_tiles, r.own_waves);
+    }
     if (a.G > 0) {
         const int64_t left = per_cu * kCus - r.plan.own.works();
-        r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size,
+        r.plan.prefix = cut(a.G * c.heads, prefix_rows, a.prefix_width * c.page_size,
                             std::max<int64_t>(left, 2 * kCus), r.prefix_tiles, r.prefix_waves);
         if (r.prefix_waves == 4)
-            r.plan.prefix = cut(a.G * c.heads, a.S / a.G * a.T * rep, a.prefix_width * c.page_size, 2 * kCus,
+            r.plan.prefix = cut(a.G * c.heads, prefix_rows, a.prefix_width * c.page_size, 2 * kCus,
                                 r.prefix_tiles, r.prefix_waves);
     }
     if (a.G > 1 && a.G <= kDealt && r.plan.prefix.splits > 1)   // a group may take more than its share
@@ -246,6 +252,35 @@ hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int tiles, int w
     if (waves == 2) return launch_tile<T, DK, kMost, 2>(p, plan, w0, w1, stream);
     return launch_tile<T, DK, kMost, 4>(p, plan, w0, w1, stream);
 }
+template <class T, int DK, int WR>
+hipError_t launch_both(const Attend &p, const AttendPlan &plan, hipStream_t stream) {
+    constexpr int RT = DK <= 4 ? 2 : 1;
+    using A = AttendTile<T, DK, RT, WR>;
+    constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
+    static const hipError_t ready = hipFuncSetAttribute(
+        reinterpret_cast<const void *>(&attend_both_kernel<T, DK, RT, WR>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, A::kLds);
+    if (ready != hipSuccess) return ready;
+    constexpr int kWaves = kOwnWaves<T, DK, RT, WR>;
+    const int64_t own = (plan.own.works() + kWaves - 1) / kWaves, all = own + plan.prefix.works();
+    for (int64_t b0 = 0; b0 < all; b0 += kMost) {
+        hipLaunchKernelGGL((attend_both_kernel<T, DK, RT, WR>), dim3(unsigned(std::min(kMost, all - b0))),
+                           dim3(64 * WR), A::kLds, stream, p, plan, unsigned(b0), unsigned(own));
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <class T>
+hipError_t launch_both(const Attend &p, const Choice &r, hipStream_t stream) {
+    const bool four = r.prefix_waves == 4;
+    switch (r.steps) {
+        case 2: return four ? launch_both<T, 2, 4>(p, r.plan, stream) : launch_both<T, 2, 2>(p, r.plan, stream);
+        case 3: return four ? launch_both<T, 3, 4>(p, r.plan, stream) : launch_both<T, 3, 2>(p, r.plan, stream);
+        case 4: return four ? launch_both<T, 4, 4>(p, r.plan, stream) : launch_both<T, 4, 2>(p, r.plan, stream);
+        default: return four ? launch_both<T, 8, 4>(p, r.plan, stream) : launch_both<T, 8, 2>(p, r.plan, stream);
+    }
+}
+
 template <class T>
 hipError_t launch_tile(const Attend &p, const Choice &r, int tiles, int waves, int64_t w0, int64_t w1,
                        hipStream_t stream) {
@@ -281,11 +316,14 @@ hipError_t launch(const Attend &p, void *workspace, hipStream_t stream) {
     const Choice r = choose(p.c, a, static_cast<char *>(workspace));
     if (!r.tiles) return launch_rows<T>(p, stream);
     const int64_t prefix = r.plan.prefix.works(), all = prefix + r.plan.own.works();
-    if (prefix > 0 && all > prefix && r.prefix_waves == 1 && r.own_waves == 1) {   // both in one launch
-        if (const hipError_t e = launch_tile<T>(p, r, std::max(r.prefix_tiles, r.own_tiles), 1, 0, all, stream);
-            e != hipSuccess)
-            return e;
-        return join<T>(p, r, stream);
+    // Both in one launch.  4 x 16 sequences of 6 tokens with 6000 of prefix and 230 of their own, 8 heads of 128:
+    // 79 to 84 us, not 88; 2 x 8 of 4 tokens, 4096 and 100: 37, not 40.
+    if (prefix > 0 && all > prefix && (r.prefix_waves == r.own_waves || r.own_waves == 1)) {
+        const hipError_t e =
+            r.prefix_waves == r.own_waves
+                ? launch_tile<T>(p, r, std::max(r.prefix_tiles, r.own_tiles), r.own_waves, 0, all, stream)
+                : launch_both<T>(p, r, stream);
+        return e != hipSuccess ? e : join<T>(p, r, stream);
     }
     if (prefix > 0)
         if (const hipError_t e = launch_tile<T>(p, r, r.prefix_tiles, r.prefix_waves, 0, prefix, stream);

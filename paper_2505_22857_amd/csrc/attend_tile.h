@@ -252,20 +252,17 @@ struct AttendTile {
     }
 };
 
-// Registers are held to what two workgroups of four wavefronts a CU leave each where that spills nothing.
+// Work `w` of the plan, for WR wavefronts with LDS from `lds0` on.
 template <class T, int DK, int RT, int WR>
-__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
-                                                                                   unsigned work0) {
+__device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &plan, unsigned w, unsigned lds0) {
     using A = AttendTile<T, DK, RT, WR>;
     using M = Matrix<T>;
-    extern __shared__ __attribute__((aligned(512))) char lds[];   // (a row's pieces are found by exclusive or)
     unsigned (*masks)[A::kChunks] = nullptr;   // per stage, a bit for each key that exists
     if constexpr (WR > 1) {
         __shared__ unsigned shared_masks[A::kStages][A::kChunks];
         masks = shared_masks;
     }
-    const unsigned lds0 = unsigned(reinterpret_cast<uintptr_t>((LdsPtr<char>)lds));
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x % kWave, wave = WR == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane % 16, quad = lane / 16;
     const ngpu_attend_t &a = p.a;
     const int H = p.c.heads, rep = a.q_heads / H, D = p.c.dim, T_ = int(a.T);
@@ -273,7 +270,6 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
     // Workgroups go to the 8 XCDs in turn.  Each XCD takes a run of the prefixes'
     // works, which share keys (row blocks) or rows of pages (heads) in its L2.
     const unsigned prefix_works = unsigned(plan.prefix.works());
-    unsigned w = work0 + blockIdx.x;
     const bool own = w >= prefix_works;
     const Cut &cut = own ? plan.own : plan.prefix;
     if (own)
@@ -723,6 +719,39 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
             }
         }
     }
+}
+
+// The first byte of the launch's LDS (a row's pieces are found by exclusive or).
+__device__ __forceinline__ unsigned tile_lds() {
+    extern __shared__ __attribute__((aligned(512))) char lds[];
+    return unsigned(reinterpret_cast<uintptr_t>((LdsPtr<char>)lds));
+}
+
+// Registers are held to what two workgroups of four wavefronts a CU leave each where that spills nothing.
+template <class T, int DK, int RT, int WR>
+__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
+                                                                              unsigned work0) {
+    attend_tiles<T, DK, RT, WR>(p, plan, work0 + blockIdx.x, tile_lds());
+}
+
+// Prefixes whose rows take WR wavefronts, and own tokens whose rows take one, in
+// one launch: the second wait for memory while the first compute.  A workgroup
+// is either WR wavefronts at one work of a prefix or, first, as many as have
+// room in the same LDS at a work of own tokens each.
+template <class T, int DK, int RT, int WR>
+constexpr int kOwnWaves = AttendTile<T, DK, RT, WR>::kLds / AttendTile<T, DK, RT, 1>::kLds;
+template <class T, int DK, int RT, int WR>
+__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_both_kernel(Attend p, AttendPlan plan,
+                                                                              unsigned block0, unsigned own_blocks) {
+    constexpr int kWaves = kOwnWaves<T, DK, RT, WR>;
+    const unsigned lds0 = tile_lds(), block = block0 + blockIdx.x;
+    if (block >= own_blocks) {
+        attend_tiles<T, DK, RT, WR>(p, plan, block - own_blocks, lds0);
+        return;
+    }
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), w = block * kWaves + wave;
+    if (wave < kWaves && w < unsigned(plan.own.works()))
+        attend_tiles<T, DK, RT, 1>(p, plan, unsigned(plan.prefix.works()) + w, lds0 + wave * AttendTile<T, DK, RT, 1>::kLds);
 }
 
 }  // namespace ngpu
