@@ -183,3 +183,11 @@ def test_refusals():
 def test_rows_past_the_caches():
     """So many rows that they are written past the caches."""
     check(*model(2048), 700, 6, 1.0, True)
+
+
+@pytest.mark.parametrize("V", [1100, 2048])
+@pytest.mark.parametrize("B", [512, 513])
+def test_many_sequences(V, B):
+    """Both sides of the batch from which fewer wavefronts take a sequence."""
+    check(*model(V), B, 2, 1.0, True)
+    check(*model(V), B, 2, 0.0, False)
