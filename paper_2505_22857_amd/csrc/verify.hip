@@ -7,7 +7,7 @@
 //
 // So every row needs its maximum and sum of exponentials (or its argmax, for
 // greedy decoding), and row a once more, with the draft's row and the noise: the
-// bound is reading the logits.  A vocabulary of up to kWhole tokens is verified
+// bound is reading the logits.  A small vocabulary is verified
 // in one launch, a workgroup a sequence; a larger one in two, the first over
 // chunks of all rows and the second over parts of row a, whose last workgroup
 // joins them.  Sums are in fp32 and joined in a fixed order.
@@ -21,14 +21,13 @@
 
 namespace ngpu {
 
-constexpr int64_t kWhole = 8192;
+constexpr int64_t kWhole = 8192;      // most tokens of a row that one workgroup takes whole
 constexpr int kWholeThreads = 1024;
 constexpr int kSegment = 1024;        // of a row, what a wavefront of the one launch takes at a time
 constexpr int kStatThreads = 256;
-constexpr int kChunk = 8192;          // logits a workgroup of the first launch takes, at least
+constexpr int kChunk = 8192;          // logits of a row, tokens of a race that a workgroup of the two launches takes
 constexpr int kMostChunks = 64;
 constexpr int kRaceThreads = 256;
-constexpr int kRacePart = 8192;       // tokens a workgroup of the second launch takes, at least
 constexpr int kMostParts = 64;
 
 struct Verify {
@@ -381,9 +380,19 @@ static Verify plan(const ngpu_verify_t &a, char *workspace, size_t *bytes) {
     v.a = a;
     v.to_log2 = a.temperature > 0.0f ? 1.44269504088896f / a.temperature : 0.0f;
     *bytes = 0;
-    if (a.V <= kWhole) return v;
-    split_row(a.V, kChunk, kMostChunks, v.chunks, v.chunk);
-    split_row(a.V, kRacePart, kMostParts, v.parts, v.part);
+    // One launch takes 8.5 / 9.4 / 19 us for 1 / 64 / 512 sequences of 5 rows of 4096 (fp32, 5 or 6 rows), two with
+    // the chunks below 8.7 / 10.2 / 20; of 8192 10.6 / 12.6 / 26.8, two 8.8 / 12.3 / 30.2; of 16384 one 18.7 / 22 / 47,
+    // two 9.5 / 14.4 / 51.
+    if (a.V <= kWhole / 2 || (a.V <= kWhole && a.B >= 64)) return v;
+    // Smaller chunks while they fill the chip at most twice: 9.7 us, not 13.2, for one sequence of 5 rows of
+    // 32768, 14.4, not 16.3, for 64 of 6 of 16384.  More of them only repeat what each does first: 96 sequences of 128001
+    // 81 us with halves for the second launch, not 74.
+    auto least = [&](int64_t rows) {
+        const int64_t full = rows * ((a.V + kChunk - 1) / kChunk);
+        return full <= 512 ? kChunk / 4 : (full < 1024 ? kChunk / 2 : kChunk);
+    };
+    split_row(a.V, least(a.B * (a.K + 1)), kMostChunks, v.chunks, v.chunk);
+    split_row(a.V, least(a.B), kMostParts, v.parts, v.part);
     const size_t stats = size_t(a.B) * size_t(a.K + 1) * size_t(v.chunks) * sizeof(i32x2);
     const size_t best = size_t(a.B) * sizeof(uint64_t);
     if (a.temperature == 0.0f) v.parts = 1, v.part = a.V;   // nothing is drawn
@@ -404,7 +413,7 @@ size_t verify_workspace(int64_t B, int K, int64_t V) {
 
 template <class T, bool GREEDY>
 static hipError_t launch(const Verify &v, hipStream_t stream) {
-    if (v.a.V <= kWhole) {
+    if (v.chunks == 0) {
         hipLaunchKernelGGL((verify_whole_kernel<T, GREEDY>), dim3(unsigned(v.a.B)), dim3(kWholeThreads), 0, stream, v);
         return hipGetLastError();
     }

@@ -248,3 +248,11 @@ def test_refusals():
                   temperature=0.0)
     out, kept, states = ng.verify(args[0][:0], args[1][:0], temperature=0.0)
     assert out.shape == (0, 3) and kept.shape == (0,) and states is None
+
+
+@pytest.mark.parametrize("B,K,V", [
+    (63, 1, 4097), (64, 1, 4097), (63, 2, 8192), (64, 2, 8192), (60, 5, 10001), (90, 5, 10001), (256, 3, 9000)])
+@pytest.mark.parametrize("temperature", [0.0, 1.3])
+def test_either_side_of_the_cuts(B, K, V, temperature):
+    """Batches for one launch and two, and for each size of the second's chunks."""
+    check(inputs(B, K, V, F32, B + V), temperature)
