@@ -5,6 +5,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -15,11 +17,12 @@ SOURCES = ["api.cpp", "trie_build.cpp", "arpa.cpp", "advance.hip", "fused_step.h
            "draft.hip", "serving.cpp", "verify.hip", "kv_append.hip", "attend.hip"]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off",                      # no contraction beyond the explicit fmaf
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
+LINK_FLAGS = ["--offload-arch=gfx950", "-shared", "-fPIC"]
 
 
 def hipcc() -> str:
@@ -29,12 +32,17 @@ def hipcc() -> str:
 
 
 def build(out: str = LIB_PATH, extra=(), verbose: bool = False) -> str:
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", out + ".tmp", *srcs]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory(dir=os.path.dirname(out)) as tmp:   # an object per source, four at a time
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(4) as pool:
+            list(pool.map(lambda s, o: run([hipcc(), *HIPCC_FLAGS, *extra, "-I", os.path.join(ROOT, "include"),
+                                            "-I", CSRC, "-c", os.path.join(CSRC, s), "-o", o]), SOURCES, objects))
+        run([hipcc(), *LINK_FLAGS, *extra, "-o", out + ".tmp", *objects])
     os.replace(out + ".tmp", out)
     return out
 

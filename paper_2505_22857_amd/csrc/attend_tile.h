@@ -11,7 +11,7 @@
 // run over a lane's own registers and four lanes, and the weights are already
 // laid out as the second operand of O^T += V^T P^T: lane l holds the keys 16 u + 4
 // (l / 16) + i, and the transposing LDS load fetches V's 4 x 16 blocks in that
-// order.  K and V go from memory straight to LDS, double-buffered; 16-byte
+// order.  K and V go from memory straight to LDS, two tiles in turn; 16-byte
 // chunks of a row are stored at their place XOR the row, which leaves neither
 // load a bank conflict.
 //
@@ -20,6 +20,14 @@
 // same): otherwise the accumulators need no rescaling.  Scores, sums and
 // accumulators are fp32; the weights are rounded to the cache's type, which the
 // matrix instructions need, before they multiply V.
+//
+// What bounds it depends on the rows.  Few: reading the cache, once (3 prefixes of
+// 100000 tokens for 5 x 4 rows, 8 heads of 128, bf16: 198 us, 1.24 GB at 6.2 TB/s,
+// 0.9 of a fill's rate).  Many: the matrix instructions, the exponentials between
+// them and LDS's reads, which take about as long as the first, share a SIMD's two
+// wavefronts (4 x 384 rows: 7.4 us per 1024 tokens of prefix, 870 TFLOP/s, behind 24 us
+// for launches, first loads, partial sums and their join; 32768 tokens ran at 630 to 710 in
+// all).  Short ones: the chain of page table, first tile and join.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -221,11 +229,12 @@ __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, u
         asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
 }
 
-// DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR:
-// wavefronts, each with rows of its own, that share the tiles of keys.
 // Steps that operands are loaded from LDS before the matrix instructions that take them.
 constexpr int kKeysAhead = 2, kValuesAhead = 3;
 
+// DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR:
+// wavefronts, each with rows of its own, that share the tiles of keys.  Two stages: three and four,
+// or tiles of 32 keys for four wavefronts, measured the same within 2 % where they fit.
 template <class T, int DK, int RT, int WR>
 struct AttendTile {
     static constexpr int kChunks = WR > 2 ? 2 : 1;              // of 32 keys, a tile
@@ -239,7 +248,7 @@ struct AttendTile {
     static constexpr int kLds = kStages * kStage;
     static constexpr int kPerLoad = kWave / kPieces;            // rows a load instruction brings
     static constexpr int kLoads = kLoad / kPerLoad;
-    static constexpr bool kOnce = WR == 1;                      // no other workgroup reads these keys
+    static constexpr bool kOnce = WR == 1;                      // one block of rows, mostly: keys are read once
     static constexpr int kTiles = 2 * DK;                       // of 16 dimensions
     static constexpr int kIssued = 2 * kLoads;                  // load instructions of a wavefront and tile
     static_assert(kKeysAhead <= DK && kValuesAhead <= kTiles, "the first steps lie in the first chunk");

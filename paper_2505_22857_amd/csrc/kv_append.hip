@@ -5,7 +5,8 @@
 // its token's position: (a cos - b sin, b cos + a sin), in fp32, rounded once to
 // the cache's type; the other dimensions and the values are copied.  Every
 // element is read and written once, so the bound is memory traffic, and for a
-// few tokens the launch.
+// few tokens the launch: one token of 8 heads of 64 5.3 us, 4 x 4001 of 32 + 8 + 8
+// heads of 128 66 to 72 us, 298 MB at 4.2 to 4.5 TB/s where a large copy reaches 5.0.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,7 +32,7 @@ __device__ __forceinline__ int64_t page_of(const Append &p, int64_t s, int64_t p
 }
 
 // Any dimension, stride and alignment: one workgroup per token; each thread writes
-// one element at a time.
+// one element at a time (4 x 4001 tokens as above: 205 us, 16 bytes at a time 68).
 template <class T>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(Append p, int64_t n0) {
     const ngpu_kv_append_t &a = p.a;
