@@ -234,7 +234,7 @@ constexpr int kKeysAhead = 2, kValuesAhead = 3;
 
 // DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR:
 // wavefronts, each with rows of its own, that share the tiles of keys.  Two stages: three and four,
-// or tiles of 32 keys for four wavefronts, measured the same within 2 % where they fit.
+// or tiles of 32 keys for four wavefronts, were no faster.
 template <class T, int DK, int RT, int WR>
 struct AttendTile {
     static constexpr int kChunks = WR > 2 ? 2 : 1;              // of 32 keys, a tile
