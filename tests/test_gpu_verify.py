@@ -254,5 +254,5 @@ def test_refusals():
     (63, 1, 4097), (64, 1, 4097), (63, 2, 8192), (64, 2, 8192), (60, 5, 10001), (90, 5, 10001), (256, 3, 9000)])
 @pytest.mark.parametrize("temperature", [0.0, 1.3])
 def test_either_side_of_the_cuts(B, K, V, temperature):
-    """Batches for one launch and two, and for each size of the second's chunks."""
+    """Batches on both sides of one launch and two, and of each size of chunk."""
     check(inputs(B, K, V, F32, B + V), temperature)
