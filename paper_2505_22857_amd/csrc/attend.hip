@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "attend_tile.h"
 
@@ -167,7 +168,7 @@ struct Choice {
 };
 
 // The matrix kernel loads 16 bytes of 8 elements at a time and keeps a row of
-// the cache as a 32-bit number of them.
+// the cache as a 32-bit number of them, and of a query as one of rows.
 bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
     const int64_t strides[] = {c.k_stride_page, c.k_stride_token, c.k_stride_head,
                                c.v_stride_page, c.v_stride_token, c.v_stride_head};
@@ -178,7 +179,7 @@ bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
     return c.dim % 8 == 0 && reinterpret_cast<uintptr_t>(c.k) % 16 == 0 && reinterpret_cast<uintptr_t>(c.v) % 16 == 0 &&
            reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && c.k_stride_page / 8 <= kMost / pages &&
            c.v_stride_page / 8 <= kMost / pages && c.k_stride_token / 8 <= kMost / c.page_size &&
-           c.v_stride_token / 8 <= kMost / c.page_size && a.S * a.T * a.q_heads < kMost / 256;
+           c.v_stride_token / 8 <= kMost / c.page_size && a.S * a.T * a.q_heads < kMost / 2;
 }
 
 // Rows of a problem to wavefronts.  4 prefixes of 8192 tokens, 8 heads of 128, us: 48 / 64 / 96 / 128 / 384 rows 35 / 38 /
@@ -236,14 +237,25 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     return r;
 }
 
+// More LDS than a launch has by default, asked for once a device (bits of `devices`).
+template <class K>
+hipError_t allow_lds(K *kernel, int bytes, std::atomic<uint64_t> &devices) {
+    int device;
+    if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+    const uint64_t bit = uint64_t(1) << device % 64;
+    if (device < 64 && (devices.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && device < 64) devices.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 template <class T, int DK, int RT, int WR>
 hipError_t launch_tile(const Attend &p, const AttendPlan &plan, int64_t w0, int64_t w1, hipStream_t stream) {
     using A = AttendTile<T, DK, RT, WR>;
     constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
-    static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void *>(&attend_tile_kernel<T, DK, RT, WR>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, A::kLds);
-    if (ready != hipSuccess) return ready;
+    static std::atomic<uint64_t> devices;
+    if (const hipError_t e = allow_lds(&attend_tile_kernel<T, DK, RT, WR>, A::kLds, devices); e != hipSuccess) return e;
     for (; w0 < w1; w0 += kMost) {
         hipLaunchKernelGGL((attend_tile_kernel<T, DK, RT, WR>), dim3(unsigned(std::min(kMost, w1 - w0))),
                            dim3(64 * WR), A::kLds, stream, p, plan, unsigned(w0));
@@ -265,10 +277,8 @@ hipError_t launch_both(const Attend &p, const AttendPlan &plan, hipStream_t stre
     constexpr int RT = DK <= 4 ? 2 : 1;
     using A = AttendTile<T, DK, RT, WR>;
     constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
-    static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void *>(&attend_both_kernel<T, DK, RT, WR>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, A::kLds);
-    if (ready != hipSuccess) return ready;
+    static std::atomic<uint64_t> devices;
+    if (const hipError_t e = allow_lds(&attend_both_kernel<T, DK, RT, WR>, A::kLds, devices); e != hipSuccess) return e;
     constexpr int kWaves = kOwnWaves<T, DK, RT, WR>;
     const int64_t own = (plan.own.works() + kWaves - 1) / kWaves, all = own + plan.prefix.works();
     for (int64_t b0 = 0; b0 < all; b0 += kMost) {

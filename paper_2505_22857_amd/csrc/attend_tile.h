@@ -248,7 +248,7 @@ struct AttendTile {
     static constexpr int kLds = kStages * kStage;
     static constexpr int kPerLoad = kWave / kPieces;            // rows a load instruction brings
     static constexpr int kLoads = kLoad / kPerLoad;
-    static constexpr bool kOnce = WR == 1;                      // one block of rows, mostly: keys are read once
+    static constexpr bool kOnce = WR == 1;                      // its problem's only block of rows: keys are read once
     static constexpr int kTiles = 2 * DK;                       // of 16 dimensions
     static constexpr int kIssued = 2 * kLoads;                  // load instructions of a wavefront and tile
     static_assert(kKeysAhead <= DK && kValuesAhead <= kTiles, "the first steps lie in the first chunk");
@@ -310,7 +310,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     const int count = int(table.count);
 
     // this split's keys
-    const int tiles = (count + A::kKeys - 1) / A::kKeys, per = (tiles + splits - 1) / splits;
+    const int tiles = int((unsigned(count) + A::kKeys - 1) / A::kKeys), per = (tiles + splits - 1) / splits;
     const int tile0 = min(tiles, split * per), tile1 = min(tiles, tile0 + per);
 
     // The keys that this wavefront loads of each tile.  Where pages hold whole
@@ -318,7 +318,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     // else each lane finds its own key's, and the loads may go in page by page.
     const unsigned page_size = unsigned(p.c.page_size);
     const bool in_page = page_size % A::kLoad == 0;
-    auto first_key = [&](int tile) { return unsigned(tile * A::kKeys + wave * A::kLoad); };
+    auto first_key = [&](int tile) { return unsigned(tile) * A::kKeys + unsigned(wave * A::kLoad); };
     auto page_index = [&](unsigned j) {   // j / page_size
         unsigned i = __umulhi(j, plan.page_magic);
         return j - i * page_size >= page_size ? i + 1 : i;
@@ -554,7 +554,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                     x[r][2 * c + u] = M::mul(kx[i % (kKeysAhead + 1)][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        const bool some_rows = own && key0 + A::kKeys > least;   // some rows do not see some of the keys
+        const bool some_rows = own && key0 > least - A::kKeys;   // some rows do not see some of the keys
         bool all = !some_rows;
 #pragma unroll
         for (int c = 0; c < C; ++c) all = all && exists[c] == 0xffffffffu;
@@ -684,7 +684,8 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
             const int nq = int(query_length(a, s0)), sees = max(0, min(count, count - nq + t + 1));
             RowPart<T> r;
             r.load(p, s0, t, head, lane);
-            for (int j = tile0 * A::kKeys; j < min(tile1 * A::kKeys, sees); ++j) r.take(p, table, j, h, lane);
+            const unsigned end = min(unsigned(tile1) * A::kKeys, unsigned(sees));
+            for (unsigned j = unsigned(tile0) * A::kKeys; j < end; ++j) r.take(p, table, j, h, lane);
             const int64_t out = (int64_t(s0) * T_ + t) * a.q_heads + head;
             if (plan.parts > 1) {
                 if (lane == 0) plan.stats[part * all_rows + out] = make_float2(r.m, r.sum);

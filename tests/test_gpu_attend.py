@@ -370,3 +370,23 @@ def test_one_part_is_written_directly():
     """A single piece of own tokens and no prefix: no join; with rows that do not count."""
     check(G=0, beam=5, T=4, own=(10, 4, 0, 63, 2), q_lengths=np.array([4, 0, 2, 3, 4]), page=64, D=128)
     check(G=0, beam=2, T=40, rep=4, H=1, own=(40, 60), page=64, D=256, q_lengths=np.array([40, 11]))
+
+
+@pytest.mark.parametrize("D", [16, 17])
+def test_more_than_2_23_rows(D):
+    """Rows past 2^23, by both kernels: the first, the last and some between against the formula."""
+    T, rep, n = (1 << 20) + 3, 8, 5
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q = torch.randn(1, T, rep, D, generator=g, device="cuda").half()
+    kc, vc = (torch.randn(2, 4, 1, D, generator=g, device="cuda").half() for _ in range(2))
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    print(f"[case] attend {T} x {rep} rows D={D}", flush=True)
+    out = ng.attend(q, kc, vc, prefix_pages=ints([[1, 0]]), prefix_lengths=ints([n]))
+    at = torch.cat([torch.arange(1000), torch.arange(T // 2, T // 2 + 1000), torch.arange(T - 1000, T)])
+    keys, values = (x[[1, 0]].reshape(8, D)[:n].double().cpu() for x in (kc, vc))
+    x = (q[0, at.cuda()].double().cpu() @ keys.T) / D ** 0.5
+    w = torch.softmax(x, -1)
+    # the weights are rounded to half before the sum, and the result once
+    u = 2.0 ** -11
+    bound = 4 * u * (w @ values.abs()) + u * (w @ values).abs() + 2.0 ** -24
+    assert ((out[0, at.cuda()].double().cpu() - w @ values).abs() <= bound).all()
