@@ -213,11 +213,19 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     const int64_t per_cu = r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2);
     const int64_t prefix_rows = a.G > 0 ? a.S / a.G * a.T * rep : 0;
     if (a.pages) {
-        // Beside prefixes of several wavefronts they wait for memory while those compute, and fewer parts are
-        // joined: 2 for a CU, not 4.  64 sequences of 300 tokens, 8 heads of 128, 2048 of prefix: 60 us, not 68.
+        // Workgroups: 2 a CU, not 4, where several wavefronts share the keys (us: 4 sequences of 500 tokens that see 3500,
+        // 32 / 8 heads of 128 129, not 164; one of 64 that sees 8000 31, not 49), and beside prefixes whose rows
+        // take several, where own tokens wait for memory while those compute (64 sequences of one token that see 300, 2048
+        // of prefix 60, not 68).
         cut_rows(prefix_rows, r.steps, r.prefix_tiles, r.prefix_waves, r.plan.prefix.blocks);
-        r.plan.own = cut(a.S * c.heads, a.T * rep, a.pages_width * c.page_size,
-                         (r.prefix_waves > 1 ? 2 : 4) * kCus, r.own_tiles, r.own_waves);
+        cut_rows(a.T * rep, r.steps, r.own_tiles, r.own_waves, r.plan.own.blocks);
+        const int64_t keys = a.pages_width * c.page_size, have = a.S * c.heads * r.plan.own.blocks;
+        r.plan.own = cut(a.S * c.heads, a.T * rep, keys, (r.prefix_waves > 1 || r.own_waves == 4 ? 2 : 4) * kCus,
+                         r.own_tiles, r.own_waves);
+        // One workgroup a block of rows would have the last block's be twice as long as the mean: one sequence of
+        // 8192 tokens that see each other, 8 heads of 64: 280 us, in two splits 178.
+        if (r.own_waves == 4 && 2 * a.T > keys && have <= 2 * kCus) r.plan.own.splits = std::max(r.plan.own.splits, 2);
+        r.plan.own.parts = r.plan.own.splits;
     }
     if (a.G > 0) {
         const int64_t left = per_cu * kCus - r.plan.own.works();

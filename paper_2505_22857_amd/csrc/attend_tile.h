@@ -285,8 +285,11 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         w -= prefix_works;
     else
         w = w % 8 * (prefix_works / 8) + min(w % 8, prefix_works % 8) + w / 8;
-    const int block = int(w % unsigned(cut.blocks));
-    w /= unsigned(cut.blocks);
+    // Of own tokens the last blocks of rows see most keys: they come first, of all problems, a head to an XCD.  A
+    // prompt of 8192 tokens, 8 heads of 64: 178 us, 301 block by block; of 4 x 4001, 32 / 8 heads of 128: 1010, 1160.
+    const unsigned each = unsigned(cut.problems) * unsigned(cut.splits);
+    const int block = own ? cut.blocks - 1 - int(w / each) : int(w % unsigned(cut.blocks));
+    w = own ? w % each : w / unsigned(cut.blocks);
     const int h = int(w % unsigned(H));
     w /= unsigned(H);
     int split = int(w % unsigned(cut.splits)), splits = cut.splits, g = int(w / unsigned(cut.splits));
@@ -309,8 +312,13 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     const PageTable table = own ? own_table(p, s0) : prefix_table(p, g);
     const int count = int(table.count);
 
-    // this split's keys
-    const int tiles = int((unsigned(count) + A::kKeys - 1) / A::kKeys), per = (tiles + splits - 1) / splits;
+    // this split's keys, of those that the last row of the block sees (4 x 4001 tokens: 1160 us, 1900 with all keys)
+    int sees = count;
+    if (own) {
+        const unsigned last = min(rows, unsigned(block + 1) * A::kRows) - 1;
+        sees = min(count, max(0, count - int(query_length(a, s0)) + int(last / unsigned(rep)) + 1));
+    }
+    const int tiles = int((unsigned(sees) + A::kKeys - 1) / A::kKeys), per = (tiles + splits - 1) / splits;
     const int tile0 = min(tiles, split * per), tile1 = min(tiles, tile0 + per);
 
     // The keys that this wavefront loads of each tile.  Where pages hold whole
@@ -681,10 +689,10 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
             const unsigned row = unsigned(block) * A::kRows + unsigned(wave) * 16 * RT + i;
             if (row >= rows) break;
             const int t = int(row / unsigned(rep)), head = h * rep + int(row % unsigned(rep));   // (own: one sequence)
-            const int nq = int(query_length(a, s0)), sees = max(0, min(count, count - nq + t + 1));
+            const int nq = int(query_length(a, s0)), seen = max(0, min(count, count - nq + t + 1));
             RowPart<T> r;
             r.load(p, s0, t, head, lane);
-            const unsigned end = min(unsigned(tile1) * A::kKeys, unsigned(sees));
+            const unsigned end = min(unsigned(tile1) * A::kKeys, unsigned(seen));
             for (unsigned j = unsigned(tile0) * A::kKeys; j < end; ++j) r.take(p, table, j, h, lane);
             const int64_t out = (int64_t(s0) * T_ + t) * a.q_heads + head;
             if (plan.parts > 1) {

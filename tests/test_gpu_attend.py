@@ -390,3 +390,12 @@ def test_more_than_2_23_rows(D):
     u = 2.0 ** -11
     bound = 4 * u * (w @ values.abs()) + u * (w @ values).abs() + 2.0 ** -24
     assert ((out[0, at.cuda()].double().cpu() - w @ values).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("D,T,own", [(64, 300, (300, 411)), (128, 300, (300, 411)), (256, 90, (90, 3)), (40, 1000, (1000, 1063))])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_prompts(D, T, own, ragged):
+    """Many blocks of rows, each of which sees other keys; some tokens do not count, some see nothing."""
+    n = np.array([T, T // 2 + 1]) if ragged else None
+    check(G=0, beam=2, T=T, H=2, rep=4, D=D, page=16, own=own, q_lengths=n, seed=D)
+    check(G=1, beam=2, T=T, H=2, rep=4, D=D, page=16, prefix=(70,), own=own, q_lengths=n, seed=D + 1)
