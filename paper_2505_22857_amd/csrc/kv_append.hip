@@ -6,7 +6,7 @@
 // the cache's type; the other dimensions and the values are copied.  Every
 // element is read and written once, so the bound is memory traffic, and for a
 // few tokens the launch: one token of 8 heads of 64 5.3 us, 4 x 4001 of 32 + 8 + 8
-// heads of 128 66 to 72 us, 298 MB at 4.2 to 4.5 TB/s where a large copy reaches 5.0.
+// heads of 128 65 to 72 us, 298 MB at 4.2 to 4.6 TB/s where a large copy reaches 5.0.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -80,21 +80,24 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(Append p, int64_
     }
 }
 
-// Dimensions in eights and everything 16-byte aligned: one workgroup per token,
+// Dimensions in eights and everything 16-byte aligned: 2^bits threads per token,
 // 16 bytes at a time.  An item is 8 dimensions of a head, or with halves the 8
 // that it pairs with too.
 template <class T, bool HALVES>
-__global__ __launch_bounds__(kAppendThreads) void append_vector_kernel(Append p, int64_t n0) {
+__global__ __launch_bounds__(kAppendThreads) void append_vector_kernel(Append p, int64_t n0, int bits) {
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     const ngpu_kv_append_t &a = p.a;
-    const int64_t n = n0 + blockIdx.x, s = n / a.T, t = n % a.T;
+    const int64_t n = n0 + ((int64_t(blockIdx.x) * kAppendThreads + threadIdx.x) >> bits);
+    if (n >= a.S * a.T) return;
+    const unsigned threads = 1u << bits, thread = threadIdx.x & (threads - 1);
+    const int64_t s = n / a.T, t = n % a.T;
     const int H = p.c.heads, Hq = a.q ? a.q_heads : 0, half = a.rotary / 2;
     const unsigned pieces = unsigned(p.c.dim) / 8, turned = HALVES ? unsigned(half) / 8 : unsigned(a.rotary) / 8;
     const unsigned items = HALVES ? pieces - turned : pieces;   // of a rotated head
     const unsigned first_v = unsigned(Hq + H) * items, all = first_v + unsigned(H) * pieces;
     T *q_out = static_cast<T *>(a.q_out) + n * Hq * p.c.dim;
     if (a.lengths && t >= a.lengths[s]) {
-        for (unsigned e = threadIdx.x; e < unsigned(Hq) * pieces; e += kAppendThreads)
+        for (unsigned e = thread; e < unsigned(Hq) * pieces; e += threads)
             *reinterpret_cast<s16x8 *>(q_out + e * 8) = s16x8{};
         return;
     }
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_vector_kernel(Append p,
     auto angle = [&](const float *table, int i) {
         return known ? *reinterpret_cast<const f32x4 *>(table + i) : f32x4{} + __builtin_nanf("");
     };
-    for (unsigned e = threadIdx.x; e < all; e += kAppendThreads) {
+    for (unsigned e = thread; e < all; e += threads) {
         if (e >= first_v) {
             if (page < 0) break;
             const unsigned h = (e - first_v) / pieces, d = (e - first_v) % pieces * 8;
@@ -179,11 +182,29 @@ static hipError_t launch(const Append &p, hipStream_t stream) {
     // a grid holds at most 2^32 - 1 work-items
     constexpr int64_t kMost = int64_t(UINT32_MAX) / kAppendThreads;
     const int64_t n = p.a.S * p.a.T;
-    const auto kernel = !in_eights(p) ? &append_kernel<T>
-                                      : (p.a.layout == NGPU_ROPE_HALF ? &append_vector_kernel<T, true>
-                                                                      : &append_vector_kernel<T, false>);
-    for (int64_t n0 = 0; n0 < n; n0 += kMost) {
-        hipLaunchKernelGGL(kernel, dim3(unsigned(std::min(kMost, n - n0))), dim3(kAppendThreads), 0, stream, p, n0);
+    if (!in_eights(p)) {
+        for (int64_t n0 = 0; n0 < n; n0 += kMost) {
+            hipLaunchKernelGGL(append_kernel<T>, dim3(unsigned(std::min(kMost, n - n0))), dim3(kAppendThreads), 0, stream,
+                               p, n0);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    const bool halves = p.a.layout == NGPU_ROPE_HALF;
+    const int64_t pieces = p.c.dim / 8, items = halves ? pieces - p.a.rotary / 16 : pieces;
+    const int64_t all = ((p.a.q ? p.a.q_heads : 0) + p.c.heads) * items + p.c.heads * pieces;
+    // Threads a token: one for each item where these are few, else one for four, whose loads are in flight together.  us: 23 x
+    // 2554 tokens of 3 + 1 + 1 heads of 128 41, with an item a thread 66, with eight 37, with 256 threads a token
+    // 104; 16 x 2000 of 16 + 4 + 4 of 64 39, 67, 35, 74; 3 x 2710 of 4 + 2 + 2 of 96 8.5, 11.3, 9.6, 16.5; 600 of 8 + 1 + 1 of
+    // 64 3.7 with an item, 5.5 with four.
+    const int64_t passes = n * all >= int64_t(1) << 18 ? 4 : 1;
+    int bits = 4;
+    while (bits < 8 && (passes << bits) < all) ++bits;
+    const auto kernel = halves ? &append_vector_kernel<T, true> : &append_vector_kernel<T, false>;
+    const int64_t per = kAppendThreads >> bits;   // tokens a workgroup
+    for (int64_t n0 = 0; n0 < n; n0 += kMost * per) {
+        hipLaunchKernelGGL(kernel, dim3(unsigned(std::min(kMost, (n - n0 + per - 1) / per))), dim3(kAppendThreads), 0, stream,
+                           p, n0, bits);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -264,3 +264,13 @@ def test_refusals():
     wide = torch.zeros(16, 9, device="cuda")
     bad(ng.NgpuError, cos=wide, sin=wide)   # more dimensions than a head has
     assert ng.kv_append(**{**ok, "k": k[:, :0], "v": k[:, :0], "q": k[:, :0]}).shape == (2, 0, 2, 16)
+
+
+@pytest.mark.parametrize("layout", [HALF, INTER])
+@pytest.mark.parametrize("S,T,H,Hq,D,rotary,query", [(61, 151, 1, 3, 128, 32, True), (251, 149, 1, 1, 64, 64, False),
+                                                     (9, 97, 8, 32, 128, 64, True), (501, 33, 1, 1, 128, 128, True)])
+def test_many_tokens_of_few_heads(S, T, H, Hq, D, rotary, query, layout):
+    """Several tokens a workgroup and several pieces a thread, the last workgroup in part."""
+    lengths = np.random.default_rng(S).integers(0, T + 1, S)
+    check(S=S, T=T, H=H, Hq=Hq, D=D, rotary=rotary, layout=layout, query=query, page=32, rows=256, dtype=F16,
+          lengths=lengths, seed=S)
