@@ -208,25 +208,27 @@ __device__ __forceinline__ void wait_loads() {
 }
 // 16 bytes a lane from memory to LDS at `at` + 16 lane (uniform `at`).  As asm, since
 // the compiler would wait for it before any later LDS load.  (m0 is a reserved register, which
-// nothing else in these kernels uses: a clobber would only be warned about.)
+// nothing else in these kernels uses: a clobber would only be warned about.)  The load has to come a
+// wait state after the write of m0, and the compiler adds none inside the asm.
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void *p, unsigned at) {
     if (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(p) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(p) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
 }
 
-// The same from a uniform address and a lane's offset.
+// The same from a uniform address and a lane's offset.  Where the base was read from vector registers the load
+// has to come five wait states after that: the move and four of the s_nop.
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, unsigned at) {
     const uint64_t a = reinterpret_cast<uint64_t>(from);   // (the compiler may hold it in vector registers)
     const uint64_t base = uint64_t(unsigned(__builtin_amdgcn_readfirstlane(int(a >> 32)))) << 32 |
                           unsigned(__builtin_amdgcn_readfirstlane(int(a)));
     if (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(at), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(at), "v"(offset), "s"(base) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
 }
 
 // Steps that operands are loaded from LDS before the matrix instructions that take them.
