@@ -218,17 +218,35 @@ __device__ __forceinline__ void load_to_lds(const void *p, unsigned at) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
 }
 
-// The same from a uniform address and a lane's offset.  Where the base was read from vector registers the load
+// A uniform address in scalar registers (the compiler may hold it in vector ones).
+__device__ __forceinline__ uint64_t uniform_address(const void *p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return uint64_t(unsigned(__builtin_amdgcn_readfirstlane(int(a >> 32)))) << 32 |
+           unsigned(__builtin_amdgcn_readfirstlane(int(a)));
+}
+// The same from a uniform address and a lane's offset.  Where the address was read from vector registers the load
 // has to come five wait states after that: the move and four of the s_nop.
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, unsigned at) {
-    const uint64_t a = reinterpret_cast<uint64_t>(from);   // (the compiler may hold it in vector registers)
-    const uint64_t base = uint64_t(unsigned(__builtin_amdgcn_readfirstlane(int(a >> 32)))) << 32 |
-                          unsigned(__builtin_amdgcn_readfirstlane(int(a)));
+    const uint64_t base = uniform_address(from);
     if (ONCE)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(at), "v"(offset), "s"(base) : "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+}
+// Two of these, which share the wait: 3 prefixes of 100000 tokens as above 202 us, 210 one by one.
+template <bool ONCE>
+__device__ __forceinline__ void load_to_lds(const void *from0, unsigned offset0, unsigned at0, const void *from1,
+                                            unsigned offset1, unsigned at1) {
+    const uint64_t base0 = uniform_address(from0), base1 = uniform_address(from1);
+    if (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\t"
+                     "s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5 nt"
+                     ::"s"(at0), "v"(offset0), "s"(base0), "s"(at1), "v"(offset1), "s"(base1) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+                     "s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5"
+                     ::"s"(at0), "v"(offset0), "s"(base0), "s"(at1), "v"(offset1), "s"(base1) : "memory");
 }
 
 // Steps that operands are loaded from LDS before the matrix instructions that take them.
@@ -421,6 +439,16 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                     *reinterpret_cast<uint16_t *>(byte) = uint16_t(valid);
             }
         };
+        // the u-th rows of a whole tile, all of whose dimensions exist
+        auto load_whole = [&](int u, const char *kb, const char *vb) {
+            const unsigned k_to = at + unsigned(u * kWave * 16), v_to = values_at + unsigned(u * kWave * 16);
+            if (4 * DK == A::kPieces) {
+                load_to_lds<A::kOnce>(kb, k_off[u], k_to, vb, v_off[u], v_to);
+            } else {
+                if (key_piece(u) < 4 * DK) load_to_lds<A::kOnce>(kb, k_off[u], k_to);
+                if (value_piece(u) < 4 * DK) load_to_lds<A::kOnce>(vb, v_off[u], v_to);
+            }
+        };
         if (in_page) {
             if (tile == base_tile + kWave) {
                 base_tile = tile;
@@ -436,12 +464,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
             const char *vb = v_head + (pg * v_page + entry * v_token) * 16;
             if (valid == kAll && whole_rows) {
 #pragma unroll
-                for (int u = 0; u < A::kLoads; ++u) {
-                    if (4 * DK == A::kPieces || key_piece(u) < 4 * DK)
-                        load_to_lds<A::kOnce>(kb, k_off[u], at + u * kWave * 16);
-                    if (4 * DK == A::kPieces || value_piece(u) < 4 * DK)
-                        load_to_lds<A::kOnce>(vb, v_off[u], values_at + u * kWave * 16);
-                }
+                for (int u = 0; u < A::kLoads; ++u) load_whole(u, kb, vb);
                 return;
             }
 #pragma unroll
@@ -478,10 +501,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                     kb = k_head + (int64_t(pg * k_page) + back * k_token) * 16;
                     vb = v_head + (int64_t(pg * v_page) + back * v_token) * 16;
                 }
-                if (4 * DK == A::kPieces || key_piece(u) < 4 * DK)
-                    load_to_lds<A::kOnce>(kb, k_off[u], at + u * kWave * 16);
-                if (4 * DK == A::kPieces || value_piece(u) < 4 * DK)
-                    load_to_lds<A::kOnce>(vb, v_off[u], values_at + u * kWave * 16);
+                load_whole(u, kb, vb);
                 e = e + A::kPerLoad == page_size ? 0 : e + A::kPerLoad;
             }
             return;
