@@ -605,9 +605,12 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                 }
             if (some_rows) {
                 u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
-                for (int i = lane; i < A::kKeys * A::kPieces; i += kWave)
+                for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
+                    // (the places of pieces that a head does not have hold what was in LDS before)
+                    if (4 * DK != A::kPieces && (i % A::kPieces ^ A::value_swizzle(i / A::kPieces)) >= 4 * DK) continue;
                     most = __builtin_elementwise_max(
                         most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
+                }
                 bool odd = false;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) odd |= most[e] >= M::kInfinity;
