@@ -19,7 +19,9 @@
 // than 2^8 (the weights then stay below 2^8, and their sum's rounding is the
 // same): otherwise the accumulators need no rescaling.  Scores, sums and
 // accumulators are fp32; the weights are rounded to the cache's type, which the
-// matrix instructions need, before they multiply V.
+// matrix instructions need, before they multiply V.  A half rounds what is below
+// 2^-25 to zero, which many keys far below one would miss: its weights are
+// taken 2^7 higher, up to 2^15, so that one counts down to 2^-32 of the row's largest.
 //
 // What bounds it depends on the rows.  Few: reading the cache, once (3 prefixes of
 // 100000 tokens for 5 x 4 rows, 8 heads of 128, bf16: 198 us, 1.24 GB at 6.2 TB/s,
@@ -159,6 +161,7 @@ struct Matrix;
 template <>
 struct Matrix<Bf16> {
     static constexpr unsigned short kInfinity = 0x7f80;   // its bits
+    static constexpr float kRoom = 0.0f;                  // of its exponents above the weights', see above
     static __device__ __forceinline__ f32x4 mul(s16x8 a, s16x8 b, f32x4 c) {
         typedef __bf16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -171,6 +174,7 @@ struct Matrix<Bf16> {
 template <>
 struct Matrix<F16> {
     static constexpr unsigned short kInfinity = 0x7c00;
+    static constexpr float kRoom = 7.0f;
     static __device__ __forceinline__ f32x4 mul(s16x8 a, s16x8 b, f32x4 c) {
         typedef _Float16 v8 __attribute__((ext_vector_type(8)));
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -529,7 +533,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     const unsigned v_first = unsigned(v_in * A::kPitch + 16 * (((col % 4) / 2) ^ A::value_swizzle(v_in)) + 8 * (col & 1));
 
     f32x4 o[RT][A::kTiles];
-    float m[RT], sum[RT];   // sum: of the weights of this lane's keys, before they are rounded
+    float m[RT], sum[RT];   // m: what weights are relative to; sum: of this lane's keys', before they are rounded
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         m[r] = -__builtin_inff();
@@ -625,12 +629,12 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
 #pragma unroll
             for (int e = 1; e < 8 * C; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
             top[r] *= to_log2;
-            rises |= top[r] > m[r] + 8.0f;   // (also while m is -inf)
+            rises |= top[r] > m[r] + (8.0f + M::kRoom);   // (also while m is -inf)
         }
         if (__ballot(rises)) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const float now = __builtin_fmaxf(m[r], row_max(top[r]));
+                const float now = __builtin_fmaxf(m[r], row_max(top[r]) - M::kRoom);
                 const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
                 m[r] = now;
                 sum[r] *= f;
