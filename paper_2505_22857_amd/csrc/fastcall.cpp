@@ -15,6 +15,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -208,6 +209,9 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 bool on_current_device(const at::Tensor &t) { return t.device().index() == c10::hip::current_device(); }
 
+// Whether a call without a backward pass would lose a gradient (the Python function refuses it).
+bool tracked(const at::Tensor *t) { return t && t->requires_grad() && c10::GradMode::is_enabled(); }
+
 // A device tensor of this type and shape on `like`'s device, or None where it may
 // be: with unit stride in its last dimension (rows) or contiguous.
 struct Input {
@@ -324,6 +328,7 @@ bool cache_of(PyObject *k, PyObject *v, ngpu_kv_cache_t &c, const at::Tensor *&k
     Input values;
     if (!values.set(v, keys->scalar_type(), keys->sizes(), *keys, true)) return false;
     if (keys->size(3) > 1 && keys->stride(3) != 1) return false;
+    if (tracked(keys) || tracked(values.t)) return false;
     for (int i = 1; i < 4; ++i)
         if (keys->size(i) > INT32_MAX) return false;
     c = {type_code(keys->scalar_type()), int32_t(keys->size(2)), int32_t(keys->size(3)), int32_t(keys->size(1)),
@@ -368,6 +373,7 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) try {
             return none();
         out = at::empty(x->sizes(), keys->options());
     }
+    if (tracked(kx.t) || tracked(v.t) || tracked(q.t) || tracked(cos.t) || tracked(sin.t)) return none();
     Ref result(q.t ? held(out) : Py_NewRef(Py_True));   // (None would say that the call was not made)
     if (!result.p) return none();
     const ngpu_kv_append_t args{S, T, kx.ptr(), v.ptr(), kx.stride(0), kx.stride(1), kx.stride(2), v.stride(0),
@@ -398,7 +404,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     Input q, pages, lengths, prefix, prefix_lengths, q_lengths;
     if (!q.set(a[0], keys->scalar_type(), {S, T, x->size(2), cache.dim}, *keys, true) ||
         !q_lengths.set(a[7], at::kInt, {S}, *keys, false, true) || (a[3] == Py_None) != (a[4] == Py_None) ||
-        (a[5] == Py_None) != (a[6] == Py_None))
+        (a[5] == Py_None) != (a[6] == Py_None) || tracked(q.t))
         return none();
     if (a[3] != Py_None && (!table_of(a[3], S, *keys, pages) || pages.t->size(1) == 0 ||
                             !lengths.set(a[4], at::kInt, {S}, *keys, false)))

@@ -6,6 +6,8 @@
 group share (the hypotheses of one utterance) read once.  All three enqueue
 their HIP kernels on the current stream (or ``stream``) and return; the C ABI is
 ``include/ngpu_lm.h``.  Page tables, lengths and tokens are int32 tensors.
+None has a gradient: ``kv_append`` and ``attend`` refuse tensors that require one
+while gradients are recorded.
 """
 
 from __future__ import annotations
@@ -118,6 +120,14 @@ def _need(t, name, device, dtype, shape, rows=False):
     elif not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _untracked(**tensors):
+    """Nothing here has a backward pass, and a result without its graph would be wrong in silence."""
+    if _torch_mod().is_grad_enabled():
+        for name, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise TypeError(f"{name} must not require a gradient: this call has none (torch.no_grad() or detach())")
 
 
 def _device_of(t, name):
@@ -248,6 +258,7 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
         a.q_heads = q.shape[2]
         a.q = _need(q, "q", dev, dt, (S, T, q.shape[2], cache.dim), rows=True)
         a.q_stride_seq, a.q_stride_token, a.q_stride_head = q.stride()[:3]
+    _untracked(k=k, v=v, k_cache=k_cache, v_cache=v_cache, q=q, cos=cos, sin=sin)
     with _on(dev, stream) as handle:
         out = torch.empty(q.shape, dtype=dt, device=dev) if q is not None else None
         a.q_out = out.data_ptr() if out is not None else None
@@ -296,6 +307,7 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
         a.lengths = _need(lengths, "lengths", dev, i32, (S,))
         if a.pages_width == 0:
             a.pages = None   # a table without pages holds no own tokens
+    _untracked(q=q, k_cache=k_cache, v_cache=v_cache)
     lib = _library()
     with _on(dev, stream) as handle:
         out = torch.empty(q.shape, dtype=dt, device=dev)
