@@ -97,6 +97,8 @@ def _on(device, stream):
     """Runs on the tensors' device, and allocates for the stream that the work is enqueued on: what is
     freed when the call returns is then handed out again in that stream's order."""
     torch = _torch_mod()
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors are on {device}")
     with contextlib.ExitStack() as stack:
         if device.index != torch.cuda.current_device():
             stack.enter_context(torch.cuda.device(device))
