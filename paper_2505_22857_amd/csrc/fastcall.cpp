@@ -257,7 +257,7 @@ PyObject *draft(PyObject *, PyObject *const *a, Py_ssize_t n) try {
         k > NGPU_LM_MAX_DRAFT)
         return none();
     const at::Tensor *states = dense(a[2], at::kInt);
-    if (!states) return none();
+    if (!states || !on_current_device(*states)) return none();
     const int64_t B = states->numel();
     const bool sample = temperature != 0.0f;
     Input noise, last;
