@@ -434,8 +434,8 @@ class NgpuLM:
                     _check(r)
                 return r
         import torch
-        from .serving import MAX_DRAFT, _need, _on
-        B, V, k, temperature = states.numel(), self.vocab_size, int(k), float(temperature)
+        from .serving import MAX_DRAFT, _need, _on, _temperature
+        B, V, k, temperature = states.numel(), self.vocab_size, int(k), _temperature(temperature)
         dev, sample = states.device, temperature != 0.0
         if not 1 <= k <= MAX_DRAFT:
             raise ValueError(f"k must lie in [1, {MAX_DRAFT}]")

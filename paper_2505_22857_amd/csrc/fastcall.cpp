@@ -232,6 +232,9 @@ struct Input {
     int64_t stride(int64_t i) const { return t ? t->stride(i) : 0; }
 };
 
+// A temperature; one that only rounds to 0, which is greedy, is left to the Python function, which refuses it.
+bool temperature_of(PyObject *o, float &t) { return real(o, t) && (t != 0.0f || PyFloat_AS_DOUBLE(o) == 0.0); }
+
 int32_t type_code(at::ScalarType t) {
     return t == at::kFloat ? NGPU_F32 : (t == at::kHalf ? NGPU_F16 : (t == at::kBFloat16 ? NGPU_BF16 : -1));
 }
@@ -253,7 +256,7 @@ PyObject *answer(int rc, Ref &result) { return rc != NGPU_OK ? PyLong_FromLong(r
 PyObject *draft(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     int64_t h, V, k;
     float temperature;
-    if (n != 7 || !whole(a[0], h) || !whole(a[1], V) || !whole(a[3], k) || !real(a[5], temperature) || k < 1 ||
+    if (n != 7 || !whole(a[0], h) || !whole(a[1], V) || !whole(a[3], k) || !temperature_of(a[5], temperature) || k < 1 ||
         k > NGPU_LM_MAX_DRAFT)
         return none();
     const at::Tensor *states = dense(a[2], at::kInt);
@@ -286,7 +289,7 @@ PyObject *draft(PyObject *, PyObject *const *a, Py_ssize_t n) try {
 // logprobs on or None
 PyObject *verify(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     float temperature;
-    if (n != 8 || !real(a[5], temperature)) return none();
+    if (n != 8 || !temperature_of(a[5], temperature)) return none();
     const at::Tensor *logits = any_tensor(a[0], 3);
     if (!logits || logits->size(1) < 1 || !on_current_device(*logits)) return none();
     const int64_t B = logits->size(0), K = logits->size(1) - 1, V = logits->size(2);

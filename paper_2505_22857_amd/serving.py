@@ -124,6 +124,12 @@ def _need(t, name, device, dtype, shape, rows=False):
     return t.data_ptr()
 
 
+def _temperature(t):
+    """A float as the library is to check it: what fp32 would round to 0, which is greedy, stays one that is refused."""
+    t = float(t)
+    return math.copysign(1e-30, t) if 0.0 < abs(t) < 1e-30 else t
+
+
 def _untracked(**tensors):
     """Nothing here has a backward pass, and a result without its graph would be wrong in silence."""
     if _torch_mod().is_grad_enabled():
@@ -167,7 +173,7 @@ def verify(logits, tokens, logprobs=None, uniforms=None, noise=None, temperature
     code = _type_code(logits.dtype)
     if code is None:
         raise TypeError("logits must be float32, float16 or bfloat16")
-    temperature = float(temperature)
+    temperature = _temperature(temperature)
     sample = temperature != 0.0
     if sample and (noise is None or (K > 0 and uniforms is None)):
         raise ValueError("sampling needs uniforms and noise")

@@ -60,3 +60,20 @@ def test_gradients_are_refused(path):
             with torch.no_grad():
                 assert torch.equal(call(**{name: leaf(x)}), want)
             assert torch.equal(call(**{name: leaf(x).detach()}), want)
+
+
+@pytest.mark.parametrize("temperature", [1e-50, -1e-50, 5e-324, 1e-40, -1e-7])
+def test_temperatures_that_round_to_zero(path, temperature):
+    """Not greedy: refused, as the library's least temperature says."""
+    from synth import make_model
+    lm = ng.NgpuLM.from_model(make_model("trigram_v128")).upload("cuda")
+    if path == "ctypes":
+        lm._fast = None
+    g = torch.Generator(device="cuda").manual_seed(1)
+    logits = torch.randn(2, 3, 128, generator=g, device="cuda")
+    noise = torch.ones(2, 2, 128, device="cuda")
+    with pytest.raises(ng.NgpuError, match="temperature"):
+        ng.verify(logits, ints(np.zeros((2, 2))), uniforms=torch.rand(2, 2, device="cuda"), noise=noise[:, 0].contiguous(),
+                  temperature=temperature)
+    with pytest.raises(ng.NgpuError, match="temperature"):
+        lm.draft(ints([0, 0]), 2, noise=noise, temperature=temperature)
