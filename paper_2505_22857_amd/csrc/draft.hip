@@ -32,6 +32,7 @@ struct Draft {
     int64_t noise_b, noise_k;
     int K;
     float to_log2;   // log2 e / temperature
+    float inverse;   // 1 / temperature
     int32_t *tokens, *draft_states;
     float *logprobs;
     bool streams;
@@ -107,11 +108,10 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
     auto write_row = [&](int k) {
         if (!rows) return;
         float *row = rows + int64_t(k) * V + g.t0;
-        constexpr float kLn2 = 0.693147180559945f;
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             if (FULL || kWave * i + lane < g.own) {
-                const float y = ((x[i] - m) * d.to_log2 - log_total) * kLn2;
+                const float y = (x[i] - m) * d.inverse - log_total;
                 if (STREAM)
                     __builtin_nontemporal_store(y, &row[kWave * i + lane]);
                 else
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(W * kWave) void draft_kernel(Draft d) {
         }
         s = to;
         enter(token);
-        if (SAMPLE) log_total = __builtin_amdgcn_logf(total);   // (v_log_f32 is log2)
+        if (SAMPLE) log_total = __builtin_amdgcn_logf(total) * 0.693147180559945f;   // (v_log_f32 is log2)
         if (threadIdx.x == 0) {
             tokens[k] = token;
             states[k + 1] = s;
@@ -247,7 +247,7 @@ hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *
     // 51.5 us instead of 58.5; 16 x 8 rows 33 instead of 30.
     const bool streams = B * K * t.vocab_size * 4 > (int64_t(32) << 20);
     const Draft d{t, uni, states, last, sample ? noise : nullptr, noise_b, noise_k, K, sample ? 1.44269504088896f / temperature : 0.0f,
-                  tokens, draft_states, sample ? logprobs : nullptr, streams};
+                  sample ? 1.0f / temperature : 0.0f, tokens, draft_states, sample ? logprobs : nullptr, streams};
     const int V = t.vocab_size;
     // Wavefronts a sequence: one exchange more against fewer tokens a lane.  us for 8 steps of 4 / 256 / 1024
     // sequences: 256 tokens 9.3 / 10.7 / 12.3 by one wavefront, 12.6 / 13.8 / 19.6 by four; 512 11.0 / 12.9 / 18.1 by one,

@@ -77,3 +77,27 @@ def test_temperatures_that_round_to_zero(path, temperature):
                   temperature=temperature)
     with pytest.raises(ng.NgpuError, match="temperature"):
         lm.draft(ints([0, 0]), 2, noise=noise, temperature=temperature)
+
+
+@pytest.mark.parametrize("V", [100, 300, 1000, 1024, 2000, 3000, 8192])
+@pytest.mark.parametrize("temperature", [1.0, 0.8, 1.3])
+def test_rows_have_the_formulas_roundings(V, temperature):
+    """Draft rows are (x - max x) / temperature - log sum to the bit, each operation rounded once in fp32 and the division
+    as a product with the rounded inverse: at the row's maximum that is the logarithm itself, negative.  That is off by
+    an ulp of log2 of at most 13 bits (1e-6), and by the sum's relative error: exponents of size 20 rounded twice (2e-6)
+    and up to 40 additions in a row that hardly ever err alike."""
+    from synth import generate_model, uniform_states
+    m = generate_model(V, [V, 3 * V, 2 * V], 1.0, seed=V)
+    lm = ng.NgpuLM.from_model(m).upload("cuda:0")
+    states = torch.from_numpy(uniform_states(m, 9, seed=2)).cuda()
+    noise = torch.empty(9, 3, V, device="cuda").exponential_()
+    _, after, rows = lm.draft(states, 3, noise=noise, temperature=temperature)
+    inverse = np.float32(1) / np.float32(temperature)
+    for k in range(3):
+        x = lm.advance(after[:, k].contiguous())[0].cpu().numpy()
+        row = rows[:, k].cpu().numpy()
+        top = x.max(1, keepdims=True)
+        log_sum = -row[x == top].reshape(9, -1)[:, :1]
+        assert np.array_equal(row, (x - top) * inverse - log_sum)
+        z = (x.astype(np.float64) - top) / np.float32(temperature)
+        assert np.all(np.abs(log_sum[:, 0] - np.log(np.exp(z).sum(1))) <= 4e-6)
