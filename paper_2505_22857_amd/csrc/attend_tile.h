@@ -204,12 +204,8 @@ __device__ __forceinline__ float row_sum(float x) {
     return both(__builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
 }
 
-// Waits until no more than N of this wavefront's loads from memory are in
-// flight, and for its LDS loads and stores.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-}
+// Waits for this wavefront's loads from memory and its LDS loads and stores.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 // 16 bytes a lane from memory to LDS at `at` + 16 lane (uniform `at`).  As asm, since
 // the compiler would wait for it before any later LDS load.  (m0 is a reserved register, which
 // nothing else in these kernels uses: a clobber would only be warned about.)  The load has to come a
@@ -268,16 +264,14 @@ struct AttendTile {
     static constexpr int kPitch = DK <= 2 ? 128 : (DK <= 4 ? 256 : 512);   // bytes of a row in LDS
     static constexpr int kPieces = kPitch / 16;                 // 16-byte chunks of it
     static constexpr int kStage = 2 * kKeys * kPitch;           // keys, then values
-    static constexpr int kStages = 2;                           // tiles in LDS: one in use, the others on their way
+    static constexpr int kStages = 2;                           // tiles in LDS: one in use, the other on its way
     static constexpr int kLds = kStages * kStage;
     static constexpr int kPerLoad = kWave / kPieces;            // rows a load instruction brings
     static constexpr int kLoads = kLoad / kPerLoad;
     static constexpr bool kOnce = WR == 1;                      // its problem's only block of rows: keys are read once
     static constexpr int kTiles = 2 * DK;                       // of 16 dimensions
-    static constexpr int kIssued = 2 * kLoads;                  // load instructions of a wavefront and tile
     static_assert(kKeysAhead <= DK && kValuesAhead <= kTiles, "the first steps lie in the first chunk");
-    static_assert(kLoad % 8 == 0 && kLoad <= 32, "a wavefront's keys are whole bytes of a mask");
-    static_assert((kStages - 2) * kIssued < 64, "the loads in flight are counted in six bits");
+    static_assert(kLoad == (WR == 1 ? 32 : 16), "a wavefront's keys are half of a mask where several share it");
 
     static __device__ __forceinline__ int key_swizzle(int row) { return kPieces == 8 ? (row >> 1) & 7 : row & 15; }
     static __device__ __forceinline__ int value_swizzle(int row) {
@@ -430,18 +424,12 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     asm volatile("" : "+s"(no_data));   // its address is loaded once
     unsigned valid = 0;   // keys that exist among those this wavefront loaded last
     auto fetch = [&](int tile, int stage) {
-        constexpr unsigned kAll = A::kLoad == 32 ? 0xffffffffu : (1u << A::kLoad % 32) - 1u;
+        constexpr unsigned kAll = A::kLoad == 32 ? 0xffffffffu : 0xffffu;
         const unsigned at = __builtin_amdgcn_readfirstlane(lds0 + unsigned(stage * A::kStage + wave * A::kLoad * A::kPitch));
         const unsigned values_at = at + A::kKeys * A::kPitch;
         const unsigned j = first_key(tile);
         auto put_mask = [&]() {
-            if (WR > 1 && lane == 0) {
-                char *byte = reinterpret_cast<char *>(masks[stage]) + wave * (A::kLoad / 8);
-                if (A::kLoad == 8)
-                    *reinterpret_cast<uint8_t *>(byte) = uint8_t(valid);
-                else
-                    *reinterpret_cast<uint16_t *>(byte) = uint16_t(valid);
-            }
+            if (WR > 1 && lane == 0) reinterpret_cast<uint16_t *>(masks[stage])[wave] = uint16_t(valid);
         };
         // the u-th rows of a whole tile, all of whose dimensions exist
         auto load_whole = [&](int u, const char *kb, const char *vb) {
@@ -681,31 +669,20 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         __builtin_amdgcn_s_setprio(0);
     };
 
-    // Tiles are fetched kStages - 1 ahead.  A tile has arrived when no more loads
-    // are in flight than those of the tiles after it.
-    unsigned ahead[A::kStages];   // WR == 1: the masks of the tiles on their way
+    // Tiles are fetched one ahead.
     int stage = 0;
-#pragma unroll
-    for (int i = 0; i < A::kStages - 1; ++i) {
-        if (tile0 + i < tile1) fetch(tile0 + i, i);
-        ahead[i] = valid;
-    }
+    if (tile0 < tile1) fetch(tile0, 0);
     for (int tile = tile0; tile < tile1; ++tile) {
-        if (A::kStages > 2 && tile + A::kStages - 2 < tile1)
-            wait_loads<(A::kStages - 2) * A::kIssued>();
-        else
-            wait_loads<0>();
+        const unsigned mine = valid;   // of this tile's keys
+        wait_loads();
         if (WR > 1) asm volatile("s_barrier" ::: "memory");
-        if (tile + A::kStages - 1 < tile1) fetch(tile + A::kStages - 1, stage == 0 ? A::kStages - 1 : stage - 1);
-        ahead[A::kStages - 1] = valid;
+        if (tile + 1 < tile1) fetch(tile + 1, 1 - stage);
         unsigned exists[A::kChunks];
 #pragma unroll
         for (int c = 0; c < A::kChunks; ++c)
-            exists[c] = __builtin_amdgcn_readfirstlane(WR > 1 ? masks[stage][c] : ahead[0]);
+            exists[c] = __builtin_amdgcn_readfirstlane(WR > 1 ? masks[stage][c] : mine);
         take(stage, tile * A::kKeys, exists);
-#pragma unroll
-        for (int i = 0; i + 1 < A::kStages; ++i) ahead[i] = ahead[i + 1];
-        stage = stage + 1 == A::kStages ? 0 : stage + 1;
+        stage = 1 - stage;
     }
 
     float total[RT];
