@@ -331,7 +331,8 @@ size_t ngpu_lm_verify_workspace(int64_t B, int32_t K, int64_t V);
  * lowest of several), and the added token is the argmax of row a.
  * A NaN logit counts as -inf; +inf logits share the row's whole mass; a row with
  * nothing above -inf gives every token p = 0, so nothing is kept there and
- * token 0 is added.  B = 0 is a no-op. */
+ * token 0 is added.  Classes that the draft does not know (an end-of-sequence class of the network's) have
+ * log-probability -inf in its rows, which have V columns.  B = 0 is a no-op. */
 int ngpu_lm_verify(const ngpu_verify_t *args, void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* A paged cache of keys and values: pages of page_size tokens, each with `heads`
@@ -404,7 +405,9 @@ typedef struct {
     float *lse;                    /* [S, T, q_heads] log of the softmax's sum, or NULL */
 } ngpu_attend_t;
 
-/* Device memory an attention needs, 16-byte aligned, not initialised. */
+/* Device memory an attention needs, 16-byte aligned, not initialised.  To be asked with the call's own arguments:
+ * it follows from the sizes, the strides, whether `pages` is NULL and the 16-byte alignment of k, v and out, and
+ * is 0 for arguments that the call refuses (a cache without its pointers among them). */
 size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args);
 
 /* Query t < q_lengths[s] attends to every token of its group's prefix and to the
@@ -412,7 +415,10 @@ size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_
  *   out = sum_j softmax_j(scale * q . k_j) v_j,
  * the sums in fp32.  Keys on a page outside [0, num_pages) do not take part, nor
  * does anything else that a query does not attend to, whatever it holds.  A row
- * without any key, and one that does not count, is zero with lse = -inf. */
+ * without any key, and one that does not count, is zero with lse = -inf.
+ * The matrix cores take caches whose dim and strides are multiples of 8 elements, with k, v and out aligned to
+ * 16 bytes, whose pages span no more than 2^34 elements (32 GiB; page stride times num_pages); a kernel that
+ * reads element by element and each row's keys by themselves takes the others, many times slower. */
 int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void *d_workspace,
                    size_t workspace_bytes, void *hip_stream);
 

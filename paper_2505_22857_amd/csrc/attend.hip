@@ -168,7 +168,8 @@ struct Choice {
 };
 
 // The matrix kernel loads 16 bytes of 8 elements at a time and keeps a row of
-// the cache as a 32-bit number of them, and of a query as one of rows.
+// the cache as a 32-bit number of them, and of a query as one of rows: pages that
+// span more than 32 GiB of keys or values go by the element kernel.
 bool takes_tiles(const ngpu_kv_cache_t &c, const ngpu_attend_t &a) {
     const int64_t strides[] = {c.k_stride_page, c.k_stride_token, c.k_stride_head,
                                c.v_stride_page, c.v_stride_token, c.v_stride_head};

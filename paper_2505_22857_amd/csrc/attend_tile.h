@@ -19,13 +19,14 @@
 // than 2^8 (the weights then stay below 2^8, and their sum's rounding is the
 // same): otherwise the accumulators need no rescaling.  Scores, sums and
 // accumulators are fp32; the weights are rounded to the cache's type, which the
-// matrix instructions need, before they multiply V.  A half rounds what is below
+// matrix instructions need, before they multiply V, which makes the result's error 1.3
+// (half) to 1.4 (bfloat16) times that of fp32 weights.  A half rounds what is below
 // 2^-25 to zero, which many keys far below one would miss: its weights are
 // taken 2^7 higher, up to 2^15, so that one counts down to 2^-32 of the row's largest.
 //
 // What bounds it depends on the rows.  Few: reading the cache, once (3 prefixes of
-// 100000 tokens for 5 x 4 rows, 8 heads of 128, bf16: 198 us, 1.24 GB at 6.2 TB/s,
-// 0.9 of a fill's rate).  Many: the matrix instructions, the exponentials between
+// 100000 tokens for 5 x 4 rows, 8 heads of 128, bf16: 197 to 204 us, 1.24 GB at 6.1
+// to 6.3 TB/s, 0.9 of a fill's rate).  Many: the matrix instructions, the exponentials between
 // them and LDS's reads, which take about as long as the first, share a SIMD's two
 // wavefronts (4 x 384 rows: 7.4 us per 1024 tokens of prefix, 870 TFLOP/s, behind 24 us
 // for launches, first loads, partial sums and their join; 32768 tokens ran at 630 to 710 in

@@ -12,10 +12,10 @@
 // A step is a chain of dependent accesses (chain record, dense row and arcs,
 // exchange, next record), so small batches are bound by latency; the noise rows
 // do not depend on the chain and are loaded a step ahead.  Large ones are bound
-// by reading the noise and writing the rows (8 bytes a token).  Measured, 20M 6-gram or models of its kind: 5.7 us
-// for 4 greedy tokens of 4 sequences (128 tokens), 28 us for 8 sampled ones of 256 (1024 tokens: 3.5 us a step, of
-// which the noise and the rows would take 0.4), 52 us for 5 of 301 (8192 tokens: 99 MB, 1.9 TB/s, and as much again of
-// the model's dense rows).
+// by reading the noise and writing the rows (8 bytes a token).  Measured, n-grams of a corpus of 5000 tokens (the first)
+// or 200,000: 5.8 us for 4 greedy tokens of 4 sequences (trigram, 128 tokens), 28 us for 8 sampled ones of 256 (6-gram,
+// 1024 tokens: 3.5 us a step, of which the noise and the rows would take 0.4), 52 us for 5 of 301 (4-gram, 8192 tokens:
+// 99 MB, 1.9 TB/s, and as much again of the model's dense rows).
 #include <hip/hip_runtime.h>
 
 #include "reduce.h"
@@ -250,9 +250,10 @@ hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *
                   sample ? 1.0f / temperature : 0.0f, tokens, draft_states, sample ? logprobs : nullptr, streams};
     const int V = t.vocab_size;
     // Wavefronts a sequence: one exchange more against fewer tokens a lane.  us for 8 steps of 4 / 256 / 1024
-    // sequences: 256 tokens 9.3 / 10.7 / 12.3 by one wavefront, 12.6 / 13.8 / 19.6 by four; 512 11.0 / 12.9 / 18.1 by one,
-    // 13.1 / 14.3 / 22.6 by four; 1024 12.6 / 14.7 / 26.6 by four, 14.4 / 16.0 / 25.4 by two, 15.2 / 17.0 / 45.4 by eight;
-    // 2048 15.0 / 20.1 / 49.2 by eight, 17.0 / 21.0 / 36.2 by four; 4096 17.4 / 26.4 / 74 by eight, 25.7 / 33.3 / 120 by 16.
+    // sequences from states of their own, 6-grams (above 1024 tokens 4-grams) of a corpus of 200,000: 256 tokens 17 / 19 /
+    // 27 by one wavefront, 20 / 22 / 36 by four; 512 20 / 22 / 31 by one, 20 / 23 / 37 by four; 1024 21 / 29 / 39 by four,
+    // 23 / 30 / 39 by two, 22 / 31 / 67 by eight; 2048 18 / 27 / 63 by eight, 20 / 28 / 43 by four; 4096 22 / 33 / 89 by
+    // eight, 24 / 34 / 125 by 16.
     if (V <= 256) return launch_group<1, 4>(d, B, stream);
     if (V <= 512) return launch_group<1, 8>(d, B, stream);
     if (V <= 1024) return launch_group<4, 4>(d, B, stream);

@@ -385,7 +385,8 @@ static Verify plan(const ngpu_verify_t &a, char *workspace, size_t *bytes) {
     *bytes = 0;
     // One launch takes 8.5 / 9.4 / 19 us for 1 / 64 / 512 sequences of 5 rows of 4096 (fp32, 5 or 6 rows), two with
     // the chunks below 8.7 / 10.2 / 20; of 8192 10.6 / 12.6 / 26.8, two 8.8 / 12.3 / 30.2; of 16384 one 18.7 / 22 / 47,
-    // two 9.5 / 14.4 / 51.
+    // two 9.5 / 14.4 / 51.  So up to 8192 tokens no batch needs a workspace, though a few sequences of 8192 would be 2 us
+    // faster by two.
     if (a.V <= kWhole) return v;
     // Smaller chunks while they fill the chip at most twice: 9.7 us, not 13.2, for one sequence of 5 rows of
     // 32768, 14.4, not 16.3, for 64 of 6 of 16384.  More of them only repeat what each does first: 96 sequences of 128001

@@ -150,8 +150,8 @@ def verify(logits, tokens, logprobs=None, uniforms=None, noise=None, temperature
 
     ``logits`` [B, K + 1, V] (float32, float16 or bfloat16): row k scores the token at place k.
     ``tokens`` [B, K] int32: the draft (a token outside [0, V) ends it); ``lengths`` [B]: how many of
-    them count.  ``logprobs`` [B, K, V] float32: the draft's log-probabilities, None where every drafted
-    token had probability 1.  ``uniforms`` [B, K] in [0, 1) and ``noise`` [B, V], unit exponential,
+    them count.  ``logprobs`` [B, K, V] float32: the draft's log-probabilities (-inf for classes that it does
+    not know, as an end of sequence), None where every drafted token had probability 1.  ``uniforms`` [B, K] in [0, 1) and ``noise`` [B, V], unit exponential,
     float32: the random numbers.  ``temperature`` 0: greedy, without the last three.
     ``draft_states`` [B, K + 1] int32 of ``NgpuLM.draft``.
 
@@ -282,7 +282,8 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
     S / G share their group's prefix, which is read once for all of them.  With ``pages`` [S, width] and
     ``lengths`` [S], each sequence has tokens of its own after it, the T query tokens (or the first
     ``q_lengths[s]`` of them) being the last: query t sees the whole prefix and the own tokens up to its
-    own.  ``scale`` is 1 / sqrt(dim) unless given.
+    own.  ``scale`` is 1 / sqrt(dim) unless given.  Dimensions and strides in multiples of 8, 16-byte alignment and
+    pages that span at most 32 GiB take the matrix cores; other caches a kernel many times slower.
 
     Returns [S, T, q heads, dim] (zero where a row sees no key or does not count), and with
     ``return_lse`` the log of each row's softmax sum [S, T, q heads] float32 (-inf there)."""
