@@ -17,7 +17,7 @@ import pytest
 
 import paper_2505_22857_amd as ng
 
-OBJDUMP = shutil.which("llvm-objdump") or "/opt/rocm/llvm/bin/llvm-objdump"
+OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"   # the compiler's own: another may not know the chip
 REGISTERS = re.compile(r"\bs(?:(\d+)|\[(\d+):(\d+)\])")
 
 
