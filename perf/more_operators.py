@@ -480,13 +480,13 @@ def _run_fork(s):
         return refs + by * more.index_add_(0, held, torch.ones_like(held, dtype=torch.int32))[:P]
     refs = count(count(refs, old, -1), pages, 1)
     # a page that is filled in part and held by others too is copied; the last holder keeps it
-    part = live & (length % page != 0) & (T > 0)
+    need_slots = torch.where(live, -(-(length + T) // page), 0)
+    part = live & (length % page != 0) & (T > 0) & (need_slots <= width)
     mine = pages.gather(2, (length // page).clamp(max=width - 1)[..., None])[..., 0]
     part &= mine >= 0
     before = ((mine[:, :, None] == mine[:, None, :]) & part[:, None, :] & part[:, :, None]).tril(-1).sum(-1)
     copy = part & (refs[mine.clamp(min=0)] - before > 1)
-    need_slots = torch.where(live, -(-(length + T) // page), 0)
-    need = copy.long() + need_slots - have
+    need = torch.where(need_slots <= width, copy.long() + need_slots - have, 0)
     upto = need.flatten().cumsum(0).view(G, K)
     free = refs == 0
     dropped = live & (((need > 0) & (upto > free.sum())) | (need_slots > width))
@@ -790,6 +790,9 @@ def _exact_fork(case, s):
     free = [p for p, r in enumerate(refs) if r == 0]
     seen, plans = dict(), []
     for i, (row, n) in enumerate(zip(rows, sizes)):
+        if n is not None and n + T > width * page:
+            plans.append((False, 0))
+            continue
         part = n is not None and T > 0 and n % page != 0
         at = (i // K, row[-1]) if part else None
         shared = part and refs[row[-1]] - seen.get(at, 0) > 1
@@ -800,7 +803,7 @@ def _exact_fork(case, s):
     for row, n, (shared, more) in zip(rows, sizes, plans):
         mine = free[taken:taken + shared + more]
         taken += shared + more
-        if n is not None and (taken > len(free) and shared + more > 0 or len(row) + more > width):
+        if n is not None and (taken > len(free) and shared + more > 0 or n + T > width * page):
             for p in row:
                 refs[p] -= 1
             row, n, shared, mine = [], -1, False, []
