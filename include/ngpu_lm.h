@@ -422,6 +422,109 @@ size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_
 int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void *d_workspace,
                    size_t workspace_bytes, void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Beam search.  One step over a batch of utterances: ngpu_lm_beam_step selects
+ * the best continuations of each utterance's hypotheses, ngpu_lm_kv_fork makes
+ * their page tables from their parents' and gives them pages to write into, and
+ * ngpu_lm_kv_copy (in each layer's cache) copies what two of them would
+ * otherwise write into.  ngpu_lm_kv_compact moves a pool's used pages together.
+ * ------------------------------------------------------------------------ */
+
+/* Most hypotheses an utterance, before a step and after it. */
+#define NGPU_LM_MAX_BEAMS 64
+
+/* Strides in elements; rows of asr have unit stride and hold V classes, outside plain fusion V + 1. */
+typedef struct {
+    int64_t B;                     /* utterances */
+    int32_t W, k;                  /* hypotheses before and after, 1..NGPU_LM_MAX_BEAMS each */
+    int32_t mode;                  /* NGPU_FUSION_PLAIN, _TRANSDUCER or _AED */
+    float lambda;
+    const float *asr;              /* [B, W, classes]; a stride may be 0 (one frame for all hypotheses) */
+    int64_t asr_stride_b, asr_stride_w;
+    const int32_t *states;         /* [B, W] */
+    const float *scores;           /* [B, W] sums so far; -inf (and NaN): no hypothesis, and its state is not looked at */
+    const int32_t *last;           /* [B, W] last classes (AED): a hypothesis whose last is V has ended; NULL: none has */
+    int32_t *out_tokens;           /* [B, k] class */
+    int32_t *out_parents;          /* [B, k] place among the W */
+    float *out_scores;             /* [B, k] */
+    int32_t *out_states;           /* [B, k] */
+} ngpu_beam_step_t;
+
+/* Device memory a step needs, 16-byte aligned, not initialised; free again when the call's work has run. */
+size_t ngpu_lm_beam_step_workspace(int64_t B, int32_t W, int32_t k);
+
+/* The k continuations with the largest sums of each utterance, over all its
+ * hypotheses w and classes c, in descending order:
+ *   total[w][c] = scores[w] + fma(lambda, lm[w][c], asr[w][c]),
+ * ties to the lowest w, then the lowest c.  lm is the query's score; class V is
+ * <eos> in AED mode, with the state's final weight, and blank in transducer
+ * mode, with lm = 0; it keeps the state.  A hypothesis that has ended continues
+ * as itself alone (class V, score and state unchanged).  A NaN total counts as
+ * -inf, and continuations at -inf are not selected: places that are left over
+ * hold token -1, parent -1, score -inf and state 0.  A state outside [0,
+ * num_states) of a hypothesis that is looked at gives no continuation and is
+ * counted for ngpu_lm_check_states.  B = 0 is a no-op.  CTC needs prefixes to be merged and is refused. */
+int ngpu_lm_beam_step(const ngpu_lm *lm, const ngpu_beam_step_t *args, void *d_workspace, size_t workspace_bytes,
+                      void *hip_stream);
+
+/* A pool of num_pages pages: refs[p] page tables hold page p, a page with 0 is free.
+ * Each row of a page table holds one reference for each of its entries in [0, num_pages); other entries are empty. */
+typedef struct {
+    int64_t G;                     /* groups (utterances) */
+    int64_t W, K;                  /* hypotheses of a group before (W) and after (K), at most NGPU_LM_MAX_FORK each */
+    const int32_t *pages;          /* [G * W, width] page tables, row stride pages_stride */
+    int64_t width, pages_stride;
+    const int32_t *lengths;        /* [G * W] tokens, clamped to what the table holds */
+    const int32_t *parents;        /* [G, K] place among the W; any other value: none */
+    const int32_t *tokens;         /* [G, K] tokens that will be appended, negative ones count as 0, or NULL: T each */
+    int64_t T;
+    int32_t page_size;
+    int64_t num_pages;
+    int32_t *refs;                 /* [num_pages], updated */
+    int32_t *out_pages;            /* [G * K, width] contiguous; must not overlap pages */
+    int32_t *out_lengths;          /* [G * K] */
+    int32_t *copies;               /* [G * K, 3] for ngpu_lm_kv_copy */
+} ngpu_kv_fork_t;
+#define NGPU_LM_MAX_FORK 4096
+#define NGPU_LM_MAX_PAGES ((int64_t)1 << 28)
+
+size_t ngpu_lm_kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages);
+
+/* Continuations take over their parents' tokens, and the old rows end.
+ *  1. Row (g, j) gets the first ceil(lengths / page_size) entries of its parent's row, and -1 behind; refs go down by one
+ *     for every entry of an old row (those behind its length too) and up by one for every entry of a new one.
+ *  2. A row that will append (tokens > 0) and whose last page is filled in part takes a fresh page for it where others
+ *     hold that page too: where refs, less the rows before it in its group that decided on that page, is above 1.
+ *     copies[row] = {that page, the fresh one, entries that are filled}; for other rows {-1, -1, 0}.
+ *  3. It takes fresh pages for the places of its new tokens behind.
+ * Fresh pages are the free ones of after step 1, the lowest to the first row (its copy first), each with refs 1.  A row
+ * whose pages, with those of the rows before, are not there, or whose tokens would not fit the table, is dropped: its
+ * entries are given back and -1, its length -1, no copy.  out_lengths: the parent's (without the new tokens), 0 without
+ * parent.  The lengths are counted in tokens the table holds, so rejected tokens are given up by passing shorter ones.
+ * Freeing is a fork without children: K = 0, or parents of -1.  A new sequence is a row of -1 entries and length 0 that
+ * is forked with as many tokens as its prompt has.  G = 0 is a no-op. */
+int ngpu_lm_kv_fork(const ngpu_kv_fork_t *args, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* For each of n rows {from, to, entries} of `copies`: entries [0, entries) of page `from` of the cache, keys and values,
+ * are copied to page `to`; entries are clamped to the page, and rows with a page outside [0, num_pages) or from = to do
+ * nothing.  No page may be the `to` of two rows, or one row's `to` and another's `from`. */
+int ngpu_lm_kv_copy(const ngpu_kv_cache_t *cache, const int32_t *copies, int64_t n, void *hip_stream);
+
+/* Device memory a compaction needs, 16-byte aligned, not initialised. */
+size_t ngpu_lm_kv_compact_workspace(int64_t num_pages);
+
+/* With n pages in use (refs other than 0), the i-th used page from n on moves to the i-th free one below n, in
+ * ascending order: copies[i] = {from, to, page_size}, {-1, -1, 0} behind the last of the num_pages / 2 rows; moved[p] is
+ * page p's new place (p itself where it stays or is free).  refs follow.  The tables are then to be put through
+ * ngpu_lm_kv_move, the caches through ngpu_lm_kv_copy. */
+int ngpu_lm_kv_compact(int32_t *refs, int64_t num_pages, int32_t page_size, int32_t *copies, int32_t *moved,
+                       void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* pages[r][i] = moved[pages[r][i]] for the entries in [0, num_pages) of a table [rows, width], row stride pages_stride
+ * (at least width where rows > 1). */
+int ngpu_lm_kv_move(int32_t *pages, int64_t rows, int64_t width, int64_t pages_stride, const int32_t *moved,
+                    int64_t num_pages, void *hip_stream);
+
 /* Synchronises hip_stream, then reports (and clears) how many out-of-range
  * input states the queries enqueued since the last check met.  Returns
  * NGPU_E_BAD_STATE when the count is non-zero. */

@@ -41,7 +41,8 @@ EXPORTED = [
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
     "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
-    "ngpu_lm_attend",
+    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy",
+    "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
 ]
 
@@ -107,7 +108,8 @@ def load_library(path: str = LIB_PATH):
     lib.ngpu_lm_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
         if name not in ("ngpu_lm_free", "ngpu_lm_device_bytes", "ngpu_lm_last_error", "ngpu_arpa_free",
-                        "ngpu_lm_verify_workspace", "ngpu_lm_attend_workspace"):
+                        "ngpu_lm_verify_workspace", "ngpu_lm_attend_workspace", "ngpu_lm_kv_fork_workspace",
+                        "ngpu_lm_kv_compact_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -481,8 +483,9 @@ class NgpuLM:
 
 from .serving import (MAX_DRAFT, MAX_HEAD_DIM, NGPU_BF16, NGPU_F16, NGPU_F32, NGPU_ROPE_HALF,  # noqa: E402
                       NGPU_ROPE_INTERLEAVED, attend, kv_append, rope_table, verify)
+from .pages import MAX_FORK, MAX_PAGES, kv_compact, kv_copy, kv_fork  # noqa: E402
 
-__all__ = ["verify", "kv_append", "attend", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
+__all__ = ["verify", "kv_append", "attend", "kv_fork", "kv_copy", "kv_compact", "MAX_FORK", "MAX_PAGES", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
            "NGPU_BF16", "NGPU_ROPE_HALF", "NGPU_ROPE_INTERLEAVED", "NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED", "NGPU_BUILD_BOS_EOS",
            "NGPU_BUILD_REPAIR_CLOSURE",
            "NGPU_FUSION_PLAIN", "NGPU_FUSION_CTC", "NGPU_FUSION_TRANSDUCER", "NGPU_FUSION_AED"]

@@ -1,5 +1,5 @@
 // C ABI entry points of the serving operators that need no language model:
-// verification, cache append and attention.  Argument checks and launches.
+// verification, the paged cache and its pages, and attention.  Argument checks and launches.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -14,6 +14,14 @@ hipError_t launch_verify(const ngpu_verify_t &a, void *workspace, hipStream_t st
 hipError_t launch_kv_append(const ngpu_kv_cache_t &c, const ngpu_kv_append_t &a, hipStream_t stream);
 size_t attend_workspace(const ngpu_kv_cache_t &c, const ngpu_attend_t &a);
 hipError_t launch_attend(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, void *workspace, hipStream_t stream);
+size_t kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages);
+hipError_t launch_kv_fork(const ngpu_kv_fork_t &a, void *workspace, hipStream_t stream);
+hipError_t launch_kv_copy(const ngpu_kv_cache_t &c, const int32_t *copies, int64_t n, hipStream_t stream);
+size_t kv_compact_workspace(int64_t num_pages);
+hipError_t launch_kv_compact(int32_t *refs, int64_t num_pages, int32_t page_size, int32_t *copies, int32_t *moved,
+                             void *workspace, hipStream_t stream);
+hipError_t launch_kv_move(int32_t *pages, int64_t rows, int64_t width, int64_t stride, const int32_t *moved,
+                          int64_t num_pages, hipStream_t stream);
 }  // namespace ngpu
 
 namespace {
@@ -98,6 +106,30 @@ int check_attend(const ngpu_kv_cache_t *c, const ngpu_attend_t *a) {
     return NGPU_OK;
 }
 
+int check_pool(int64_t num_pages, int32_t page_size) {
+    if (num_pages < 0 || num_pages > NGPU_LM_MAX_PAGES)
+        return refuse("num_pages = %lld outside [0, %lld]", (long long)num_pages, (long long)NGPU_LM_MAX_PAGES);
+    if (page_size < 1) return refuse("page_size = %d must be positive", page_size);
+    return NGPU_OK;
+}
+
+bool fork_sizes(int64_t G, int64_t W, int64_t K) {
+    return G >= 0 && G <= NGPU_LM_MAX_SEQUENCES && W >= 0 && W <= NGPU_LM_MAX_FORK && K >= 0 && K <= NGPU_LM_MAX_FORK &&
+           G * W <= NGPU_LM_MAX_SEQUENCES && G * K <= NGPU_LM_MAX_SEQUENCES;
+}
+
+int check_fork(const ngpu_kv_fork_t *a) {
+    if (!a) return refuse("null argument");
+    if (!fork_sizes(a->G, a->W, a->K))
+        return refuse("G = %lld, W = %lld, K = %lld: W and K lie in [0, %d], G W and G K in [0, %d]", (long long)a->G,
+                      (long long)a->W, (long long)a->K, NGPU_LM_MAX_FORK, NGPU_LM_MAX_SEQUENCES);
+    if (const int rc = check_pool(a->num_pages, a->page_size)) return rc;
+    if (a->width < 0 || a->width > INT32_MAX || a->pages_stride < 0) return refuse("bad page tables");
+    if (a->T < 0 || a->T > INT32_MAX) return refuse("T = %lld outside [0, 2^31 - 1]", (long long)a->T);
+    if (a->G * (a->W + a->K) > 0 && a->width > kMostElements / (a->G * (a->W + a->K))) return refuse("the call is too large");
+    return NGPU_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -162,6 +194,58 @@ int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void
         return refuse("null device pointer");
     if (const int rc = check_workspace(d_workspace, workspace_bytes, ngpu::attend_workspace(*cache, a))) return rc;
     return done(ngpu::launch_attend(*cache, a, d_workspace, static_cast<hipStream_t>(hip_stream)), "attend launch");
+}
+
+size_t ngpu_lm_kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages) {
+    if (!fork_sizes(G, 0, K) || num_pages < 0 || num_pages > NGPU_LM_MAX_PAGES || G * K == 0) return 0;
+    return ngpu::kv_fork_workspace(G, K, num_pages);
+}
+
+int ngpu_lm_kv_fork(const ngpu_kv_fork_t *args, void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_fork(args)) return rc;
+    const ngpu_kv_fork_t &a = *args;
+    const bool old = a.G * a.W > 0, made = a.G * a.K > 0;
+    if (!old && !made) return done(hipSuccess, "");
+    if ((old && (!a.lengths || (a.width > 0 && !a.pages))) || (a.num_pages > 0 && !a.refs) ||
+        (made && (!a.parents || !a.out_lengths || !a.copies || (a.width > 0 && !a.out_pages))))
+        return refuse("null device pointer");
+    if (a.out_pages && a.out_pages == a.pages) return refuse("out_pages must not overlap pages");
+    if (const int rc = check_workspace(d_workspace, workspace_bytes, ngpu_lm_kv_fork_workspace(a.G, a.K, a.num_pages)))
+        return rc;
+    return done(ngpu::launch_kv_fork(a, d_workspace, static_cast<hipStream_t>(hip_stream)), "fork launch");
+}
+
+int ngpu_lm_kv_copy(const ngpu_kv_cache_t *cache, const int32_t *copies, int64_t n, void *hip_stream) {
+    if (const int rc = check_cache(cache)) return rc;
+    if (n < 0 || n > NGPU_LM_MAX_PAGES) return refuse("n = %lld out of range", (long long)n);
+    if (n == 0 || cache->num_pages == 0) return done(hipSuccess, "");
+    if (!copies) return refuse("null device pointer");
+    return done(ngpu::launch_kv_copy(*cache, copies, n, static_cast<hipStream_t>(hip_stream)), "copy launch");
+}
+
+size_t ngpu_lm_kv_compact_workspace(int64_t num_pages) {
+    return num_pages <= 0 || num_pages > NGPU_LM_MAX_PAGES ? 0 : ngpu::kv_compact_workspace(num_pages);
+}
+
+int ngpu_lm_kv_compact(int32_t *refs, int64_t num_pages, int32_t page_size, int32_t *copies, int32_t *moved,
+                       void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_pool(num_pages, page_size)) return rc;
+    if (num_pages == 0) return done(hipSuccess, "");
+    if (!refs || !moved || (num_pages > 1 && !copies)) return refuse("null device pointer");
+    if (const int rc = check_workspace(d_workspace, workspace_bytes, ngpu::kv_compact_workspace(num_pages))) return rc;
+    return done(ngpu::launch_kv_compact(refs, num_pages, page_size, copies, moved, d_workspace,
+                                        static_cast<hipStream_t>(hip_stream)), "compaction launch");
+}
+
+int ngpu_lm_kv_move(int32_t *pages, int64_t rows, int64_t width, int64_t pages_stride, const int32_t *moved,
+                    int64_t num_pages, void *hip_stream) {
+    if (const int rc = check_pool(num_pages, 1)) return rc;
+    if (rows < 0 || width < 0 || width > INT32_MAX || rows > kMostElements / (width + 1)) return refuse("bad page tables");
+    if (rows > 1 && pages_stride < width) return refuse("the rows of a page table must not overlap");
+    if (rows == 0 || width == 0 || num_pages == 0) return done(hipSuccess, "");
+    if (!pages || !moved) return refuse("null device pointer");
+    return done(ngpu::launch_kv_move(pages, rows, width, pages_stride, moved, num_pages,
+                                     static_cast<hipStream_t>(hip_stream)), "move launch");
 }
 
 }  // extern "C"

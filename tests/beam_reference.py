@@ -1,0 +1,87 @@
+"""The beam search's operators from their definitions, one after the other, in plain Python and numpy."""
+
+import numpy as np
+
+
+def fork(pages, lengths, parents, refs, page, tokens):
+    """Rows, lengths, copies and counts after a fork; ``pages`` [G * W, width], ``parents`` and ``tokens`` [G, K]."""
+    (G, K), width, P = parents.shape, pages.shape[1], len(refs)
+    W, refs = len(pages) // G if G else 0, [int(r) for r in refs]
+
+    def count(row, by):
+        for p in row:
+            if 0 <= p < P:
+                refs[p] += by
+    rows, sizes, wants = [], [], []
+    for g in range(G):
+        for j in range(K):
+            w = int(parents[g, j])
+            live = 0 <= w < W
+            n = min(max(int(lengths[g * W + w]), 0), width * page) if live else None
+            rows.append([int(p) for p in pages[g * W + w, :-(-n // page)]] if live else [])
+            sizes.append(n)
+            wants.append(max(int(tokens[g, j]), 0))
+    for row in pages.tolist():
+        count(row, -1)
+    for row in rows:
+        count(row, 1)
+    free = [p for p in range(P) if refs[p] == 0]
+    after_step1 = list(refs)
+    decided, plans = {}, []
+    for i, (row, n, T) in enumerate(zip(rows, sizes, wants)):
+        if n is None or n + T > width * page:
+            plans.append((False, 0))
+            continue
+        shared = False
+        if T > 0 and n % page and 0 <= row[-1] < P:
+            key = i // K, row[-1]
+            shared = after_step1[row[-1]] - decided.get(key, 0) > 1
+            decided[key] = decided.get(key, 0) + 1
+        plans.append((shared, -(-(n + T) // page) - len(row) if T > 0 else 0))
+    taken, out, after, copies = 0, [], [], []
+    for row, n, T, (shared, more) in zip(rows, sizes, wants, plans):
+        need = int(shared) + more
+        mine = free[taken:taken + need]
+        taken += need
+        if n is not None and (n + T > width * page or need > 0 and taken > len(free)):
+            count(row, -1)
+            row, n, shared, mine = [], -1, False, []
+        copies.append((row[-1], mine[0], n % page) if shared else (-1, -1, 0))
+        if shared:
+            count(row[-1:], -1)
+            row = row[:-1]
+        count(mine, 1)
+        row = row + mine
+        out.append(row + [-1] * (width - len(row)))
+        after.append(n or 0)
+    i32 = np.int32
+    return (np.array(out, i32).reshape(G * K, width), np.array(after, i32), np.array(copies, i32).reshape(G * K, 3),
+            np.array(refs, i32))
+
+
+def compact(refs, page, tables):
+    """Copies, new numbers, counts and tables after a compaction."""
+    refs = [int(r) for r in refs]
+    P = len(refs)
+    used = [p for p in range(P) if refs[p]]
+    holes = [p for p in range(len(used)) if not refs[p]]
+    moved, copies = list(range(P)), []
+    for p in used[len(used) - len(holes):]:
+        moved[p] = holes[len(copies)]
+        copies.append((p, moved[p], page))
+    for p, to, _ in copies:
+        refs[to], refs[p] = refs[p], 0
+    copies += [(-1, -1, 0)] * (P // 2 - len(copies))
+    new = [np.array([moved[p] if 0 <= p < P else p for p in t.flatten().tolist()], np.int32).reshape(t.shape)
+           for t in tables]
+    return np.array(copies, np.int32).reshape(P // 2, 3), np.array(moved, np.int32), np.array(refs, np.int32), new
+
+
+def copy(cache, copies):
+    """A cache [pages, page size, ...] after the copies."""
+    out = cache.copy()
+    for src, dst, entries in np.asarray(copies).tolist():
+        if 0 <= src < len(cache) and 0 <= dst < len(cache) and src != dst:
+            n = min(max(entries, 0), cache.shape[1])
+            out[dst, :n] = cache[src, :n]
+    return out
