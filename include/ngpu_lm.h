@@ -422,6 +422,34 @@ size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_
 int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void *d_workspace,
                    size_t workspace_bytes, void *hip_stream);
 
+/* A paged cache in 8 bits.  An element is an e4m3 value (1 sign, 4 exponent and 3 mantissa bits, largest 448, no
+ * infinities) and stands for that times the scale of its block of tokens and its head: entry i of page p and head h has
+ * scale [p][i / block][h].  Scales are finite and positive. */
+typedef struct {
+    ngpu_kv_cache_t cache;         /* k and v: bytes, as strides are; dtype: NGPU_F16 or NGPU_BF16, the type of the queries,
+                                    * keys and values that go with it */
+    int32_t block;                 /* tokens a scale, divides page_size; at most NGPU_LM_MAX_SCALE_BLOCK */
+    float *k_scale, *v_scale;      /* [num_pages, page_size / block, heads] */
+    int64_t k_scale_stride_page, k_scale_stride_block, k_scale_stride_head;
+    int64_t v_scale_stride_page, v_scale_stride_block, v_scale_stride_head;
+} ngpu_kv_cache8_t;
+#define NGPU_LM_MAX_SCALE_BLOCK 65536
+
+/* ngpu_lm_kv_append for a cache in 8 bits.  The rotated keys, in fp32, and the values are rounded once to e4m3.  A block's
+ * scale for a head is the least power of two s (2^-100 at least) with 448 s no smaller than the new tokens' finite elements;
+ * a block whose entries before the first new one are kept (that one is not its entry 0) keeps its scale where that holds the
+ * new tokens, and else takes the new one, and the entries before are rounded again to it.  What lies behind the last
+ * new token of a block is no longer meaningful.  Elements that are not finite become NaN.  No two sequences of a call
+ * may append to one block. */
+int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *args, void *hip_stream);
+
+/* ngpu_lm_attend over a cache in 8 bits: keys and values are the elements times their scales, in fp32.
+ * The matrix cores take caches whose dim and strides are multiples of 16 elements, with k and v aligned to 16 bytes and out
+ * to 8, and whose pages span no more than 2^35 elements; an element kernel takes the others. */
+size_t ngpu_lm_attend8_workspace(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args);
+int ngpu_lm_attend8(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args, void *d_workspace,
+                    size_t workspace_bytes, void *hip_stream);
+
 /* ---------------------------------------------------------------------------
  * Beam search.  One step over a batch of utterances: ngpu_lm_beam_step selects
  * the best continuations of each utterance's hypotheses, ngpu_lm_kv_fork makes
@@ -509,6 +537,9 @@ int ngpu_lm_kv_fork(const ngpu_kv_fork_t *args, void *d_workspace, size_t worksp
  * are copied to page `to`; entries are clamped to the page, and rows with a page outside [0, num_pages) or from = to do
  * nothing.  No page may be the `to` of two rows, or one row's `to` and another's `from`. */
 int ngpu_lm_kv_copy(const ngpu_kv_cache_t *cache, const int32_t *copies, int64_t n, void *hip_stream);
+
+/* The same for a cache in 8 bits; all scales of the page are copied with the entries. */
+int ngpu_lm_kv_copy8(const ngpu_kv_cache8_t *cache, const int32_t *copies, int64_t n, void *hip_stream);
 
 /* Device memory a compaction needs, 16-byte aligned, not initialised. */
 size_t ngpu_lm_kv_compact_workspace(int64_t num_pages);

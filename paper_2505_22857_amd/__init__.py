@@ -41,8 +41,8 @@ EXPORTED = [
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
     "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
-    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy",
-    "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
+    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8",
+        "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
 ]
 

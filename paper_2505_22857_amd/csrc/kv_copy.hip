@@ -14,6 +14,7 @@ constexpr int kCopyThreads = 256;
 
 struct Copy {
     ngpu_kv_cache_t c;     // dim and strides in units
+    ngpu_kv_cache8_t s;    // its scales; block 0: it has none
     const int32_t *copies;
     int64_t n;
     int slices;            // workgroups a page's keys (or values)
@@ -28,6 +29,17 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(Copy p, int64_t w0) 
     const int32_t *copy = p.copies + 3 * row;
     const int32_t from = copy[0], to = copy[1], entries = min(copy[2], p.c.page_size);
     if (from < 0 || from >= p.c.num_pages || to < 0 || to >= p.c.num_pages || from == to || entries <= 0) return;
+    if (p.s.block > 0 && slice == 0) {
+        float *const scale = values ? p.s.v_scale : p.s.k_scale;
+        const int64_t sp = values ? p.s.v_scale_stride_page : p.s.k_scale_stride_page;
+        const int64_t sb = values ? p.s.v_scale_stride_block : p.s.k_scale_stride_block;
+        const int64_t sh = values ? p.s.v_scale_stride_head : p.s.k_scale_stride_head;
+        const int64_t blocks = p.c.page_size / p.s.block;
+        for (int64_t i = threadIdx.x; i < blocks * p.c.heads; i += kCopyThreads) {
+            const int64_t at = i / p.c.heads * sb + i % p.c.heads * sh;
+            scale[to * sp + at] = scale[from * sp + at];
+        }
+    }
     const int64_t page = values ? p.c.v_stride_page : p.c.k_stride_page;
     const int64_t token = values ? p.c.v_stride_token : p.c.k_stride_token;
     const int64_t head = values ? p.c.v_stride_head : p.c.k_stride_head;
@@ -65,14 +77,23 @@ static hipError_t launch(Copy p, int64_t size, hipStream_t stream) {   // size: 
     return hipSuccess;
 }
 
-hipError_t launch_kv_copy(const ngpu_kv_cache_t &c, const int32_t *copies, int64_t n, hipStream_t stream) {
-    const Copy p{c, copies, n, 1};
-    constexpr int64_t size = 2, per = 16 / size;
+// size: bytes of an element
+static hipError_t launch_all(const Copy &p, int64_t size, hipStream_t stream) {
+    const ngpu_kv_cache_t &c = p.c;
+    const int64_t per = 16 / size;
     bool wide = c.dim % per == 0 && reinterpret_cast<uintptr_t>(c.k) % 16 == 0 && reinterpret_cast<uintptr_t>(c.v) % 16 == 0;
     for (const int64_t s : {c.k_stride_page, c.k_stride_token, c.k_stride_head, c.v_stride_page, c.v_stride_token,
                             c.v_stride_head})
         wide = wide && s % per == 0;
-    return wide ? launch<i32x4>(p, size, stream) : launch<uint16_t>(p, size, stream);
+    if (wide) return launch<i32x4>(p, size, stream);
+    return size == 1 ? launch<uint8_t>(p, size, stream) : launch<uint16_t>(p, size, stream);
+}
+
+hipError_t launch_kv_copy(const ngpu_kv_cache_t &c, const int32_t *copies, int64_t n, hipStream_t stream) {
+    return launch_all(Copy{c, {}, copies, n, 1}, 2, stream);
+}
+hipError_t launch_kv_copy8(const ngpu_kv_cache8_t &c, const int32_t *copies, int64_t n, hipStream_t stream) {
+    return launch_all(Copy{c.cache, c, copies, n, 1}, 1, stream);
 }
 
 }  // namespace ngpu

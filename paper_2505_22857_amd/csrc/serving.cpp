@@ -14,6 +14,8 @@ hipError_t launch_verify(const ngpu_verify_t &a, void *workspace, hipStream_t st
 hipError_t launch_kv_append(const ngpu_kv_cache_t &c, const ngpu_kv_append_t &a, hipStream_t stream);
 size_t attend_workspace(const ngpu_kv_cache_t &c, const ngpu_attend_t &a);
 hipError_t launch_attend(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, void *workspace, hipStream_t stream);
+hipError_t launch_kv_append8(const ngpu_kv_cache8_t &c, const ngpu_kv_append_t &a, hipStream_t stream);
+hipError_t launch_kv_copy8(const ngpu_kv_cache8_t &c, const int32_t *copies, int64_t n, hipStream_t stream);
 size_t kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages);
 hipError_t launch_kv_fork(const ngpu_kv_fork_t &a, void *workspace, hipStream_t stream);
 hipError_t launch_kv_copy(const ngpu_kv_cache_t &c, const int32_t *copies, int64_t n, hipStream_t stream);
@@ -80,12 +82,50 @@ int check_cache(const ngpu_kv_cache_t *c) {
     return NGPU_OK;
 }
 
+int check_cache8(const ngpu_kv_cache8_t *c) {
+    if (!c) return refuse("null argument");
+    if (const int rc = check_cache(&c->cache)) return rc;
+    if (c->block < 1 || c->block > NGPU_LM_MAX_SCALE_BLOCK || c->cache.page_size % c->block != 0)
+        return refuse("block = %d must lie in [1, %d] and divide a page of %d tokens", c->block, NGPU_LM_MAX_SCALE_BLOCK,
+                      c->cache.page_size);
+    if (c->k_scale_stride_page < 0 || c->k_scale_stride_block < 0 || c->k_scale_stride_head < 0 ||
+        c->v_scale_stride_page < 0 || c->v_scale_stride_block < 0 || c->v_scale_stride_head < 0)
+        return refuse("negative strides of the scales");
+    if (c->cache.num_pages > 0 && (!c->k_scale || !c->v_scale)) return refuse("null device pointer of the scales");
+    return NGPU_OK;
+}
+
 int check_rows(int64_t S, int64_t T, int64_t heads, int64_t dim) {
     if (S < 0 || S > NGPU_LM_MAX_SEQUENCES) return refuse("S = %lld outside [0, %d]", (long long)S,
                                                           NGPU_LM_MAX_SEQUENCES);
     if (T < 0 || T > INT32_MAX) return refuse("T = %lld outside [0, 2^31 - 1]", (long long)T);
     if (heads < 0 || heads > 65536) return refuse("q_heads = %lld out of range", (long long)heads);
     if (S > 0 && T > 0 && S * T > kMostElements / (heads + 1) / dim) return refuse("the call is too large");
+    return NGPU_OK;
+}
+
+// `a`: the arguments as the kernels take them; `empty`: there is nothing to append.
+int check_append(const ngpu_kv_cache_t &c, const ngpu_kv_append_t *args, ngpu_kv_append_t &a, bool &empty) {
+    if (!args) return refuse("null argument");
+    a = *args;
+    if (!a.q) a.q_heads = 0;
+    if (const int rc = check_rows(a.S, a.T, int64_t(a.q_heads) + 2 * c.heads, c.dim)) return rc;
+    if (a.q && a.q_heads < 1) return refuse("q_heads = %d must be positive", a.q_heads);
+    if (a.k_stride_seq < 0 || a.k_stride_token < 0 || a.k_stride_head < 0 || a.v_stride_seq < 0 ||
+        a.v_stride_token < 0 || a.v_stride_head < 0 ||
+        (a.q && (a.q_stride_seq < 0 || a.q_stride_token < 0 || a.q_stride_head < 0)))
+        return refuse("negative strides");
+    if (a.pages_width < 0 || a.pages_width > INT32_MAX || a.pages_stride < 0) return refuse("bad page tables");
+    if (a.rotary < 0 || a.rotary > c.dim || a.rotary % 2 != 0)
+        return refuse("rotary = %d must be even and lie in [0, %d]", a.rotary, c.dim);
+    if (a.layout != NGPU_ROPE_HALF && a.layout != NGPU_ROPE_INTERLEAVED)
+        return refuse("unknown rotation layout %d", a.layout);
+    empty = a.S == 0 || a.T == 0;
+    if (empty) return NGPU_OK;
+    if (!a.k || !a.v || !a.start || (!a.pages && a.pages_width > 0) || (a.q && !a.q_out) ||
+        (a.rotary > 0 && a.positions_count > 0 && (!a.cos || !a.sin)))
+        return refuse("null device pointer");
+    if (a.q && a.q_out == a.q) return refuse("q_out must not overlap q");
     return NGPU_OK;
 }
 
@@ -156,26 +196,20 @@ int ngpu_lm_verify(const ngpu_verify_t *args, void *d_workspace, size_t workspac
 
 int ngpu_lm_kv_append(const ngpu_kv_cache_t *cache, const ngpu_kv_append_t *args, void *hip_stream) {
     if (const int rc = check_cache(cache)) return rc;
-    if (!args) return refuse("null argument");
-    ngpu_kv_append_t a = *args;
-    if (!a.q) a.q_heads = 0;
-    if (const int rc = check_rows(a.S, a.T, int64_t(a.q_heads) + 2 * cache->heads, cache->dim)) return rc;
-    if (a.q && a.q_heads < 1) return refuse("q_heads = %d must be positive", a.q_heads);
-    if (a.k_stride_seq < 0 || a.k_stride_token < 0 || a.k_stride_head < 0 || a.v_stride_seq < 0 ||
-        a.v_stride_token < 0 || a.v_stride_head < 0 ||
-        (a.q && (a.q_stride_seq < 0 || a.q_stride_token < 0 || a.q_stride_head < 0)))
-        return refuse("negative strides");
-    if (a.pages_width < 0 || a.pages_width > INT32_MAX || a.pages_stride < 0) return refuse("bad page tables");
-    if (a.rotary < 0 || a.rotary > cache->dim || a.rotary % 2 != 0)
-        return refuse("rotary = %d must be even and lie in [0, %d]", a.rotary, cache->dim);
-    if (a.layout != NGPU_ROPE_HALF && a.layout != NGPU_ROPE_INTERLEAVED)
-        return refuse("unknown rotation layout %d", a.layout);
-    if (a.S == 0 || a.T == 0) return done(hipSuccess, "");
-    if (!a.k || !a.v || !a.start || (!a.pages && a.pages_width > 0) || (a.q && !a.q_out) ||
-        (a.rotary > 0 && a.positions_count > 0 && (!a.cos || !a.sin)))
-        return refuse("null device pointer");
-    if (a.q && a.q_out == a.q) return refuse("q_out must not overlap q");
+    ngpu_kv_append_t a;
+    bool empty;
+    if (const int rc = check_append(*cache, args, a, empty)) return rc;
+    if (empty) return done(hipSuccess, "");
     return done(ngpu::launch_kv_append(*cache, a, static_cast<hipStream_t>(hip_stream)), "append launch");
+}
+
+int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *args, void *hip_stream) {
+    if (const int rc = check_cache8(cache)) return rc;
+    ngpu_kv_append_t a;
+    bool empty;
+    if (const int rc = check_append(cache->cache, args, a, empty)) return rc;
+    if (empty) return done(hipSuccess, "");
+    return done(ngpu::launch_kv_append8(*cache, a, static_cast<hipStream_t>(hip_stream)), "append launch");
 }
 
 size_t ngpu_lm_attend_workspace(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args) {
@@ -221,6 +255,14 @@ int ngpu_lm_kv_copy(const ngpu_kv_cache_t *cache, const int32_t *copies, int64_t
     if (n == 0 || cache->num_pages == 0) return done(hipSuccess, "");
     if (!copies) return refuse("null device pointer");
     return done(ngpu::launch_kv_copy(*cache, copies, n, static_cast<hipStream_t>(hip_stream)), "copy launch");
+}
+
+int ngpu_lm_kv_copy8(const ngpu_kv_cache8_t *cache, const int32_t *copies, int64_t n, void *hip_stream) {
+    if (const int rc = check_cache8(cache)) return rc;
+    if (n < 0 || n > NGPU_LM_MAX_PAGES) return refuse("n = %lld out of range", (long long)n);
+    if (n == 0 || cache->cache.num_pages == 0) return done(hipSuccess, "");
+    if (!copies) return refuse("null device pointer");
+    return done(ngpu::launch_kv_copy8(*cache, copies, n, static_cast<hipStream_t>(hip_stream)), "copy launch");
 }
 
 size_t ngpu_lm_kv_compact_workspace(int64_t num_pages) {

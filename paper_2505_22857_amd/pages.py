@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes
 
 from . import _check, _torch_mod, load_library
-from .serving import _cache, _Cache, _device_of, _need, _on, _table, _untracked
+from .serving import _cache, _Cache, _cache8, _Cache8, _device_of, _need, _on, _table, _untracked
 
 MAX_FORK = 4096                  # NGPU_LM_MAX_FORK
 MAX_PAGES = 1 << 28              # NGPU_LM_MAX_PAGES
@@ -40,6 +40,7 @@ def _library():
         lib.ngpu_lm_kv_fork_workspace.restype = ctypes.c_size_t
         lib.ngpu_lm_kv_fork.argtypes = [p(_Fork), _vp, ctypes.c_size_t, _vp]
         lib.ngpu_lm_kv_copy.argtypes = [p(_Cache), _vp, _i64, _vp]
+        lib.ngpu_lm_kv_copy8.argtypes = [p(_Cache8), _vp, _i64, _vp]
         lib.ngpu_lm_kv_compact_workspace.argtypes = [_i64]
         lib.ngpu_lm_kv_compact_workspace.restype = ctypes.c_size_t
         lib.ngpu_lm_kv_compact.argtypes = [_vp, _i64, _i32, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -102,19 +103,22 @@ def kv_fork(pages, lengths, parents, refs, page_size: int, tokens=0, stream=None
     return new, after, copies
 
 
-def kv_copy(k_cache, v_cache, copies, stream=None):
+def kv_copy(k_cache, v_cache, copies, k_scale=None, v_scale=None, stream=None):
     """Copy entries of pages to other pages of a cache [pages, page size, heads, dim], in place.
 
     ``copies`` [n, 3] int32 of ``kv_fork`` or ``kv_compact``: {from, to, entries} a row; rows with a page outside
-    the cache are skipped.  No page may be written by two rows, or written by one and read by another."""
+    the cache are skipped.  No page may be written by two rows, or written by one and read by another.  Of an
+    8-bit cache all scales of a page, ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32, go with it."""
     torch = _torch_mod()
-    dev, cache = _cache(k_cache, v_cache)
+    eight = k_scale is not None or v_scale is not None
+    dev, cache = _cache8(k_cache, v_cache, k_scale, v_scale, torch.float16) if eight else _cache(k_cache, v_cache)
     if copies.dim() != 2:
         raise ValueError("copies must be a [n, 3] tensor")
     at = _need(copies, "copies", dev, torch.int32, (copies.shape[0], 3))
-    _untracked(k_cache=k_cache, v_cache=v_cache)
+    _untracked(k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
+    lib = _library()
     with _on(dev, stream) as handle:
-        _check(_library().ngpu_lm_kv_copy(ctypes.byref(cache), at, copies.shape[0], handle))
+        _check((lib.ngpu_lm_kv_copy8 if eight else lib.ngpu_lm_kv_copy)(ctypes.byref(cache), at, copies.shape[0], handle))
 
 
 def kv_compact(refs, page_size: int, tables=(), stream=None):

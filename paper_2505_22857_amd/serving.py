@@ -40,6 +40,12 @@ class _Cache(ctypes.Structure):
                 ("v_stride_page", _i64), ("v_stride_token", _i64), ("v_stride_head", _i64)]
 
 
+class _Cache8(ctypes.Structure):
+    _fields_ = [("cache", _Cache), ("block", _i32), ("k_scale", _vp), ("v_scale", _vp), ("k_scale_stride_page", _i64),
+                ("k_scale_stride_block", _i64), ("k_scale_stride_head", _i64), ("v_scale_stride_page", _i64),
+                ("v_scale_stride_block", _i64), ("v_scale_stride_head", _i64)]
+
+
 class _Append(ctypes.Structure):
     _fields_ = [("S", _i64), ("T", _i64), ("k", _vp), ("v", _vp), ("k_stride_seq", _i64), ("k_stride_token", _i64),
                 ("k_stride_head", _i64), ("v_stride_seq", _i64), ("v_stride_token", _i64), ("v_stride_head", _i64),
@@ -69,6 +75,7 @@ def _library():
         lib.ngpu_lm_verify_workspace.restype = ctypes.c_size_t
         lib.ngpu_lm_verify.argtypes = [p(_Verify), _vp, ctypes.c_size_t, _vp]
         lib.ngpu_lm_kv_append.argtypes = [p(_Cache), p(_Append), _vp]
+        lib.ngpu_lm_kv_append8.argtypes = [p(_Cache8), p(_Append), _vp]
         lib.ngpu_lm_attend_workspace.argtypes = [p(_Cache), p(_Attend)]
         lib.ngpu_lm_attend_workspace.restype = ctypes.c_size_t
         lib.ngpu_lm_attend.argtypes = [p(_Cache), p(_Attend), _vp, ctypes.c_size_t, _vp]
@@ -205,14 +212,41 @@ def _cache(k_cache, v_cache):
     dev = _device_of(k_cache, "k_cache")
     code = _type_code(k_cache.dtype)
     if code not in (NGPU_F16, NGPU_BF16):
-        raise TypeError("the cache must be float16 or bfloat16")
+        raise TypeError("the cache must be float16 or bfloat16, or float8_e4m3fn with scales")
+    return dev, _layout(k_cache, v_cache, dev, code)
+
+
+def _layout(k_cache, v_cache, dev, code):
     if k_cache.dim() != 4:
         raise ValueError("the cache must be a [pages, page size, heads, dim] tensor")
     pages, page_size, heads, dim = k_cache.shape
-    return dev, _Cache(code, heads, dim, page_size, pages,
-                       _need(k_cache, "k_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
-                       _need(v_cache, "v_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
-                       *k_cache.stride()[:3], *v_cache.stride()[:3])
+    return _Cache(code, heads, dim, page_size, pages,
+                  _need(k_cache, "k_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
+                  _need(v_cache, "v_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
+                  *k_cache.stride()[:3], *v_cache.stride()[:3])
+
+
+def _cache8(k_cache, v_cache, k_scale, v_scale, dtype):
+    """A cache in 8 bits, with queries, keys and values of ``dtype``."""
+    torch = _torch_mod()
+    dev, code = _device_of(k_cache, "k_cache"), _type_code(dtype)
+    if k_cache.dtype is not torch.float8_e4m3fn:
+        raise TypeError("a cache with scales must be float8_e4m3fn")
+    if code not in (NGPU_F16, NGPU_BF16):
+        raise TypeError("an 8-bit cache goes with float16 or bfloat16")
+    if k_scale is None or v_scale is None:
+        raise ValueError("k_scale and v_scale come together")
+    c = _layout(k_cache, v_cache, dev, code)
+    if k_scale.dim() != 3 or k_scale.shape[1] < 1 or c.page_size % k_scale.shape[1] != 0:
+        raise ValueError("the scales must be [pages, blocks of a page, heads] tensors whose blocks divide a page")
+    shape = (c.num_pages, k_scale.shape[1], c.heads)
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if not hasattr(t, "is_cuda") or t.device != dev or t.dtype is not torch.float32:
+            raise TypeError(f"{name} must be a torch.float32 tensor on {dev}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    return dev, _Cache8(c, c.page_size // k_scale.shape[1], k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride(),
+                        *v_scale.stride())
 
 
 def _table(t, name, dev, rows):
@@ -223,7 +257,7 @@ def _table(t, name, dev, rows):
 
 
 def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, sin=None,
-              layout: int = NGPU_ROPE_HALF, q=None, lengths=None, stream=None):
+              layout: int = NGPU_ROPE_HALF, q=None, lengths=None, k_scale=None, v_scale=None, stream=None):
     """Store new keys and values in a paged cache, rotating keys and queries on the way.
 
     ``k``, ``v`` [S, T, heads, dim] go to places ``start[s] + t`` of the sequences' own tokens, entry
@@ -231,20 +265,28 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
     page size, heads, dim]; only the first ``lengths[s]`` of a sequence's T tokens count.  With ``cos`` and
     ``sin`` [positions, rotary / 2] (``rope_table``) the first ``rotary`` dimensions of the keys, and of
     ``q`` [S, T, q heads, dim], are rotated by row ``positions[s, t]`` (without it: the token's place).
+
+    With ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32 the caches are float8_e4m3fn, a value being the
+    element times the scale of its block of page size / blocks tokens and its head.  A block's scale is the least power of
+    two that holds its tokens; where tokens before the new ones are in the block it grows when it has to, and they
+    are rounded again; entries behind the new ones are not kept.  No two sequences may append to one block.
     Returns the rotated queries (zero where a token does not count), None without ``q``."""
     native = _native()
-    if stream is None and native:
+    eight = k_scale is not None or v_scale is not None
+    if stream is None and native and not eight:
         r = native.kv_append(k, v, k_cache, v_cache, pages, start, positions, cos, sin, layout, q, lengths)
         if r is not None:
             if r.__class__ is int:
                 _check(r)
             return r if q is not None else None
     torch = _torch_mod()
-    dev, cache = _cache(k_cache, v_cache)
+    dt, i32 = k.dtype if eight else k_cache.dtype, torch.int32
+    dev, whole = _cache8(k_cache, v_cache, k_scale, v_scale, dt) if eight else _cache(k_cache, v_cache)
+    cache = whole.cache if eight else whole
     if k.dim() != 4:
         raise ValueError("k must be a [S, T, heads, dim] tensor")
     S, T = k.shape[:2]
-    shape, dt, i32 = (S, T, cache.heads, cache.dim), k_cache.dtype, torch.int32
+    shape = (S, T, cache.heads, cache.dim)
     a = _Append(S, T, _need(k, "k", dev, dt, shape, rows=True), _need(v, "v", dev, dt, shape, rows=True),
                 *k.stride()[:3], *v.stride()[:3])
     a.pages, a.pages_width, a.pages_stride = _table(pages, "pages", dev, S)
@@ -266,11 +308,12 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
         a.q_heads = q.shape[2]
         a.q = _need(q, "q", dev, dt, (S, T, q.shape[2], cache.dim), rows=True)
         a.q_stride_seq, a.q_stride_token, a.q_stride_head = q.stride()[:3]
-    _untracked(k=k, v=v, k_cache=k_cache, v_cache=v_cache, q=q, cos=cos, sin=sin)
+    _untracked(k=k, v=v, k_cache=k_cache, v_cache=v_cache, q=q, cos=cos, sin=sin, k_scale=k_scale, v_scale=v_scale)
     with _on(dev, stream) as handle:
         out = torch.empty(q.shape, dtype=dt, device=dev) if q is not None else None
         a.q_out = out.data_ptr() if out is not None else None
-        _check(_library().ngpu_lm_kv_append(ctypes.byref(cache), ctypes.byref(a), handle))
+        lib = _library()
+        _check((lib.ngpu_lm_kv_append8 if eight else lib.ngpu_lm_kv_append)(ctypes.byref(whole), ctypes.byref(a), handle))
     return out
 
 

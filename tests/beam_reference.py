@@ -85,3 +85,65 @@ def copy(cache, copies):
             n = min(max(entries, 0), cache.shape[1])
             out[dst, :n] = cache[src, :n]
     return out
+
+
+def e4m3_values():
+    """The value of each byte: sign, 4 bits of exponent (bias 7), 3 of mantissa, 0x7f and 0xff no number."""
+    b = np.arange(256)
+    e, m = b >> 3 & 15, b & 7
+    x = np.where(e == 0, m / 8 * 2.0 ** -6, (1 + m / 8) * 2.0 ** (e.astype(float) - 7))
+    x[b & 0x7f == 0x7f] = np.nan
+    return np.where(b & 0x80, -x, x)
+
+
+_LEVELS = e4m3_values()[:127]
+
+
+def to_e4m3(x):
+    """The nearest e4m3 value of each |x| <= 464, of two the one with an even mantissa; no number for what is not finite."""
+    with np.errstate(invalid="ignore"):
+        a = np.abs(x)
+        hi = np.clip(np.searchsorted(_LEVELS, a), 1, 126)
+        lo = hi - 1
+        below, above = a - _LEVELS[lo], _LEVELS[hi] - a
+        pick = np.where((above < below) | ((above == below) & (hi % 2 == 0)), hi, lo)
+        return np.where(np.isfinite(x), np.copysign(_LEVELS[pick], x), np.nan)
+
+
+def append8(x, cache, scale, pages, start, counts):
+    """``cache`` [pages, page, heads, dim] of e4m3 values and ``scale`` [pages, blocks, heads] after x [S, T, heads, dim]
+    in fp32; and which entries are new or kept."""
+    cache, scale = cache.copy(), scale.copy()
+    P, page, H, D = cache.shape
+    block = page // scale.shape[1]
+    known = np.zeros(cache.shape[:2], bool)
+    for s in range(len(x)):
+        groups = {}
+        for t in range(counts[s]):
+            place = int(start[s]) + t
+            if 0 <= place < pages.shape[1] * page and 0 <= pages[s, place // page] < P:
+                groups.setdefault((place // block, int(pages[s, place // page])), []).append((place, t))
+        for (b, p), new in groups.items():
+            at = b * block % page // block
+            lead = new[0][0] % block
+            first = b * block % page
+            for h in range(H):
+                y = x[s, [t for _, t in new], h].astype(np.float32)
+                most = np.where(np.isfinite(y), np.abs(y), 0).max()
+                e = -100
+                while np.float64(most) > 448 * 2.0 ** e:
+                    e += 1
+                now = np.float32(2.0 ** e)
+                if lead:
+                    old = scale[p, at, h]
+                    old = old if 2.0 ** -100 <= old < np.inf else np.float32(2.0 ** -100)
+                    if most > np.float32(448) * old:
+                        ratio = np.float32(old) / now
+                        cache[p, first:first + lead, h] = to_e4m3(cache[p, first:first + lead, h].astype(np.float32) * ratio)
+                    else:
+                        now = old
+                scale[p, at, h] = now
+                with np.errstate(invalid="ignore"):
+                    cache[p, first + lead:first + lead + len(new), h] = to_e4m3(y * (np.float32(1) / now))
+            known[p, first:first + lead + len(new)] = True
+    return cache, scale, known

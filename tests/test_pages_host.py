@@ -27,7 +27,7 @@ def error():
 def test_structures_match_the_header(tmp_path):
     if shutil.which("gcc") is None:
         pytest.skip("gcc is not available")
-    names = {"ngpu_kv_fork_t": pages._Fork}
+    names = {"ngpu_kv_fork_t": pages._Fork, "ngpu_kv_cache8_t": serving._Cache8}
     lines = ["#include <stdio.h>", '#include "ngpu_lm.h"', "int main(void) {"]
     for name, cls in names.items():
         lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
@@ -81,6 +81,41 @@ def test_copy_refuses(lib):
     assert lib.ngpu_lm_kv_copy(ctypes.byref(cache), None, 0, None) == 0
     cache.dtype = 0
     assert lib.ngpu_lm_kv_copy(ctypes.byref(cache), 64, 1, None) == INVALID
+
+
+def ok_cache8(**kw):
+    a = dict(cache=serving._Cache(1, 2, 64, 16, 10, 64, 64, 2048, 128, 64, 2048, 128, 64), block=8, k_scale=64, v_scale=64,
+             k_scale_stride_page=4, k_scale_stride_block=2, k_scale_stride_head=1, v_scale_stride_page=4,
+             v_scale_stride_block=2, v_scale_stride_head=1)
+    return serving._Cache8(**{**a, **kw})
+
+
+@pytest.mark.parametrize("change", [
+    dict(block=0), dict(block=-8), dict(block=5), dict(block=32), dict(k_scale=None), dict(v_scale=None),
+    dict(k_scale_stride_page=-1), dict(k_scale_stride_block=-1), dict(k_scale_stride_head=-1), dict(v_scale_stride_page=-1),
+    dict(v_scale_stride_block=-1), dict(v_scale_stride_head=-1),
+    dict(cache=serving._Cache(0, 2, 64, 16, 10, 64, 64, 2048, 128, 64, 2048, 128, 64)),
+    dict(cache=serving._Cache(1, 2, 257, 16, 10, 64, 64, 2048, 128, 64, 2048, 128, 64)),
+    dict(cache=serving._Cache(1, 1, 1, 1 << 20, 1, 64, 64, 1, 1, 1, 1, 1, 1), block=1 << 20)])
+def test_bad_caches_of_8_bits_are_refused(lib, change):
+    from test_serving_host import ok_append
+    c = ok_cache8(**change)
+    lib8 = serving._library()
+    assert lib8.ngpu_lm_kv_append8(ctypes.byref(c), ctypes.byref(ok_append()), None) == INVALID and error()
+    assert lib.ngpu_lm_kv_copy8(ctypes.byref(c), 64, 1, None) == INVALID and error()
+
+
+def test_append8_and_copy8_refuse(lib):
+    from test_serving_host import ok_append
+    lib8, c = serving._library(), ok_cache8()
+    assert lib8.ngpu_lm_kv_append8(None, ctypes.byref(ok_append()), None) == INVALID
+    assert lib8.ngpu_lm_kv_append8(ctypes.byref(c), None, None) == INVALID
+    for change in (dict(k=None), dict(start=None), dict(rotary=66), dict(layout=2), dict(q=64, q_heads=2, q_out=64)):
+        assert lib8.ngpu_lm_kv_append8(ctypes.byref(c), ctypes.byref(ok_append(**change)), None) == INVALID
+    assert lib8.ngpu_lm_kv_append8(ctypes.byref(c), ctypes.byref(ok_append(T=0)), None) == 0
+    assert lib.ngpu_lm_kv_copy8(None, 64, 1, None) == INVALID
+    assert lib.ngpu_lm_kv_copy8(ctypes.byref(c), None, 1, None) == INVALID
+    assert lib.ngpu_lm_kv_copy8(ctypes.byref(c), None, 0, None) == 0
 
 
 def test_compact_refuses(lib):
