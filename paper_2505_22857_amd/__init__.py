@@ -27,6 +27,7 @@ NGPU_BUILD_REPAIR_CLOSURE = 2
 MAX_ORDER = 10
 MAX_VOCAB = 8192
 MAX_BATCH = (1 << 26) - 256      # NGPU_LM_MAX_BATCH
+MAX_BEAMS = 64                   # NGPU_LM_MAX_BEAMS
 
 ERROR_NAMES = {
     -1: "INVALID_ARG", -2: "TOKEN_RANGE", -3: "ORDER_RANGE", -4: "DUPLICATE_NGRAM",
@@ -41,7 +42,8 @@ EXPORTED = [
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
     "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
-    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8",
+    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8", "ngpu_lm_beam_step_workspace",
+    "ngpu_lm_beam_step",
         "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
 ]
@@ -57,6 +59,14 @@ class _NgramList(ctypes.Structure):
     _fields_ = [("num_ngrams", ctypes.c_int64), ("max_order", ctypes.c_int32),
                 ("order", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
                 ("logprob", ctypes.c_void_p), ("backoff", ctypes.c_void_p)]
+
+
+class _BeamStep(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("W", ctypes.c_int32), ("k", ctypes.c_int32), ("mode", ctypes.c_int32),
+                ("lam", ctypes.c_float), ("asr", ctypes.c_void_p), ("asr_stride_b", ctypes.c_int64),
+                ("asr_stride_w", ctypes.c_int64), ("states", ctypes.c_void_p), ("scores", ctypes.c_void_p),
+                ("last", ctypes.c_void_p), ("out_tokens", ctypes.c_void_p), ("out_parents", ctypes.c_void_p),
+                ("out_scores", ctypes.c_void_p), ("out_states", ctypes.c_void_p)]
 
 
 class _Info(ctypes.Structure):
@@ -95,6 +105,9 @@ def load_library(path: str = LIB_PATH):
     lib.ngpu_lm_final_weights.argtypes = [vp, vp, i64, vp, vp]
     lib.ngpu_lm_fused_topk.argtypes = [vp, vp, i64, i64, ctypes.c_float, i32, vp, vp, vp, vp, vp]
     lib.ngpu_lm_draft.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, i64, i64, vp, vp, vp, vp]
+    lib.ngpu_lm_beam_step_workspace.argtypes = [i64, i32, i32]
+    lib.ngpu_lm_beam_step_workspace.restype = ctypes.c_size_t
+    lib.ngpu_lm_beam_step.argtypes = [vp, ctypes.POINTER(_BeamStep), vp, ctypes.c_size_t, vp]
     lib.ngpu_lm_check_states.argtypes = [vp, vp, ctypes.POINTER(i64)]
     lib.ngpu_lm_sync_check.argtypes = [vp, vp]
     lib.ngpu_lm_query_bytes.argtypes = [vp, vp, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
@@ -109,7 +122,7 @@ def load_library(path: str = LIB_PATH):
     for name in EXPORTED:
         if name not in ("ngpu_lm_free", "ngpu_lm_device_bytes", "ngpu_lm_last_error", "ngpu_arpa_free",
                         "ngpu_lm_verify_workspace", "ngpu_lm_attend_workspace", "ngpu_lm_kv_fork_workspace",
-                        "ngpu_lm_kv_compact_workspace"):
+                        "ngpu_lm_kv_compact_workspace", "ngpu_lm_beam_step_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -455,6 +468,47 @@ class NgpuLM:
                                            rows.data_ptr() if sample else None, handle))
         return tokens, after, rows
 
+    def beam_step(self, asr, lam: float, states, scores, k: Optional[int] = None, last=None,
+                  mode: int = NGPU_FUSION_PLAIN, stream=None):
+        """The ``k`` best continuations of each utterance's hypotheses, over all of them and the whole vocabulary.
+
+        ``asr`` [B, W, C] float32: log-probabilities of the classes after each of W hypotheses (an expanded tensor where
+        they share one frame); ``states`` [B, W] int32; ``scores`` [B, W] float32: their sums so far, -inf for none.
+        The sums score + asr + ``lam`` * lm are ordered; ``k`` is W unless given.  Class V is <eos> in AED mode, with
+        the state's final weight, and blank in transducer mode, which the model does not weigh; both keep the state.  In
+        AED mode ``last`` [B, W] int32 are the hypotheses' last classes: one whose last is V has ended and goes on as it is.
+
+        Returns (classes, parents among the W, scores, states), [B, k] each, in descending order (ties to the lowest parent,
+        then class); what is left over has class and parent -1, score -inf and state 0.  The parents are
+        ``kv_fork``'s; the classes the next step's ``last``."""
+        import torch
+        from .serving import _need, _on
+        if not hasattr(asr, "is_cuda") or not asr.is_cuda or asr.dtype is not torch.float32:
+            raise TypeError("asr must be a float32 device tensor")
+        if asr.dim() != 3:
+            raise ValueError("asr must be a [B, W, classes] tensor")
+        B, W, C = asr.shape
+        if C < self._classes(mode):
+            raise ValueError(f"asr rows must hold {self._classes(mode)} classes for mode {mode}")
+        if C > 1 and asr.stride(2) != 1 and asr.numel() > 0:
+            raise TypeError("asr must have unit stride in the last dimension")
+        dev, k = asr.device, W if k is None else int(k)
+        if not 1 <= W <= MAX_BEAMS or not 1 <= k <= MAX_BEAMS:
+            raise ValueError(f"hypotheses before and after a step must lie in [1, {MAX_BEAMS}]")
+        a = _BeamStep(B, W, k, int(mode), float(lam), asr.data_ptr(), asr.stride(0), asr.stride(1),
+                      _need(states, "states", dev, torch.int32, (B, W)),
+                      _need(scores, "scores", dev, torch.float32, (B, W)),
+                      _need(last, "last", dev, torch.int32, (B, W)))
+        with _on(dev, stream) as handle:
+            tokens, parents, after = (torch.empty((B, k), dtype=torch.int32, device=dev) for _ in range(3))
+            best = torch.empty((B, k), dtype=torch.float32, device=dev)
+            size = self._lib.ngpu_lm_beam_step_workspace(B, W, k)
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+            a.out_tokens, a.out_parents = tokens.data_ptr(), parents.data_ptr()
+            a.out_scores, a.out_states = best.data_ptr(), after.data_ptr()
+            _check(self._lib.ngpu_lm_beam_step(self._h, ctypes.byref(a), workspace.data_ptr(), size, handle))
+        return tokens, parents, best, after
+
     def check_states(self, stream=None) -> int:
         n = ctypes.c_int64()
         rc = self._lib.ngpu_lm_check_states(self._h, _stream_handle(stream), ctypes.byref(n))
@@ -485,7 +539,7 @@ from .serving import (MAX_DRAFT, MAX_HEAD_DIM, NGPU_BF16, NGPU_F16, NGPU_F32, NG
                       NGPU_ROPE_INTERLEAVED, attend, kv_append, rope_table, verify)
 from .pages import MAX_FORK, MAX_PAGES, kv_compact, kv_copy, kv_fork  # noqa: E402
 
-__all__ = ["verify", "kv_append", "attend", "kv_fork", "kv_copy", "kv_compact", "MAX_FORK", "MAX_PAGES", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
+__all__ = ["MAX_BEAMS", "verify", "kv_append", "attend", "kv_fork", "kv_copy", "kv_compact", "MAX_FORK", "MAX_PAGES", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
            "NGPU_BF16", "NGPU_ROPE_HALF", "NGPU_ROPE_INTERLEAVED", "NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED", "NGPU_BUILD_BOS_EOS",
            "NGPU_BUILD_REPAIR_CLOSURE",
            "NGPU_FUSION_PLAIN", "NGPU_FUSION_CTC", "NGPU_FUSION_TRANSDUCER", "NGPU_FUSION_AED"]

@@ -24,6 +24,8 @@ hipError_t launch_fused_topk(const DevTrie &t, const float *asr, int64_t B, int6
 hipError_t launch_draft(const DevTrie &t, const int32_t *states, const int32_t *last, int64_t B, int K,
                         float temperature, const float *noise, int64_t noise_b, int64_t noise_k, int32_t *tokens,
                         int32_t *draft_states, float *logprobs, hipStream_t stream);
+size_t beam_step_workspace(int64_t B, int W, int k);
+hipError_t launch_beam_step(const DevTrie &t, const ngpu_beam_step_t &a, void *workspace, hipStream_t stream);
 }  // namespace ngpu
 
 namespace {
@@ -251,6 +253,41 @@ int ngpu_lm_fused_topk(const ngpu_lm *lm, const float *d_asr, int64_t B, int64_t
     hipError_t e = ngpu::launch_fused_topk(t, d_asr, B, asr_ld, lambda, k, d_states, d_tokens, d_scores, d_next,
                                            static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return hip_fail(e, "fused top-k launch");
+    return ok();
+}
+
+size_t ngpu_lm_beam_step_workspace(int64_t B, int32_t W, int32_t k) {
+    if (B <= 0 || W < 1 || W > NGPU_LM_MAX_BEAMS || k < 1 || k > NGPU_LM_MAX_BEAMS || B > kMaxBatch / W) return 0;
+    return ngpu::beam_step_workspace(B, W, k);
+}
+
+int ngpu_lm_beam_step(const ngpu_lm *lm, const ngpu_beam_step_t *args, void *d_workspace, size_t workspace_bytes,
+                      void *hip_stream) {
+    if (!lm || !args) return fail(NGPU_E_INVALID_ARG, "null argument");
+    if (const int rc = ready(lm)) return rc;
+    const ngpu_beam_step_t &a = *args;
+    if (a.mode != NGPU_FUSION_PLAIN && a.mode != NGPU_FUSION_TRANSDUCER && a.mode != NGPU_FUSION_AED)
+        return fail(NGPU_E_INVALID_ARG, "fusion mode %d: a beam step is plain, transducer or AED", a.mode);
+    if (a.mode == NGPU_FUSION_AED && !lm->hdr.has_final)
+        return fail(NGPU_E_INVALID_ARG, "AED fusion needs a model with </s> (NGPU_BUILD_BOS_EOS)");
+    if (a.last && a.mode != NGPU_FUSION_AED) return fail(NGPU_E_INVALID_ARG, "hypotheses end in AED mode only");
+    if (a.W < 1 || a.W > NGPU_LM_MAX_BEAMS || a.k < 1 || a.k > NGPU_LM_MAX_BEAMS)
+        return fail(NGPU_E_INVALID_ARG, "W = %d and k = %d must lie in [1, %d]", a.W, a.k, NGPU_LM_MAX_BEAMS);
+    if (a.B < 0 || a.B > kMaxBatch / a.W)
+        return fail(NGPU_E_INVALID_ARG, "B = %lld: at most %lld hypotheses", (long long)a.B, (long long)kMaxBatch);
+    if (a.asr_stride_b < 0 || a.asr_stride_w < 0) return fail(NGPU_E_INVALID_ARG, "negative strides");
+    if (!std::isfinite(a.lambda)) return fail(NGPU_E_INVALID_ARG, "lambda must be finite");
+    if (a.B == 0) return ok();
+    if (!a.asr || !a.states || !a.scores || !a.out_tokens || !a.out_parents || !a.out_scores || !a.out_states)
+        return fail(NGPU_E_INVALID_ARG, "null device pointer");
+    const size_t need = ngpu::beam_step_workspace(a.B, a.W, a.k);
+    if (!d_workspace || workspace_bytes < need)
+        return fail(NGPU_E_INVALID_ARG, "the workspace has %zu bytes, %zu are needed", d_workspace ? workspace_bytes : 0, need);
+    if (reinterpret_cast<uintptr_t>(d_workspace) % 16 != 0)
+        return fail(NGPU_E_INVALID_ARG, "the workspace must be 16-byte aligned");
+    if (const hipError_t e = ngpu::launch_beam_step(dev_view(lm), a, d_workspace, static_cast<hipStream_t>(hip_stream));
+        e != hipSuccess)
+        return hip_fail(e, "beam step launch");
     return ok();
 }
 

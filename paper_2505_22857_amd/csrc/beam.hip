@@ -1,0 +1,343 @@
+// One step of a beam search with the n-gram model fused in: the k best
+// continuations over all hypotheses of an utterance and the whole vocabulary.
+//
+// Two launches.  The first expands a hypothesis a workgroup: the query's walk
+// and the fused scores stay in its registers (group.h), as in the top-k, the
+// hypothesis's score is added (the sums are what is ordered, since adding rounds) and its k
+// best sums are listed, a key each: the sum's order-preserving bits above the
+// complement of the continuation's place in (hypothesis, class) order, so
+// that larger keys come first and all differ.  Selection as in the top-k
+// kernel: a lower bound of the k-th largest from the maxima of disjoint parts,
+// halvings of the interval while too many reach it, then a short list in LDS
+// whose entries find their ranks by counting.  The second selects the k
+// largest of an utterance's keys in the same way and writes them out.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "reduce.h"
+
+namespace ngpu {
+
+typedef unsigned long long u64;
+
+struct Beam {
+    ngpu_beam_step_t a;
+    int classes;         // of a row: V, or V + 1
+    u64 *keys;           // [B, W, k + 1] the hypothesis's best, descending, and that of class V; 0: none
+    int32_t *next;       // [B, W, k + 1] their states
+};
+
+__device__ __forceinline__ int lanes_below(u64 mask) {   // bits of the lanes before this one
+    return int(__builtin_amdgcn_mbcnt_hi(unsigned(mask >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(mask), 0u)));
+}
+
+template <int W>
+constexpr int beam_list() { return W * kWave > NGPU_LM_MAX_BEAMS ? W * kWave : NGPU_LM_MAX_BEAMS; }
+
+template <int W, int NT, bool FULL>
+__global__ __launch_bounds__(W * kWave) void beam_expand_kernel(DevTrie t, Beam p, int64_t n0) {
+    extern __shared__ i32x4 lds4[];
+    load_trie_args(t);
+    load_args(p.a.asr, p.a.states, p.a.scores, p.a.last, p.keys, p.next, p.a.W, p.a.k, p.a.lambda);
+    constexpr int kList = beam_list<W>();
+    const int64_t n = n0 + blockIdx.x, b = n / p.a.W;
+    const int V = t.vocab_size, hyp = int(n - b * p.a.W), k = p.a.k;
+    Meet *meet = reinterpret_cast<Meet *>(lds4);
+    const Group<W, NT, FULL> g(V, reinterpret_cast<i32x2 *>(meet + 1));
+    // the list takes the slots' place: every wavefront has read its slots before the barrier of the first exchange
+    u64 *lkey = reinterpret_cast<u64 *>(meet + 1);       // kList: key of the sum, ~token
+    int *lnext = reinterpret_cast<int *>(lkey + kList);  // kList: next state
+    const int wave = g.wave, lane = g.lane, tid = threadIdx.x;
+    u64 *const keys = p.keys + n * (k + 1);
+    int32_t *const next = p.next + n * (k + 1);
+    const unsigned place0 = unsigned(hyp) * unsigned(p.classes);
+
+    const int s_l = p.a.states[n];   // issued before the row, so its wait leaves the row in flight
+    const float score_l = p.a.scores[n];
+    const int last_l = p.a.last ? p.a.last[n] : -1;
+    Words<NT> row, dw, dt;
+    const float *const asr = p.a.asr + b * p.a.asr_stride_b + hyp * p.a.asr_stride_w;
+    g.load_row(asr, row);
+    const RecordIndex ri = record_index(t, lane);
+    g.clear_slots();
+    const int s = __builtin_amdgcn_readfirstlane(s_l), last = __builtin_amdgcn_readfirstlane(last_l);
+    const float score = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(score_l)));
+    const bool is = score > -__builtin_inff(), ended = last == V;
+    if (!is || ended || s < 0 || s >= t.num_states) {
+        if (tid == 0 && is && !ended) atomicAdd(&t.status[0], 1);
+        for (int j = tid; j < k; j += W * kWave) keys[j] = 0;
+        if (tid == 0) {
+            keys[k] = is && ended ? u64(float_key(score)) << 32 | ~(place0 + unsigned(V)) : 0;
+            next[k] = s;
+        }
+        return;
+    }
+    const int4 rec = load_record(ri, s, lane);
+    if (tid == 0) {   // class V keeps the state
+        u64 key = 0;
+        if (p.classes > V) {
+            const float lm = p.a.mode == kAed ? t.final_w[s] : 0.0f;
+            const float total = score + __builtin_fmaf(p.a.lambda, lm, asr[V]);
+            if (total > -__builtin_inff()) key = u64(float_key(total)) << 32 | ~(place0 + unsigned(V));
+        }
+        keys[k] = key;
+        next[k] = s;
+    }
+    const ChainHead h = head_of(rec);
+    g.load_dense(t, unsigned(h.dense_row), dw, dt);
+    const bool any = g.template put_levels<true>(t, rec, h);
+    float x[NT];
+    int nx[NT];
+    unsigned key[NT];
+    g.lm_values(h, dw, dt, any, x, nx);
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        x[i] = score + __builtin_fmaf(p.a.lambda, x[i], row.f(i));
+        // a token's key lies from -inf's (also a NaN's) to +inf's, below ~0; past V: below every token's
+        key[i] = FULL || kWave * i + lane < g.own ? float_key(or_lowest(x[i])) : 0u;
+        m = max(m, key[i]);
+    }
+
+    int xi = 0;
+    // value of every wavefront, entry l mod W in lane l
+    auto gather = [&](unsigned a) -> unsigned {
+        if (W == 1) return a;
+        const int buf = xi & 1;
+        ++xi;
+        if (lane == 0) meet->b[buf][wave] = int(a);
+        lds_barrier();
+        return unsigned(meet->b[buf][lane & (W - 1)]);
+    };
+    // 1. the bound, and the largest key
+    const int wanted = min(k, V);
+    const int full = ((V >> 6) * kWave + g.range - 1) / g.range;   // wavefronts whose lanes all hold tokens
+    unsigned part = m;
+    if (wanted <= 16 * full) {
+        part = max_over_waves<4>(part);
+        if (wanted <= 4 * full) part = max_over_waves<16>(part);
+    }
+    const unsigned wtop = wave_max_u32(m);
+    if (wanted <= full) part = wtop;
+    const unsigned wlow = wave < full ? wave_max_u32(~part) : 0u;   // complement of the smallest part
+    const unsigned top = __builtin_amdgcn_readfirstlane(max_over_waves<W>(gather(wtop)));
+    unsigned lo = wanted <= kWave * full ? ~unsigned(__builtin_amdgcn_readfirstlane(max_over_waves<W>(gather(wlow)))) : 0u;
+    if (lo == 0) lo = 1;   // every token's key is above 0
+
+    // keys >= x in this wavefront, and in the group: total, and of the wavefronts before this one
+    int total = 0, before = 0;
+    auto count = [&](unsigned at) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) c += __builtin_popcountll(__ballot(key[i] >= at));
+        const int e = int(gather(unsigned(c)));
+        total = 0;
+        before = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int u = W == 1 ? c : __builtin_amdgcn_readlane(e, w);
+            before += w < wave ? u : 0;
+            total += u;
+        }
+    };
+    // 2. at least `wanted` keys reach lo, fewer reach hi (hi - lo modulo 2^32)
+    const int most = min(kList, max(kWave, wanted + wanted / 4));
+    unsigned hi = top + 1;
+    count(lo);
+    for (int halvings = 0; total > most && hi - lo > 1 && (halvings < 6 || total > kList); ++halvings) {
+        const unsigned mid = lo + (hi - lo) / 2;
+        const int t0 = total, b0 = before;
+        count(mid);
+        if (total >= wanted) {
+            lo = mid;
+        } else {
+            hi = mid;
+            total = t0;
+            before = b0;
+        }
+    }
+    // 3. the list
+    int listed = total;
+    auto put = [&](bool take, int at, int i) {
+        if (take) {
+            lkey[at] = (u64(key[i]) << 32) | ~unsigned(g.token(i));
+            lnext[at] = nx[i] & kStateMask;
+        }
+    };
+    if (listed <= kList) {
+        int at = before;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const bool take = key[i] >= lo;
+            const u64 mask = __ballot(take);
+            put(take, at + lanes_below(mask), i);
+            at += __builtin_popcountll(mask);
+        }
+    } else {   // hi = lo + 1: the last key is lo, shared by more tokens than the list holds
+        const int all_before = before;
+        count(hi);
+        const int above = total;
+        int at = before, tie = above + all_before - before;
+        listed = wanted;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const bool over = key[i] >= hi, same = key[i] == lo;
+            const u64 mo = __ballot(over), ms = __ballot(same);
+            put(over, at + lanes_below(mo), i);
+            put(same && tie + lanes_below(ms) < wanted, tie + lanes_below(ms), i);
+            at += __builtin_popcountll(mo);
+            tie += __builtin_popcountll(ms);
+        }
+    }
+    if (W > 1) lds_barrier();
+    // entry tid of the list (which has no more than the group has threads, as k is at most 64)
+    static_assert(kList <= W * kWave, "an entry a thread");
+    const u64 mine = tid < listed ? lkey[tid] : ~0ull;
+    int rank = 0;
+#pragma unroll 8
+    for (int q = 0; q < listed; ++q) rank += lkey[q] > mine ? 1 : 0;
+    if (tid < listed && rank < wanted) {
+        const unsigned sum = unsigned(mine >> 32);   // -inf is not selected
+        keys[rank] = sum > kInfKey ? u64(sum) << 32 | ~(place0 + ~unsigned(mine)) : 0;
+        next[rank] = lnext[tid];
+    }
+    for (int j = wanted + tid; j < k; j += W * kWave) keys[j] = 0;
+}
+
+// An utterance's k largest of its hypotheses' keys, E a thread.
+constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / kWave;
+template <int E>
+__global__ __launch_bounds__(kSelectThreads) void beam_select_kernel(Beam p, int64_t b0) {
+    __shared__ u64 list[E * kSelectThreads];
+    __shared__ int from[E * kSelectThreads];
+    __shared__ int counts[2][kSelectWaves];
+    const int64_t b = b0 + blockIdx.x;
+    const int k = p.a.k, n = p.a.W * (k + 1), tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const u64 *const keys = p.keys + b * n;
+    u64 x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = e * kSelectThreads + tid < n ? keys[e * kSelectThreads + tid] : 0;
+    int turn = 0, total = 0, before = 0;
+    auto count = [&](unsigned at) {   // keys whose sum's bits reach `at`: all, and those of the wavefronts before
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) c += __builtin_popcountll(__ballot(unsigned(x[e] >> 32) >= at));
+        if (lane == 0) counts[turn][wave] = c;
+        __syncthreads();
+        total = before = 0;
+#pragma unroll
+        for (int w = 0; w < kSelectWaves; ++w) {
+            before += w < wave ? counts[turn][w] : 0;
+            total += counts[turn][w];
+        }
+        turn ^= 1;
+    };
+    // at least min(k, keys that there are) reach lo; fewer than k reach hi, where hi is not 0
+    unsigned lo = 1, hi = 0;
+    count(lo);
+    const int there = total;
+    while (total > max(kWave, 2 * k) && hi - lo > 1) {
+        const unsigned mid = lo + (hi - lo) / 2;
+        const int t0 = total, c0 = before;
+        count(mid);
+        if (total >= k) {
+            lo = mid;
+        } else {
+            hi = mid;
+            total = t0;
+            before = c0;
+        }
+    }
+    int at = before;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const bool take = unsigned(x[e] >> 32) >= lo;
+        const u64 mask = __ballot(take);
+        if (take) {
+            list[at + lanes_below(mask)] = x[e];
+            from[at + lanes_below(mask)] = e * kSelectThreads + tid;
+        }
+        at += __builtin_popcountll(mask);
+    }
+    __syncthreads();
+    for (int i = tid; i < total; i += kSelectThreads) {
+        const u64 mine = list[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int q = 0; q < total; ++q) rank += list[q] > mine ? 1 : 0;
+        if (rank >= k) continue;
+        const unsigned place = ~unsigned(mine), parent = place / unsigned(p.classes);
+        const int64_t out = b * k + rank;
+        p.a.out_tokens[out] = int32_t(place - parent * unsigned(p.classes));
+        p.a.out_parents[out] = int32_t(parent);
+        p.a.out_scores[out] = key_float(unsigned(mine >> 32));
+        p.a.out_states[out] = p.next[b * n + from[i]];
+    }
+    for (int j = there + tid; j < k; j += kSelectThreads) {   // left over
+        const int64_t out = b * k + j;
+        p.a.out_tokens[out] = p.a.out_parents[out] = -1;
+        p.a.out_scores[out] = -__builtin_inff();
+        p.a.out_states[out] = 0;
+    }
+}
+
+template <int W, int NT>
+static hipError_t expand(const DevTrie &t, const Beam &p, hipStream_t stream) {
+    constexpr int64_t kMost = int64_t(1) << 22;   // workgroups a launch
+    const size_t lds = sizeof(Meet) + std::max(size_t(beam_list<W>()) * 12, size_t(W) * kWave * NT * sizeof(i32x2));
+    const int64_t all = p.a.B * p.a.W;
+    for (int64_t n0 = 0; n0 < all; n0 += kMost) {
+        const dim3 grid(unsigned(std::min(kMost, all - n0))), block(W * kWave);
+        if (t.vocab_size == W * kWave * NT)
+            hipLaunchKernelGGL((beam_expand_kernel<W, NT, true>), grid, block, lds, stream, t, p, n0);
+        else
+            hipLaunchKernelGGL((beam_expand_kernel<W, NT, false>), grid, block, lds, stream, t, p, n0);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int E>
+static hipError_t select(const Beam &p, hipStream_t stream) {
+    constexpr int64_t kMost = int64_t(1) << 22;
+    for (int64_t b0 = 0; b0 < p.a.B; b0 += kMost) {
+        hipLaunchKernelGGL(beam_select_kernel<E>, dim3(unsigned(std::min(kMost, p.a.B - b0))), dim3(kSelectThreads), 0, stream,
+                           p, b0);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Wavefronts and tokens per lane of a hypothesis: the top-k kernel's rules for k up to 64.
+static hipError_t expand(const DevTrie &t, const Beam &p, int V, hipStream_t stream) {
+    const int64_t n = p.a.B * p.a.W;
+    if (V <= 256) return expand<1, 4>(t, p, stream);
+    if (V <= 512) return p.a.k > 32 && n <= 1024 ? expand<2, 4>(t, p, stream) : expand<1, 8>(t, p, stream);
+    if (V <= 768 && n > 1024) return expand<1, 12>(t, p, stream);
+    if (V <= 1024) return n > 1024 ? expand<2, 8>(t, p, stream) : expand<4, 4>(t, p, stream);
+    if (V <= 1536 && n > 768) return V <= 1280 ? expand<2, 10>(t, p, stream) : expand<2, 12>(t, p, stream);
+    if (V <= 2048) return expand<4, 8>(t, p, stream);
+    if (V <= 4096) return n <= 128 ? expand<8, 8>(t, p, stream) : expand<4, 16>(t, p, stream);
+    if (V <= 6144) return expand<8, 12>(t, p, stream);
+    return expand<8, 16>(t, p, stream);
+}
+
+size_t beam_step_workspace(int64_t B, int W, int k) {
+    return (size_t(B) * size_t(W) * size_t(k + 1) * 12 + 15) / 16 * 16;
+}
+
+hipError_t launch_beam_step(const DevTrie &t, const ngpu_beam_step_t &a, void *workspace, hipStream_t stream) {
+    const size_t n = size_t(a.B) * size_t(a.W) * size_t(a.k + 1);
+    u64 *const keys = static_cast<u64 *>(workspace);
+    const Beam p{a, t.vocab_size + (a.mode == kPlain ? 0 : 1), keys, reinterpret_cast<int32_t *>(keys + n)};
+    if (const hipError_t e = expand(t, p, t.vocab_size, stream); e != hipSuccess) return e;
+    const int each = a.W * (a.k + 1);
+    if (each <= kSelectThreads) return select<1>(p, stream);
+    if (each <= 4 * kSelectThreads) return select<4>(p, stream);
+    static_assert(NGPU_LM_MAX_BEAMS * (NGPU_LM_MAX_BEAMS + 1) <= 17 * kSelectThreads, "the largest beams' keys");
+    return select<17>(p, stream);
+}
+
+}  // namespace ngpu

@@ -147,3 +147,40 @@ def append8(x, cache, scale, pages, start, counts):
                     cache[p, first + lead:first + lead + len(new), h] = to_e4m3(y * (np.float32(1) / now))
             known[p, first:first + lead + len(new)] = True
     return cache, scale, known
+
+
+def beam_step(oracle, V, asr, lam, states, scores, k, mode="plain", last=None):
+    """Classes, parents, sums and states of the k best continuations.  The sums are the operator's own fp32 ones: one
+    rounding of asr + lam * lm (through 64 bits of mantissa, which the 48 of the product fit) and one of the sum."""
+    B, W = states.shape
+    C = V + (mode != "plain")
+    out = np.full((B, k), -1, np.int32), np.full((B, k), -1, np.int32), np.full((B, k), -np.inf, np.float32), \
+        np.zeros((B, k), np.int32)
+    bad = 0
+    for b in range(B):
+        total, after = np.full((W, C), -np.inf, np.float32), np.zeros((W, C), np.int32)
+        for w in range(W):
+            if not scores[b, w] > -np.inf:
+                continue
+            s = int(states[b, w])
+            if last is not None and last[b, w] == V:
+                total[w, V], after[w, V] = scores[b, w], s
+                continue
+            if not 0 <= s < oracle.num_states:
+                bad += 1
+                continue
+            lm, to = oracle.advance(np.array([s], np.int32))[:2]
+            lm, to = lm[0], to[0]
+            if mode != "plain":
+                end = oracle.final(np.array([s], np.int32))[0] if mode == "aed" else np.float32(0)
+                lm, to = np.append(lm, np.float32(end)), np.append(to, s)
+            with np.errstate(invalid="ignore", over="ignore"):
+                fused = (np.longdouble(np.float32(lam)) * lm.astype(np.longdouble) + asr[b, w, :C]).astype(np.float32)
+                total[w] = scores[b, w] + fused
+            after[w] = to
+        flat = np.where(np.isnan(total), -np.inf, total).ravel()
+        for j, i in enumerate(np.argsort(-flat, kind="stable")[:k]):
+            if flat[i] > -np.inf:
+                out[1][b, j], out[0][b, j] = divmod(int(i), C)
+                out[2][b, j], out[3][b, j] = flat[i], after.ravel()[i]
+    return (*out, bad)

@@ -27,11 +27,11 @@ def error():
 def test_structures_match_the_header(tmp_path):
     if shutil.which("gcc") is None:
         pytest.skip("gcc is not available")
-    names = {"ngpu_kv_fork_t": pages._Fork, "ngpu_kv_cache8_t": serving._Cache8}
+    names = {"ngpu_beam_step_t": ng._BeamStep, "ngpu_kv_fork_t": pages._Fork, "ngpu_kv_cache8_t": serving._Cache8}
     lines = ["#include <stdio.h>", '#include "ngpu_lm.h"', "int main(void) {"]
     for name, cls in names.items():
         lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
-        lines += [f'printf("{name}.{f} %zu\\n", offsetof({name}, {f}));' for f, _ in cls._fields_]
+        lines += [f'printf("{name}.{f} %zu\\n", offsetof({name}, {"lambda" if f == "lam" else f}));' for f, _ in cls._fields_]
     lines.append('printf("fork %d\\npages %lld\\n", NGPU_LM_MAX_FORK, (long long)NGPU_LM_MAX_PAGES);')
     src, exe = tmp_path / "sizes.c", tmp_path / "sizes"
     src.write_text("\n".join(lines + ["return 0; }"]))
@@ -144,3 +144,15 @@ def test_device_tensors_are_asked_for():
         ng.kv_compact(x[0], 16)
     with pytest.raises(TypeError):
         ng.kv_copy(c, c, x[:, :3])
+
+
+def test_a_beam_step_needs_an_uploaded_model():
+    from synth import make_model
+    lib, m = ng.load_library(), ng.NgpuLM.from_model(make_model("trigram_v128"))
+    a = ng._BeamStep(1, 2, 2, 0, 0.5, 64, 256, 128, 64, 64, None, 64, 64, 64, 64)
+    assert lib.ngpu_lm_beam_step(None, ctypes.byref(a), 64, 1 << 20, None) == INVALID
+    assert lib.ngpu_lm_beam_step(m._h, None, 64, 1 << 20, None) == INVALID
+    assert lib.ngpu_lm_beam_step(m._h, ctypes.byref(a), 64, 1 << 20, None) == -8
+    assert lib.ngpu_lm_beam_step_workspace(4, 8, 8) >= 4 * 8 * 9 * 12
+    for none in ((0, 8, 8), (-1, 8, 8), (4, 0, 8), (4, 65, 8), (4, 8, 0), (4, 8, 65), (1 << 26, 8, 8)):
+        assert lib.ngpu_lm_beam_step_workspace(*none) == 0
