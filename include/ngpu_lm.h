@@ -444,8 +444,8 @@ typedef struct {
 int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *args, void *hip_stream);
 
 /* ngpu_lm_attend over a cache in 8 bits: keys and values are the elements times their scales, in fp32.
- * The matrix cores take caches whose dim and strides are multiples of 16 elements, with k and v aligned to 16 bytes and out
- * to 8, and whose pages span no more than 2^35 elements; an element kernel takes the others. */
+ * The matrix cores take caches whose dim and strides are multiples of 16 elements, with k, v and out aligned to 16 bytes,
+ * whose pages span no more than 2^35 elements; an element kernel takes the others, many times slower. */
 size_t ngpu_lm_attend8_workspace(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args);
 int ngpu_lm_attend8(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args, void *d_workspace,
                     size_t workspace_bytes, void *hip_stream);

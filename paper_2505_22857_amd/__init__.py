@@ -42,7 +42,8 @@ EXPORTED = [
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
     "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
-    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8", "ngpu_lm_beam_step_workspace",
+    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8", "ngpu_lm_attend8_workspace", "ngpu_lm_attend8",
+    "ngpu_lm_beam_step_workspace",
     "ngpu_lm_beam_step",
         "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
@@ -122,7 +123,8 @@ def load_library(path: str = LIB_PATH):
     for name in EXPORTED:
         if name not in ("ngpu_lm_free", "ngpu_lm_device_bytes", "ngpu_lm_last_error", "ngpu_arpa_free",
                         "ngpu_lm_verify_workspace", "ngpu_lm_attend_workspace", "ngpu_lm_kv_fork_workspace",
-                        "ngpu_lm_kv_compact_workspace", "ngpu_lm_beam_step_workspace"):
+                        "ngpu_lm_kv_compact_workspace", "ngpu_lm_beam_step_workspace",
+                        "ngpu_lm_attend8_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libngpu_lm.so")
 FAST_PATH = os.path.join(HERE, "_fastcall.so")
 SOURCES = ["api.cpp", "trie_build.cpp", "arpa.cpp", "advance.hip", "fused_step.hip", "decode.hip", "topk.hip",
-           "draft.hip", "serving.cpp", "verify.hip", "kv_append.hip", "attend.hip",
+           "draft.hip", "serving.cpp", "verify.hip", "kv_append.hip", "attend.hip", "attend8.hip",
            "pages.hip", "kv_copy.hip", "kv_append8.hip", "beam.hip"]
 
 HIPCC_FLAGS = [

@@ -38,6 +38,7 @@
 #include <type_traits>
 
 #include "cache.h"
+#include "values8.h"
 #include "walk.h"
 
 namespace ngpu {
@@ -47,10 +48,27 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
 struct Attend {
     ngpu_kv_cache_t c;
     ngpu_attend_t a;
 };
+// The same over a cache in 8 bits.
+struct Attend8 : Attend {
+    const float *k_scale, *v_scale;
+    int64_t k_scale_page, k_scale_block, k_scale_head, v_scale_page, v_scale_block, v_scale_head;
+    unsigned block, block_magic;   // tokens a scale; floor(2^32 / that), 2^32 - 1 for 1
+};
+// Of a call whose cache holds elements of type C, queries and output of type T.
+template <class C>
+using AttendOf = std::conditional_t<std::is_same_v<C, E4m3>, Attend8, Attend>;
+
+// n / d, by floor(2^32 / d) (2^32 - 1 for d = 1): the product is up to one too low.
+__device__ __forceinline__ unsigned divided(unsigned n, unsigned d, unsigned magic) {
+    const unsigned i = __umulhi(n, magic);
+    return n - i * d >= d ? i + 1 : i;
+}
 
 __device__ __forceinline__ int64_t query_length(const ngpu_attend_t &a, int64_t s) {
     return a.q_lengths ? min(max(int64_t(a.q_lengths[s]), int64_t(0)), a.T) : a.T;
@@ -100,10 +118,11 @@ struct AttendPlan {
 
 // 16 bytes of zeros, which stand for keys and dimensions that do not exist.
 static __device__ __attribute__((aligned(16))) unsigned kNoData[4];
+static __device__ float kNoScale = 1.0f;
 
 // One row's running maximum (in log2) and sums, a wavefront's lanes holding every
 // 64th dimension: for what the matrix instructions do not take.
-template <class T>
+template <class T, class C>
 struct RowPart {
     static constexpr int kDims = NGPU_LM_MAX_HEAD_DIM / kWave;
     float q[kDims], o[kDims], m = -__builtin_inff(), sum = 0.0f;
@@ -116,13 +135,13 @@ struct RowPart {
             o[i] = 0.0f;
         }
     }
-    __device__ __forceinline__ void take(const Attend &p, const PageTable &table, int64_t j, int kv, int lane) {
+    __device__ __forceinline__ void take(const AttendOf<C> &p, const PageTable &table, int64_t j, int kv, int lane) {
         int64_t entry;
         const int64_t page = table.page(p.c, j, entry);
         if (page < 0) return;
-        const T *k = static_cast<const T *>(p.c.k) + page * p.c.k_stride_page + entry * p.c.k_stride_token +
+        const C *k = static_cast<const C *>(p.c.k) + page * p.c.k_stride_page + entry * p.c.k_stride_token +
                      kv * p.c.k_stride_head;
-        const T *v = static_cast<const T *>(p.c.v) + page * p.c.v_stride_page + entry * p.c.v_stride_token +
+        const C *v = static_cast<const C *>(p.c.v) + page * p.c.v_stride_page + entry * p.c.v_stride_token +
                      kv * p.c.v_stride_head;
         float x = 0.0f;
 #pragma unroll
@@ -130,6 +149,12 @@ struct RowPart {
             if (const int d = lane + kWave * i; d < p.c.dim) x = __builtin_fmaf(q[i], to_float(k[d]), x);
         for (int d = kWave / 2; d > 0; d /= 2) x += __shfl_xor(x, d);
         x *= p.a.scale * 1.44269504088896f;
+        float vs = 1.0f;
+        if constexpr (std::is_same_v<C, E4m3>) {
+            const int64_t block = entry / p.block;
+            x *= p.k_scale[page * p.k_scale_page + block * p.k_scale_block + kv * p.k_scale_head];
+            vs = p.v_scale[page * p.v_scale_page + block * p.v_scale_block + kv * p.v_scale_head];
+        }
         if (!(x <= m)) {   // a NaN score makes the row NaN
             const float f = __builtin_amdgcn_exp2f(m - x);
             sum *= f;
@@ -139,9 +164,10 @@ struct RowPart {
         }
         const float w = x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x - m);
         sum += w;
+        const float by = w * vs;
 #pragma unroll
         for (int i = 0; i < kDims; ++i)
-            if (const int d = lane + kWave * i; d < p.c.dim) o[i] = __builtin_fmaf(w, to_float(v[d]), o[i]);
+            if (const int d = lane + kWave * i; d < p.c.dim) o[i] = __builtin_fmaf(by, to_float(v[d]), o[i]);
     }
     // the finished row; `counts`: of a query token that counts
     __device__ __forceinline__ void finish(const Attend &p, int64_t row, int lane, bool counts) const {
@@ -171,6 +197,13 @@ struct Matrix<Bf16> {
         typedef __bf16 v2 __attribute__((ext_vector_type(2)));
         return __builtin_bit_cast(unsigned, v2{__bf16(a), __bf16(b)});
     }
+    // eight e4m3 values, which bfloat16 and half hold exactly
+    static __device__ __forceinline__ s16x8 widen(int a, int b) {
+        return __builtin_bit_cast(s16x8, u32x4{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true))});
+    }
 };
 template <>
 struct Matrix<F16> {
@@ -183,6 +216,12 @@ struct Matrix<F16> {
     static __device__ __forceinline__ unsigned round(float a, float b) {
         typedef _Float16 v2 __attribute__((ext_vector_type(2)));
         return __builtin_bit_cast(unsigned, v2{_Float16(a), _Float16(b)});
+    }
+    static __device__ __forceinline__ s16x8 widen(int a, int b) {
+        return __builtin_bit_cast(s16x8, u32x4{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false)),
+                                               __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true))});
     }
 };
 
@@ -250,21 +289,29 @@ __device__ __forceinline__ void load_to_lds(const void *from0, unsigned offset0,
                      ::"s"(at0), "v"(offset0), "s"(base0), "s"(at1), "v"(offset1), "s"(base1) : "memory");
 }
 
+// 4 bytes a lane from memory to LDS at `at` + 4 lane, as above.
+__device__ __forceinline__ void load_word_to_lds(const void *p, unsigned at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(p) : "memory");
+}
+
 // Steps that operands are loaded from LDS before the matrix instructions that take them.
 constexpr int kKeysAhead = 2, kValuesAhead = 3;
 
 // DK: 32-dimension steps of a head; RT: tiles of 16 rows a wavefront; WR:
 // wavefronts, each with rows of its own, that share the tiles of keys.  Two stages: three and four,
 // or tiles of 32 keys for four wavefronts, were no faster.
-template <class T, int DK, int RT, int WR>
+template <class T, class C, int DK, int RT, int WR>
 struct AttendTile {
+    static constexpr bool kEight = std::is_same_v<C, E4m3>;
+    static constexpr int kPer = 16 / int(sizeof(C));            // elements of a 16-byte chunk
     static constexpr int kChunks = WR > 2 ? 2 : 1;              // of 32 keys, a tile
     static constexpr int kKeys = 32 * kChunks;                  // a tile
     static constexpr int kLoad = kKeys / WR;                // keys a wavefront loads
     static constexpr int kRows = 16 * RT * WR;                  // a workgroup
-    static constexpr int kPitch = DK <= 2 ? 128 : (DK <= 4 ? 256 : 512);   // bytes of a row in LDS
+    static constexpr int kPitch = (DK <= 2 ? 64 : (DK <= 4 ? 128 : 256)) * int(sizeof(C));   // bytes of a row in LDS
     static constexpr int kPieces = kPitch / 16;                 // 16-byte chunks of it
-    static constexpr int kStage = 2 * kKeys * kPitch;           // keys, then values
+    static constexpr int kUsed = 32 * DK / kPer;                // of which DK steps read
+    static constexpr int kStage = 2 * kKeys * kPitch + (kEight ? 8 * kKeys : 0);   // keys, values, and their scales
     static constexpr int kStages = 2;                           // tiles in LDS: one in use, the other on its way
     static constexpr int kLds = kStages * kStage;
     static constexpr int kPerLoad = kWave / kPieces;            // rows a load instruction brings
@@ -274,16 +321,21 @@ struct AttendTile {
     static_assert(kKeysAhead <= DK && kValuesAhead <= kTiles, "the first steps lie in the first chunk");
     static_assert(kLoad == (WR == 1 ? 32 : 16), "a wavefront's keys are half of a mask where several share it");
 
-    static __device__ __forceinline__ int key_swizzle(int row) { return kPieces == 8 ? (row >> 1) & 7 : row & 15; }
+    static __device__ __forceinline__ int key_swizzle(int row) {
+        return kPieces == 4 ? (row >> 2) & 3 : (kPieces == 8 ? (row >> 1) & 7 : row & 15);
+    }
     static __device__ __forceinline__ int value_swizzle(int row) {
+        if (kEight)   // a transposing load of 8 bits reads rows 0 to 3 and 16 to 19 of its 32 with a quarter of the lanes
+            return kPieces == 4 ? ((row >> 2) & 1) | ((row >> 3) & 2)
+                                : (kPieces == 8 ? ((row >> 1) & 3) | ((row >> 2) & 4) : (row & 7) | ((row >> 1) & 8));
         return kPieces == 8 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
     }
 };
 
 // Work `w` of the plan, for WR wavefronts with LDS from `lds0` on.
-template <class T, int DK, int RT, int WR>
-__device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &plan, unsigned w, unsigned lds0) {
-    using A = AttendTile<T, DK, RT, WR>;
+template <class T, class C, int DK, int RT, int WR>
+__device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendPlan &plan, unsigned w, unsigned lds0) {
+    using A = AttendTile<T, C, DK, RT, WR>;
     using M = Matrix<T>;
     unsigned (*masks)[A::kChunks] = nullptr;   // per stage, a bit for each key that exists
     if constexpr (WR > 1) {
@@ -346,10 +398,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     const unsigned page_size = unsigned(p.c.page_size);
     const bool in_page = page_size % A::kLoad == 0;
     auto first_key = [&](int tile) { return unsigned(tile) * A::kKeys + unsigned(wave * A::kLoad); };
-    auto page_index = [&](unsigned j) {   // j / page_size
-        unsigned i = __umulhi(j, plan.page_magic);
-        return j - i * page_size >= page_size ? i + 1 : i;
-    };
+    auto page_index = [&](unsigned j) { return divided(j, page_size, plan.page_magic); };
     // in_page: lane l has the page of tile base + l, so that no load is waited for between tiles; else the
     // page of its key of the next tile
     int base_tile = tile0, pages = -1;
@@ -389,7 +438,8 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         const T *src = static_cast<const T *>(a.q) + s * a.q_stride_seq + t * a.q_stride_token + head * a.q_stride_head;
 #pragma unroll
         for (int k = 0; k < DK; ++k) {
-            const int d = 32 * k + 8 * quad;
+            // (16 bytes of a key in 8 bits are a lane's dimensions of two steps)
+            const int d = A::kEight ? 64 * (k / 2) + 16 * quad + 8 * (k % 2) : 32 * k + 8 * quad;
             s16x8 x = {};
             if (is && d < D) {   // D is a multiple of 8
                 if (aligned) {
@@ -404,11 +454,11 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     }
     least = __builtin_amdgcn_readfirstlane(least);
 
-    const uint64_t k_page = uint64_t(p.c.k_stride_page) / 8, v_page = uint64_t(p.c.v_stride_page) / 8;
-    const unsigned k_token = unsigned(p.c.k_stride_token / 8), v_token = unsigned(p.c.v_stride_token / 8);
-    const char *k_head = static_cast<const char *>(p.c.k) + int64_t(h) * p.c.k_stride_head * 2;
-    const char *v_head = static_cast<const char *>(p.c.v) + int64_t(h) * p.c.v_stride_head * 2;
-    const int piece = lane % A::kPieces, in_load = lane / A::kPieces, pieces = D / 8;
+    const uint64_t k_page = uint64_t(p.c.k_stride_page) / A::kPer, v_page = uint64_t(p.c.v_stride_page) / A::kPer;
+    const unsigned k_token = unsigned(p.c.k_stride_token / A::kPer), v_token = unsigned(p.c.v_stride_token / A::kPer);
+    const char *k_head = static_cast<const char *>(p.c.k) + int64_t(h) * p.c.k_stride_head * int(sizeof(C));
+    const char *v_head = static_cast<const char *>(p.c.v) + int64_t(h) * p.c.v_stride_head * int(sizeof(C));
+    const int piece = lane % A::kPieces, in_load = lane / A::kPieces, pieces = D / A::kPer;
     auto key_piece = [&](int u) { return piece ^ A::key_swizzle(wave * A::kLoad + u * A::kPerLoad + in_load); };
     auto value_piece = [&](int u) { return piece ^ A::value_swizzle(wave * A::kLoad + u * A::kPerLoad + in_load); };
     // A lane's offsets from the first of its keys in one page, kept where several
@@ -420,7 +470,15 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         v_off[u] = (unsigned(u * A::kPerLoad + in_load) * v_token + unsigned(value_piece(u))) * 16;
         if (WR > 1) asm volatile("" : "+v"(k_off[u]), "+v"(v_off[u]));
     }
-    const bool whole_rows = D == 32 * DK && k_token < (1u << 21) && v_token < (1u << 21);
+    // In 8 bits, the chunks that a head does not have are zeros from here on: no load writes them otherwise.
+    const bool whole_head = D == 32 * DK;
+    if (A::kEight && !whole_head) {
+        for (int i = WR == 1 ? lane : int(threadIdx.x); i < A::kLds / 16; i += 64 * WR)
+            *lds_at<u32x4>(lds0 + 16 * unsigned(i)) = u32x4{0, 0, 0, 0};
+        wait_loads();
+        if (WR > 1) asm volatile("s_barrier" ::: "memory");
+    }
+    const bool whole_rows = (A::kEight || whole_head) && k_token < (1u << 21) && v_token < (1u << 21);
     const char *no_data = reinterpret_cast<const char *>(kNoData);
     asm volatile("" : "+s"(no_data));   // its address is loaded once
     unsigned valid = 0;   // keys that exist among those this wavefront loaded last
@@ -435,11 +493,24 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         // the u-th rows of a whole tile, all of whose dimensions exist
         auto load_whole = [&](int u, const char *kb, const char *vb) {
             const unsigned k_to = at + unsigned(u * kWave * 16), v_to = values_at + unsigned(u * kWave * 16);
-            if (4 * DK == A::kPieces) {
+            if (A::kUsed == A::kPieces && (!A::kEight || whole_head)) {
                 load_to_lds<A::kOnce>(kb, k_off[u], k_to, vb, v_off[u], v_to);
             } else {
-                if (key_piece(u) < 4 * DK) load_to_lds<A::kOnce>(kb, k_off[u], k_to);
-                if (value_piece(u) < 4 * DK) load_to_lds<A::kOnce>(vb, v_off[u], v_to);
+                const int used = A::kEight ? pieces : A::kUsed;
+                if (key_piece(u) < used) load_to_lds<A::kOnce>(kb, k_off[u], k_to);
+                if (value_piece(u) < used) load_to_lds<A::kOnce>(vb, v_off[u], v_to);
+            }
+        };
+        // the scales of this wavefront's keys, then values, a lane each; 1 where there is no key
+        auto load_scales = [&](int64_t page, unsigned entry, bool there) {
+            if constexpr (A::kEight) {
+                const bool values = lane >= A::kLoad;
+                const int64_t block = divided(entry, p.block, p.block_magic);
+                const float *from = values ? p.v_scale + page * p.v_scale_page + block * p.v_scale_block + h * p.v_scale_head
+                                           : p.k_scale + page * p.k_scale_page + block * p.k_scale_block + h * p.k_scale_head;
+                if (lane < 2 * A::kLoad)
+                    load_word_to_lds(there ? from : &kNoScale, lds0 + unsigned(stage * A::kStage + 2 * A::kKeys * A::kPitch +
+                                                                              wave * 8 * A::kLoad));
             }
         };
         if (in_page) {
@@ -455,6 +526,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
             const uint64_t entry = is ? j - page_index(j) * page_size : 0u, pg = is ? unsigned(p0) : 0u;
             const char *kb = k_head + (pg * k_page + entry * k_token) * 16;
             const char *vb = v_head + (pg * v_page + entry * v_token) * 16;
+            load_scales(int64_t(pg), unsigned(entry) + unsigned(lane % A::kLoad), is && lane % A::kLoad < left);
             if (valid == kAll && whole_rows) {
 #pragma unroll
                 for (int u = 0; u < A::kLoads; ++u) load_whole(u, kb, vb);
@@ -483,6 +555,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         const bool is = page >= 0 && page < p.c.num_pages;
         valid = unsigned(__ballot(is)) & kAll;
         put_mask();
+        load_scales(is ? page : 0, entry, is);
         if (valid == kAll && whole_rows && page_size % A::kPerLoad == 0) {   // a load's keys lie in one page
             unsigned e = j - page_index(j) * page_size;
             const char *kb = nullptr, *vb = nullptr;   // of the page's entry 0, for this load's offsets
@@ -517,9 +590,17 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
 
     // This lane's places in a tile: step 0 of its operand row of K, dimensions 0 of its blocks of V; step k
     // is at the first XOR 64 k, dimensions 16 d at the second XOR 32 d.
-    const int v_in = 4 * quad + col / 4;
+    // (In 8 bits a step is of 64 dimensions, and a transposing load brings 8 keys, which come as two blocks of 4 do.)
+    const int v_in = A::kEight ? 4 * quad + col / 2 % 4 + 16 * (col / 8) : 4 * quad + col / 4;
     const unsigned k_first = unsigned(col * A::kPitch + 16 * (quad ^ A::key_swizzle(col)));
-    const unsigned v_first = unsigned(v_in * A::kPitch + 16 * (((col % 4) / 2) ^ A::value_swizzle(v_in)) + 8 * (col & 1));
+    const unsigned v_first = unsigned(v_in * A::kPitch +
+                                      16 * ((A::kEight ? 0 : (col % 4) / 2) ^ A::value_swizzle(v_in)) + 8 * (col & 1));
+    // the scales of this lane's keys of chunk c, block u
+    auto scales_at = [&](unsigned tile_at, int c, int u, bool values) {
+        const unsigned at = tile_at + 2 * A::kKeys * A::kPitch;
+        return *lds_at<f32x4>(at + unsigned(A::kLoad == 32 ? 64 * u + (values ? 128 : 0) : 128 * (2 * c + u) + (values ? 64 : 0)) +
+                              16 * unsigned(quad));
+    };
 
     f32x4 o[RT][A::kTiles];
     float m[RT], sum[RT];   // m: what weights are relative to; sum: of this lane's keys', before they are rounded
@@ -532,26 +613,39 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
     }
     // (a factor of 0 would make NaN of the -inf of a key that is not seen)
     const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.scale) * 1.44269504088896f, 1e-30f);
+    constexpr float kRoom = A::kEight ? 0.0f : M::kRoom;   // (weights of values in 8 bits are bfloat16 always)
 
     // A value that is not finite would reach the rows that do not see its key (0 *
     // inf): where a tile holds such keys and values, the rows are computed one by one at the end.
     bool one_by_one = false;
     // A tile's keys into every row's sums: those whose bit of `exists` is set.
     auto take = [&](int stage, int key0, const unsigned (&exists)[A::kChunks]) {
-        constexpr int C = A::kChunks;
+        constexpr int N = A::kChunks;
         const unsigned tile_at = lds0 + unsigned(stage * A::kStage);
         unsigned k_at = tile_at + k_first, v_at = tile_at + A::kKeys * A::kPitch + v_first;
         asm volatile("" : "+v"(k_at), "+v"(v_at));   // their steps are computed below, not kept in registers
         // Operands are loaded a few steps ahead of the matrix instructions, which hides LDS's latency, and no
         // further: hoisted loads would not fit the registers.
-        f32x4 x[RT][2 * C];
-        s16x8 kx[kKeysAhead + 1][2], vx[kValuesAhead + 1];
+        f32x4 x[RT][2 * N];
+        s16x8 kx[kKeysAhead + 1][2], vx[kValuesAhead + 1];   // as they are multiplied, or
+        i32x4 kx8[2][2];                                     // in 8 bits
+        i32x2 vx8[kValuesAhead + 1];
+        auto load_keys8 = [&](int i) {   // 32 keys of steps 2 i mod DK and the one behind
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                kx8[i % 2][u] = *lds_at<i32x4>((k_at ^ unsigned(64 * (i % (DK / 2)))) + (i / (DK / 2) * 2 + u) * 16 * A::kPitch);
+        };
         auto load_keys = [&](int i) {   // 32 keys of step i mod DK
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 kx[i % (kKeysAhead + 1)][u] = *lds_at<s16x8>((k_at ^ unsigned(64 * (i % DK))) + (i / DK * 2 + u) * 16 * A::kPitch);
         };
         auto load_values = [&](int i) {   // 32 keys, dimensions 16 (i mod kTiles) on
+            if constexpr (A::kEight) {
+                vx8[i % (kValuesAhead + 1)] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    lds_at<i32x2>((v_at ^ unsigned(16 * (i % A::kTiles))) + i / A::kTiles * 32 * A::kPitch));
+                return;
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const s16x4 part = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(
@@ -560,12 +654,45 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                 for (int e = 0; e < 4; ++e) vx[i % (kValuesAhead + 1)][4 * u + e] = part[e];
             }
         };
+        if constexpr (A::kEight) {
+            constexpr int kSteps = N * DK / 2;
+            load_keys8(0);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                if (i + 1 < kSteps) load_keys8(i + 1);
+                if (i + 1 == kSteps) {
+#pragma unroll
+                    for (int j = 0; j < kValuesAhead; ++j) load_values(j);
+                }
+                const int c = i / (DK / 2), k = i % (DK / 2) * 2;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const i32x4 raw = kx8[i % 2][u];
+                        const s16x8 key = e == 0 ? M::widen(raw[0], raw[1]) : M::widen(raw[2], raw[3]);
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            x[r][2 * c + u] = M::mul(key, q[r][k + e], k + e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // the scores in log2, from here on
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const f32x4 by = scales_at(tile_at, c, u, false) * to_log2;
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) x[r][2 * c + u] *= by;
+                }
+        } else {
 #pragma unroll
         for (int i = 0; i < kKeysAhead; ++i) load_keys(i);
 #pragma unroll
-        for (int i = 0; i < C * DK; ++i) {
-            if (i + kKeysAhead < C * DK) load_keys(i + kKeysAhead);
-            if (i + 1 == C * DK) {
+        for (int i = 0; i < N * DK; ++i) {
+            if (i + kKeysAhead < N * DK) load_keys(i + kKeysAhead);
+            if (i + 1 == N * DK) {
 #pragma unroll
                 for (int j = 0; j < kValuesAhead; ++j) load_values(j);
             }
@@ -577,15 +704,16 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                     x[r][2 * c + u] = M::mul(kx[i % (kKeysAhead + 1)][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        }
         const bool some_rows = own && key0 > least - A::kKeys;   // some rows do not see some of the keys
         bool all = !some_rows;
 #pragma unroll
-        for (int c = 0; c < C; ++c) all = all && exists[c] == 0xffffffffu;
+        for (int c = 0; c < N; ++c) all = all && exists[c] == 0xffffffffu;
         if (!all) {
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
+                for (int c = 0; c < N; ++c) {
                     // the row's view of this lane's keys: bit 16 u + i is key 16 u + 4 quad + i
                     const int below = limit[r] - key0 - 32 * c - 4 * quad;
                     const unsigned sees = exists[c] >> (4 * quad) &
@@ -597,10 +725,28 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
                     __builtin_amdgcn_sched_barrier(0);
                 }
             if (some_rows) {
-                u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
+if constexpr (A::kEight) {
+                    unsigned nan = 0;   // a byte whose lower bits are all set
+                    for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
+                        const u32x4 v = *lds_at<u32x4>(tile_at + A::kKeys * A::kPitch + 16 * i) & 0x7f7f7f7fu;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) nan |= (v[e] + 0x01010101u) & 0x80808080u;
+                    }
+                    bool odd = nan != 0;
+#pragma unroll
+                    for (int c = 0; c < N; ++c)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const f32x4 vs = scales_at(tile_at, c, u, true);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) odd |= !(__builtin_fabsf(vs[e]) < __builtin_inff());
+                        }
+                    if (__ballot(odd)) one_by_one = true;
+                } else {
+                                u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
                 for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
                     // (the places of pieces that a head does not have hold what was in LDS before)
-                    if (4 * DK != A::kPieces && (i % A::kPieces ^ A::value_swizzle(i / A::kPieces)) >= 4 * DK) continue;
+                    if (A::kUsed != A::kPieces && (i % A::kPieces ^ A::value_swizzle(i / A::kPieces)) >= A::kUsed) continue;
                     most = __builtin_elementwise_max(
                         most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
                 }
@@ -608,6 +754,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
 #pragma unroll
                 for (int e = 0; e < 8; ++e) odd |= most[e] >= M::kInfinity;
                 if (__ballot(odd)) one_by_one = true;
+                }
             }
         }
         float top[RT];
@@ -616,14 +763,14 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         for (int r = 0; r < RT; ++r) {
             top[r] = x[r][0][0];
 #pragma unroll
-            for (int e = 1; e < 8 * C; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
-            top[r] *= to_log2;
-            rises |= top[r] > m[r] + (8.0f + M::kRoom);   // (also while m is -inf)
+            for (int e = 1; e < 8 * N; ++e) top[r] = __builtin_fmaxf(top[r], x[r][e / 4][e % 4]);
+            if (!A::kEight) top[r] *= to_log2;
+            rises |= top[r] > m[r] + (8.0f + kRoom);   // (also while m is -inf)
         }
         if (__ballot(rises)) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const float now = __builtin_fmaxf(m[r], row_max(top[r]) - M::kRoom);
+                const float now = __builtin_fmaxf(m[r], row_max(top[r]) - kRoom);
                 const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[r] - now);
                 m[r] = now;
                 sum[r] *= f;
@@ -634,9 +781,32 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         float base[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) base[r] = m[r] == -__builtin_inff() ? 0.0f : m[r];
-        u32x4 weights[RT][C];   // of chunk c: pairs of rounded ones
+        u32x4 weights[RT][N];   // of chunk c: pairs of rounded ones
+        // In 8 bits a weight takes its value's scale along, in bfloat16, whose exponents have room for both; where the
+        // output is half, in two parts, the second what the first's rounding has left.
+        constexpr bool kParts = A::kEight && std::is_same_v<T, F16>;
+        u32x4 rests[RT][N];
+        f32x4 v_scales[N][2];
+        if constexpr (A::kEight) {
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) v_scales[c][u] = scales_at(tile_at, c, u, true);
+        }
         auto weigh = [&](int c, int pair) {   // the pair-th of the chunk's 4 RT
             const int r = pair / 4, e = pair % 4 * 2;
+            if constexpr (A::kEight) {
+                const float z0 = __builtin_amdgcn_exp2f(x[r][2 * c + e / 4][e % 4] - base[r]);
+                const float z1 = __builtin_amdgcn_exp2f(x[r][2 * c + e / 4][e % 4 + 1] - base[r]);
+                sum[r] += z0;
+                sum[r] += z1;
+                const float y0 = z0 * v_scales[c][e / 4][e % 4], y1 = z1 * v_scales[c][e / 4][e % 4 + 1];
+                const unsigned both = Matrix<Bf16>::round(y0, y1);
+                weights[r][c][pair % 4] = both;
+                if constexpr (kParts)
+                    rests[r][c][pair % 4] = Matrix<Bf16>::round(y0 - __uint_as_float(both << 16), y1 - __uint_as_float(both & 0xffff0000u));
+                return;
+            }
             const float z0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4], to_log2, -base[r]));
             const float z1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4 + 1], to_log2, -base[r]));
             sum[r] += z0;
@@ -652,13 +822,23 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
         // the next chunk's weights are computed between the matrix instructions of this one
         constexpr int kPairs = (4 * RT + A::kTiles - 1) / A::kTiles;
 #pragma unroll
-        for (int i = 0; i < C * A::kTiles; ++i) {
+        for (int i = 0; i < N * A::kTiles; ++i) {
             const int c = i / A::kTiles, d = i % A::kTiles;
-            if (i + kValuesAhead < C * A::kTiles) load_values(i + kValuesAhead);
+            if (i + kValuesAhead < N * A::kTiles) load_values(i + kValuesAhead);
+            if constexpr (A::kEight) {
+                const i32x2 raw = vx8[i % (kValuesAhead + 1)];
+                const s16x8 value = Matrix<Bf16>::widen(raw[0], raw[1]);
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-                o[r][d] = M::mul(vx[i % (kValuesAhead + 1)], __builtin_bit_cast(s16x8, weights[r][c]), o[r][d]);
-            if (c + 1 < C) {
+                for (int r = 0; r < RT; ++r) {
+                    o[r][d] = Matrix<Bf16>::mul(value, __builtin_bit_cast(s16x8, weights[r][c]), o[r][d]);
+                    if constexpr (kParts) o[r][d] = Matrix<Bf16>::mul(value, __builtin_bit_cast(s16x8, rests[r][c]), o[r][d]);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    o[r][d] = M::mul(vx[i % (kValuesAhead + 1)], __builtin_bit_cast(s16x8, weights[r][c]), o[r][d]);
+            }
+            if (c + 1 < N) {
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j)
                     if (d * kPairs + j < 4 * RT) weigh(c + 1, d * kPairs + j);
@@ -697,7 +877,7 @@ __device__ __forceinline__ void attend_tiles(const Attend &p, const AttendPlan &
             if (row >= rows) break;
             const int t = int(row / unsigned(rep)), head = h * rep + int(row % unsigned(rep));   // (own: one sequence)
             const int nq = int(query_length(a, s0)), seen = max(0, min(count, count - nq + t + 1));
-            RowPart<T> r;
+            RowPart<T, C> r;
             r.load(p, s0, t, head, lane);
             const unsigned end = min(unsigned(tile1) * A::kKeys, unsigned(seen));
             for (unsigned j = unsigned(tile0) * A::kKeys; j < end; ++j) r.take(p, table, j, h, lane);
@@ -753,30 +933,30 @@ __device__ __forceinline__ unsigned tile_lds() {
 }
 
 // Registers are held to what two workgroups of four wavefronts a CU leave each where that spills nothing.
-template <class T, int DK, int RT, int WR>
-__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(Attend p, AttendPlan plan,
+template <class T, class C, int DK, int RT, int WR>
+__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(AttendOf<C> p, AttendPlan plan,
                                                                               unsigned work0) {
-    attend_tiles<T, DK, RT, WR>(p, plan, work0 + blockIdx.x, tile_lds());
+    attend_tiles<T, C, DK, RT, WR>(p, plan, work0 + blockIdx.x, tile_lds());
 }
 
 // Prefixes whose rows take WR wavefronts, and own tokens whose rows take one, in
 // one launch: the second wait for memory while the first compute.  A workgroup
 // is either WR wavefronts at one work of a prefix or, first, as many as have
 // room in the same LDS at a work of own tokens each.
-template <class T, int DK, int RT, int WR>
-constexpr int kOwnWaves = AttendTile<T, DK, RT, WR>::kLds / AttendTile<T, DK, RT, 1>::kLds;
-template <class T, int DK, int RT, int WR>
-__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_both_kernel(Attend p, AttendPlan plan,
+template <class T, class C, int DK, int RT, int WR>
+constexpr int kOwnWaves = AttendTile<T, C, DK, RT, WR>::kLds / AttendTile<T, C, DK, RT, 1>::kLds;
+template <class T, class C, int DK, int RT, int WR>
+__global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_both_kernel(AttendOf<C> p, AttendPlan plan,
                                                                               unsigned block0, unsigned own_blocks) {
-    constexpr int kWaves = kOwnWaves<T, DK, RT, WR>;
+    constexpr int kWaves = kOwnWaves<T, C, DK, RT, WR>;
     const unsigned lds0 = tile_lds(), block = block0 + blockIdx.x;
     if (block >= own_blocks) {
-        attend_tiles<T, DK, RT, WR>(p, plan, block - own_blocks, lds0);
+        attend_tiles<T, C, DK, RT, WR>(p, plan, block - own_blocks, lds0);
         return;
     }
     const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), w = block * kWaves + wave;
     if (wave < kWaves && w < unsigned(plan.own.works()))
-        attend_tiles<T, DK, RT, 1>(p, plan, unsigned(plan.prefix.works()) + w, lds0 + wave * AttendTile<T, DK, RT, 1>::kLds);
+        attend_tiles<T, C, DK, RT, 1>(p, plan, unsigned(plan.prefix.works()) + w, lds0 + wave * AttendTile<T, C, DK, RT, 1>::kLds);
 }
 
 }  // namespace ngpu

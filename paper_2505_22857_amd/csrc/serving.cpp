@@ -14,6 +14,8 @@ hipError_t launch_verify(const ngpu_verify_t &a, void *workspace, hipStream_t st
 hipError_t launch_kv_append(const ngpu_kv_cache_t &c, const ngpu_kv_append_t &a, hipStream_t stream);
 size_t attend_workspace(const ngpu_kv_cache_t &c, const ngpu_attend_t &a);
 hipError_t launch_attend(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, void *workspace, hipStream_t stream);
+size_t attend8_workspace(const ngpu_kv_cache8_t &c, const ngpu_attend_t &a);
+hipError_t launch_attend8(const ngpu_kv_cache8_t &c, const ngpu_attend_t &a, void *workspace, hipStream_t stream);
 hipError_t launch_kv_append8(const ngpu_kv_cache8_t &c, const ngpu_kv_append_t &a, hipStream_t stream);
 hipError_t launch_kv_copy8(const ngpu_kv_cache8_t &c, const int32_t *copies, int64_t n, hipStream_t stream);
 size_t kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages);
@@ -146,6 +148,13 @@ int check_attend(const ngpu_kv_cache_t *c, const ngpu_attend_t *a) {
     return NGPU_OK;
 }
 
+int check_attend_pointers(const ngpu_attend_t &a) {
+    if (!a.q || !a.out || (a.G > 0 && (!a.prefix_lengths || (a.prefix_width > 0 && !a.prefix_pages))) ||
+        (a.pages && !a.lengths))
+        return refuse("null device pointer");
+    return NGPU_OK;
+}
+
 int check_pool(int64_t num_pages, int32_t page_size) {
     if (num_pages < 0 || num_pages > NGPU_LM_MAX_PAGES)
         return refuse("num_pages = %lld outside [0, %lld]", (long long)num_pages, (long long)NGPU_LM_MAX_PAGES);
@@ -223,11 +232,26 @@ int ngpu_lm_attend(const ngpu_kv_cache_t *cache, const ngpu_attend_t *args, void
     if (const int rc = check_attend(cache, args)) return rc;
     const ngpu_attend_t &a = *args;
     if (a.S == 0 || a.T == 0) return done(hipSuccess, "");
-    if (!a.q || !a.out || (a.G > 0 && (!a.prefix_lengths || (a.prefix_width > 0 && !a.prefix_pages))) ||
-        (a.pages && !a.lengths))
-        return refuse("null device pointer");
+    if (const int rc = check_attend_pointers(a)) return rc;
     if (const int rc = check_workspace(d_workspace, workspace_bytes, ngpu::attend_workspace(*cache, a))) return rc;
     return done(ngpu::launch_attend(*cache, a, d_workspace, static_cast<hipStream_t>(hip_stream)), "attend launch");
+}
+
+size_t ngpu_lm_attend8_workspace(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args) {
+    if (check_cache8(cache) != NGPU_OK || check_attend(&cache->cache, args) != NGPU_OK) return 0;
+    if (args->S == 0 || args->T == 0) return 0;
+    return ngpu::attend8_workspace(*cache, *args);
+}
+
+int ngpu_lm_attend8(const ngpu_kv_cache8_t *cache, const ngpu_attend_t *args, void *d_workspace,
+                    size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_cache8(cache)) return rc;
+    if (const int rc = check_attend(&cache->cache, args)) return rc;
+    const ngpu_attend_t &a = *args;
+    if (a.S == 0 || a.T == 0) return done(hipSuccess, "");
+    if (const int rc = check_attend_pointers(a)) return rc;
+    if (const int rc = check_workspace(d_workspace, workspace_bytes, ngpu::attend8_workspace(*cache, a))) return rc;
+    return done(ngpu::launch_attend8(*cache, a, d_workspace, static_cast<hipStream_t>(hip_stream)), "attend launch");
 }
 
 size_t ngpu_lm_kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages) {

@@ -78,6 +78,9 @@ def _library():
         lib.ngpu_lm_kv_append8.argtypes = [p(_Cache8), p(_Append), _vp]
         lib.ngpu_lm_attend_workspace.argtypes = [p(_Cache), p(_Attend)]
         lib.ngpu_lm_attend_workspace.restype = ctypes.c_size_t
+        lib.ngpu_lm_attend8_workspace.argtypes = [p(_Cache8), p(_Attend)]
+        lib.ngpu_lm_attend8_workspace.restype = ctypes.c_size_t
+        lib.ngpu_lm_attend8.argtypes = [p(_Cache8), p(_Attend), _vp, ctypes.c_size_t, _vp]
         lib.ngpu_lm_attend.argtypes = [p(_Cache), p(_Attend), _vp, ctypes.c_size_t, _vp]
         _lib = lib
     return _lib
@@ -318,7 +321,7 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
 
 
 def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, prefix_lengths=None, q_lengths=None,
-           scale=None, return_lse: bool = False, stream=None):
+           scale=None, return_lse: bool = False, k_scale=None, v_scale=None, stream=None):
     """Attention of ``q`` [S, T, q heads, dim] over a paged cache [pages, page size, heads, dim].
 
     With ``prefix_pages`` [G, width] and ``prefix_lengths`` [G], consecutive sequences in G groups of
@@ -328,10 +331,15 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
     own.  ``scale`` is 1 / sqrt(dim) unless given.  Dimensions and strides in multiples of 8, 16-byte alignment and
     pages that span at most 32 GiB take the matrix cores; other caches a kernel many times slower.
 
+    With ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32 the caches are float8_e4m3fn, as ``kv_append``
+    writes them: keys and values are the elements times the scale of their block of page size / blocks tokens and their
+    head.  Multiples of 16 elements take the matrix cores then.
+
     Returns [S, T, q heads, dim] (zero where a row sees no key or does not count), and with
     ``return_lse`` the log of each row's softmax sum [S, T, q heads] float32 (-inf there)."""
     native = _native()
-    if stream is None and native and not return_lse:
+    eight = k_scale is not None or v_scale is not None
+    if stream is None and native and not return_lse and not eight:
         r = native.attend(q, k_cache, v_cache, pages, lengths, prefix_pages, prefix_lengths, q_lengths,
                           scale if scale is None else float(scale))
         if r is not None:
@@ -339,10 +347,12 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
                 _check(r)
             return r
     torch = _torch_mod()
-    dev, cache = _cache(k_cache, v_cache)
+    dt, i32 = q.dtype if eight else k_cache.dtype, torch.int32
+    dev, whole = _cache8(k_cache, v_cache, k_scale, v_scale, dt) if eight else _cache(k_cache, v_cache)
+    cache = whole.cache if eight else whole
     if q.dim() != 4:
         raise ValueError("q must be a [S, T, q heads, dim] tensor")
-    S, T, heads, dt, i32 = q.shape[0], q.shape[1], q.shape[2], k_cache.dtype, torch.int32
+    S, T, heads = q.shape[:3]
     a = _Attend(S, T, heads, _need(q, "q", dev, dt, (S, T, heads, cache.dim), rows=True), *q.stride()[:3],
                 _need(q_lengths, "q_lengths", dev, i32, (S,)),
                 scale=1.0 / math.sqrt(cache.dim) if scale is None else float(scale))
@@ -359,15 +369,17 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
         a.lengths = _need(lengths, "lengths", dev, i32, (S,))
         if a.pages_width == 0:
             a.pages = None   # a table without pages holds no own tokens
-    _untracked(q=q, k_cache=k_cache, v_cache=v_cache)
+    _untracked(q=q, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
     lib = _library()
+    space, run = (lib.ngpu_lm_attend8_workspace, lib.ngpu_lm_attend8) if eight else \
+        (lib.ngpu_lm_attend_workspace, lib.ngpu_lm_attend)
     with _on(dev, stream) as handle:
         out = torch.empty(q.shape, dtype=dt, device=dev)
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev) if return_lse else None
         a.out, a.lse = out.data_ptr(), lse.data_ptr() if return_lse else None
-        size = lib.ngpu_lm_attend_workspace(ctypes.byref(cache), ctypes.byref(a))
+        size = space(ctypes.byref(whole), ctypes.byref(a))
         workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-        _check(lib.ngpu_lm_attend(ctypes.byref(cache), ctypes.byref(a), workspace.data_ptr(), size, handle))
+        _check(run(ctypes.byref(whole), ctypes.byref(a), workspace.data_ptr(), size, handle))
     return (out, lse) if return_lse else out
 
 

@@ -103,6 +103,24 @@ def test_bad_caches_of_8_bits_are_refused(lib, change):
     lib8 = serving._library()
     assert lib8.ngpu_lm_kv_append8(ctypes.byref(c), ctypes.byref(ok_append()), None) == INVALID and error()
     assert lib.ngpu_lm_kv_copy8(ctypes.byref(c), 64, 1, None) == INVALID and error()
+    from test_serving_host import ok_attend
+    assert lib8.ngpu_lm_attend8(ctypes.byref(c), ctypes.byref(ok_attend()), 64, 1 << 30, None) == INVALID and error()
+    assert lib8.ngpu_lm_attend8_workspace(ctypes.byref(c), ctypes.byref(ok_attend())) == 0
+
+
+def test_attend8_refuses(lib):
+    from test_serving_host import ok_attend
+    lib8, c = serving._library(), ok_cache8()
+    need = lib8.ngpu_lm_attend8_workspace(ctypes.byref(c), ctypes.byref(ok_attend()))
+    assert need >= 2 * 4 * 2 * 4 * (64 * 4 + 8)
+    assert lib8.ngpu_lm_attend8(ctypes.byref(c), ctypes.byref(ok_attend()), 64, need - 1, None) == INVALID
+    assert lib8.ngpu_lm_attend8(None, ctypes.byref(ok_attend()), 64, need, None) == INVALID
+    assert lib8.ngpu_lm_attend8(ctypes.byref(c), None, 64, need, None) == INVALID
+    assert lib8.ngpu_lm_attend8_workspace(None, ctypes.byref(ok_attend())) == 0
+    for change in (dict(S=-1), dict(T=1 << 31), dict(q_heads=3), dict(G=3), dict(q=None), dict(out=None), dict(lengths=None),
+                   dict(prefix_lengths=None), dict(q_stride_seq=-1), dict(scale=float("nan"))):
+        assert lib8.ngpu_lm_attend8(ctypes.byref(c), ctypes.byref(ok_attend(**change)), 64, 1 << 30, None) == INVALID
+    assert lib8.ngpu_lm_attend8(ctypes.byref(c), ctypes.byref(ok_attend(S=0, G=1)), None, 0, None) == 0
 
 
 def test_append8_and_copy8_refuse(lib):
