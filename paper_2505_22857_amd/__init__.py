@@ -157,6 +157,11 @@ def _load_fast():
         mod.bind_serving(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                            (lib.ngpu_lm_draft, lib.ngpu_lm_verify_workspace, lib.ngpu_lm_verify, lib.ngpu_lm_kv_append,
                             lib.ngpu_lm_attend_workspace, lib.ngpu_lm_attend)))
+        mod.bind_beam(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                        (lib.ngpu_lm_kv_append8, lib.ngpu_lm_attend8_workspace, lib.ngpu_lm_attend8, lib.ngpu_lm_kv_copy,
+                         lib.ngpu_lm_kv_copy8, lib.ngpu_lm_kv_fork_workspace, lib.ngpu_lm_kv_fork,
+                         lib.ngpu_lm_kv_compact_workspace, lib.ngpu_lm_kv_compact, lib.ngpu_lm_kv_move,
+                         lib.ngpu_lm_beam_step_workspace, lib.ngpu_lm_beam_step)))
         _fast = mod
     return _fast
 
@@ -483,6 +488,12 @@ class NgpuLM:
         Returns (classes, parents among the W, scores, states), [B, k] each, in descending order (ties to the lowest parent,
         then class); what is left over has class and parent -1, score -inf and state 0.  The parents are
         ``kv_fork``'s; the classes the next step's ``last``."""
+        if stream is None and self._fast is not None:
+            r = self._fast.beam_step(self._h.value, self.vocab_size, asr, float(lam), states, scores, k, last, mode)
+            if r is not None:   # None: not the ordinary call, handled (or refused) below
+                if r.__class__ is int:
+                    _check(r)
+                return r
         import torch
         from .serving import _need, _on
         if not hasattr(asr, "is_cuda") or not asr.is_cuda or asr.dtype is not torch.float32:

@@ -215,7 +215,9 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     // Workgroups a CU: more of them only disturb each other's streams.  One prefix
     // of 100000 tokens for 5 x 4 rows, 8 heads of 128, us: 238 / 205 / 214 / 273 with 2 / 3 /
     // 4 / 5; heads of 64: 67 / 51 / 49 / 52; of 256 (2 fit): 48, 62 with 3.
-    const int64_t per_cu = r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2);
+    // In 8 bits a tile has half the bytes on their way, and more workgroups keep as many: 4 prefixes of 120000 tokens for 2 x
+    // 4 rows, 8 heads of 128, us: 298 / 207 / 172 / 184 / 197 with 3 / 4 / 5 / 6 / 8; 2 of 30000, 4 heads of 256: 41 / 42 / 45 with 3 / 4 / 5.
+    const int64_t per_cu = kEight ? (r.steps <= 4 ? 5 : 3) : (r.steps == 2 ? 4 : (r.steps <= 4 ? 3 : 2));
     const int64_t prefix_rows = a.G > 0 ? a.S / a.G * a.T * rep : 0;
     if (a.pages) {
         // Workgroups: 2 a CU, not 4, where several wavefronts share the keys (us: 4 sequences of 500 tokens that see 3500,

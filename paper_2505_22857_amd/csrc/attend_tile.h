@@ -784,7 +784,7 @@ if constexpr (A::kEight) {
         u32x4 weights[RT][N];   // of chunk c: pairs of rounded ones
         // In 8 bits a weight takes its value's scale along, in bfloat16, whose exponents have room for both; where the
         // output is half, in two parts, the second what the first's rounding has left.
-        constexpr bool kParts = A::kEight && std::is_same_v<T, F16>;
+        constexpr bool kParts = A::kEight;
         u32x4 rests[RT][N];
         f32x4 v_scales[N][2];
         if constexpr (A::kEight) {

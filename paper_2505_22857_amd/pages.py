@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes
 
 from . import _check, _torch_mod, load_library
-from .serving import _cache, _Cache, _cache8, _Cache8, _device_of, _need, _on, _table, _untracked
+from .serving import _cache, _Cache, _cache8, _Cache8, _device_of, _native, _need, _on, _table, _untracked
 
 MAX_FORK = 4096                  # NGPU_LM_MAX_FORK
 MAX_PAGES = 1 << 28              # NGPU_LM_MAX_PAGES
@@ -74,6 +74,13 @@ def kv_fork(pages, lengths, parents, refs, page_size: int, tokens=0, stream=None
     and length 0 that is forked with its prompt's tokens.
 
     Returns (pages [G * K, width], lengths [G * K] without the new tokens, copies [G * K, 3]), int32."""
+    native = _native()
+    if stream is None and native:
+        r = native.kv_fork(pages, lengths, parents, refs, page_size, tokens)
+        if r is not None:   # None: not the ordinary call, handled (or refused) below
+            if r.__class__ is int:
+                _check(r)
+            return r
     torch = _torch_mod()
     dev, refs_at, P = _pool(refs)
     i32 = torch.int32
@@ -109,8 +116,15 @@ def kv_copy(k_cache, v_cache, copies, k_scale=None, v_scale=None, stream=None):
     ``copies`` [n, 3] int32 of ``kv_fork`` or ``kv_compact``: {from, to, entries} a row; rows with a page outside
     the cache are skipped.  No page may be written by two rows, or written by one and read by another.  Of an
     8-bit cache all scales of a page, ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32, go with it."""
-    torch = _torch_mod()
+    native = _native()
     eight = k_scale is not None or v_scale is not None
+    if stream is None and native:
+        r = native.kv_copy(k_cache, v_cache, copies, *((k_scale, v_scale) if eight else ()))
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return
+    torch = _torch_mod()
     dev, cache = _cache8(k_cache, v_cache, k_scale, v_scale, torch.float16) if eight else _cache(k_cache, v_cache)
     if copies.dim() != 2:
         raise ValueError("copies must be a [n, 3] tensor")
@@ -129,9 +143,15 @@ def kv_compact(refs, page_size: int, tables=(), stream=None):
     updated in place; ``kv_copy`` then has to move the pages of each layer's cache.
 
     Returns (copies [pages // 2, 3] int32, moved [pages] int32: each page's new number)."""
+    native, tables = _native(), tuple(tables)
+    if stream is None and native:
+        r = native.kv_compact(refs, page_size, tables)
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r
     torch = _torch_mod()
     dev, refs_at, P = _pool(refs)
-    tables = list(tables)
     found = [_table(t, f"tables[{i}]", dev, t.shape[0]) for i, t in enumerate(tables)]
     for i, t in enumerate(tables):
         if t.shape[0] > 1 and t.stride(0) < t.shape[1]:

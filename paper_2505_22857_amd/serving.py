@@ -231,14 +231,14 @@ def _layout(k_cache, v_cache, dev, code):
 
 def _cache8(k_cache, v_cache, k_scale, v_scale, dtype):
     """A cache in 8 bits, with queries, keys and values of ``dtype``."""
+    if k_scale is None or v_scale is None:
+        raise ValueError("k_scale and v_scale come together")
     torch = _torch_mod()
     dev, code = _device_of(k_cache, "k_cache"), _type_code(dtype)
     if k_cache.dtype is not torch.float8_e4m3fn:
         raise TypeError("a cache with scales must be float8_e4m3fn")
     if code not in (NGPU_F16, NGPU_BF16):
         raise TypeError("an 8-bit cache goes with float16 or bfloat16")
-    if k_scale is None or v_scale is None:
-        raise ValueError("k_scale and v_scale come together")
     c = _layout(k_cache, v_cache, dev, code)
     if k_scale.dim() != 3 or k_scale.shape[1] < 1 or c.page_size % k_scale.shape[1] != 0:
         raise ValueError("the scales must be [pages, blocks of a page, heads] tensors whose blocks divide a page")
@@ -276,8 +276,9 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
     Returns the rotated queries (zero where a token does not count), None without ``q``."""
     native = _native()
     eight = k_scale is not None or v_scale is not None
-    if stream is None and native and not eight:
-        r = native.kv_append(k, v, k_cache, v_cache, pages, start, positions, cos, sin, layout, q, lengths)
+    if stream is None and native:
+        r = native.kv_append(k, v, k_cache, v_cache, pages, start, positions, cos, sin, layout, q, lengths,
+                             *((k_scale, v_scale) if eight else ()))
         if r is not None:
             if r.__class__ is int:
                 _check(r)
@@ -339,9 +340,9 @@ def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, pre
     ``return_lse`` the log of each row's softmax sum [S, T, q heads] float32 (-inf there)."""
     native = _native()
     eight = k_scale is not None or v_scale is not None
-    if stream is None and native and not return_lse and not eight:
+    if stream is None and native and not return_lse:
         r = native.attend(q, k_cache, v_cache, pages, lengths, prefix_pages, prefix_lengths, q_lengths,
-                          scale if scale is None else float(scale))
+                          scale if scale is None else float(scale), *((k_scale, v_scale) if eight else ()))
         if r is not None:
             if r.__class__ is int:
                 _check(r)
