@@ -8,8 +8,9 @@
 // so a row that is to get the r-th free page finds its block in the counts'
 // prefix sums and reads the page from the list.
 //
-// Three launches, as each needs the one before whole: tables and counts; what
-// every row needs and what is free; the pages.  Bound by these launches until
+// Three steps, as each needs the one before whole: tables and counts; what every
+// row needs and what is free; the pages.  A few rows of a small pool are taken
+// by one workgroup in one launch, others by a launch a step; bound by these launches until
 // tables and pool are large.
 #include <hip/hip_runtime.h>
 
@@ -23,7 +24,10 @@ namespace ngpu {
 constexpr int kPageThreads = 256;
 constexpr int kPageWaves = kPageThreads / kWave;
 constexpr int kRowBlock = kPageThreads;        // rows whose needs are summed together
-constexpr int kTile = 4096;                    // pages a workgroup takes at a time: 16 a lane
+constexpr int kTileSteps = 4;                  // pages a lane takes at a time
+constexpr int kTile = kTileSteps * kPageThreads;
+constexpr int kOneThreads = 1024;              // of the workgroup that takes a call alone
+constexpr int kOneWaves = kOneThreads / kWave;
 constexpr int kMostPageBlocks = 1024;          // whose counts a workgroup holds
 
 // Blocks of pages: at most kMostPageBlocks, of whole tiles.
@@ -50,8 +54,9 @@ struct Fork {
 };
 
 // Sum over the workgroup's threads before this one; `total`: over all.
+template <int WAVES = kPageWaves>
 __device__ __forceinline__ int64_t scan_threads(int64_t x, int64_t &total) {
-    __shared__ int64_t sums[kPageWaves];
+    __shared__ int64_t sums[WAVES];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int64_t upto = x;
 #pragma unroll
@@ -65,7 +70,7 @@ __device__ __forceinline__ int64_t scan_threads(int64_t x, int64_t &total) {
     int64_t before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kPageWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         before += w < wave ? sums[w] : 0;
         total += sums[w];
     }
@@ -76,16 +81,16 @@ __device__ __forceinline__ int below(unsigned long long mask) {   // bits of the
     return int(__builtin_amdgcn_mbcnt_hi(unsigned(mask >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(mask), 0u)));
 }
 
-// The pages of a block for which `is` holds, in ascending order, a tile of coalesced loads at a time:
-// take(page, its number among them).  Returns how many there are; for the whole workgroup.
-template <class Is, class Take>
-__device__ __forceinline__ int over_pages(const int32_t *refs, int64_t p0, int64_t p1, Is is, Take take) {
-    constexpr int kSteps = kTile / kPageThreads;
-    __shared__ int sums[2][kPageWaves];
+// The pages of a block in ascending order, a tile of coalesced loads at a time: visit(page, whether its count meets `is`, how
+// many of the block before it do).  Returns how many do; for the whole workgroup.
+template <int WAVES = kPageWaves, class Is, class Visit>
+__device__ __forceinline__ int over_pages(const int32_t *refs, int64_t p0, int64_t p1, Is is, Visit visit) {
+    constexpr int kSteps = kTileSteps;
+    __shared__ int sums[2][WAVES];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int done = 0, turn = 0;
-    for (int64_t t0 = p0; t0 < p1; t0 += kTile, turn ^= 1) {
-        const int64_t w0 = t0 + wave * (kTile / kPageWaves) + lane;
+    for (int64_t t0 = p0; t0 < p1; t0 += kSteps * kWave * WAVES, turn ^= 1) {
+        const int64_t w0 = t0 + wave * (kSteps * kWave) + lane;
         int r[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) r[i] = w0 + kWave * i < p1 ? refs[w0 + kWave * i] : 0;
@@ -93,20 +98,20 @@ __device__ __forceinline__ int over_pages(const int32_t *refs, int64_t p0, int64
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            masks[i] = __ballot(w0 + kWave * i < p1 && is(r[i], w0 + kWave * i));
+            masks[i] = __ballot(w0 + kWave * i < p1 && is(r[i]));
             mine += __builtin_popcountll(masks[i]);
         }
         if (lane == 0) sums[turn][wave] = mine;
         __syncthreads();
         int at = done;
 #pragma unroll
-        for (int w = 0; w < kPageWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             at += w < wave ? sums[turn][w] : 0;
             done += sums[turn][w];
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            if (masks[i] >> lane & 1) take(w0 + kWave * i, at + below(masks[i]));
+            if (w0 + kWave * i < p1) visit(w0 + kWave * i, (masks[i] >> lane & 1) != 0, at + below(masks[i]));
             at += __builtin_popcountll(masks[i]);
         }
     }
@@ -118,11 +123,18 @@ __device__ __forceinline__ int64_t held_tokens(const ngpu_kv_fork_t &a, int64_t 
 }
 __device__ __forceinline__ bool in_pool(const ngpu_kv_fork_t &a, int32_t page) { return page >= 0 && page < a.num_pages; }
 
+// Counts are changed by many workgroups, or (ONE) by one, which then reads them.
+template <bool ONE>
+__device__ __forceinline__ void count_page(const ngpu_kv_fork_t &a, int32_t page, int by) {
+    if (!in_pool(a, page)) return;
+    __hip_atomic_fetch_add(a.refs + page, by, __ATOMIC_RELAXED, ONE ? __HIP_MEMORY_SCOPE_WORKGROUP : __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // 1. A wavefront a row, the new ones first: a new row's entries, and an old row's part of the counts (children less one).
-__global__ __launch_bounds__(kPageThreads) void fork_tables_kernel(Fork f, int64_t row0) {
+template <bool ONE>
+__device__ __forceinline__ void fork_tables(const Fork &f, int64_t row, int lane) {
     const ngpu_kv_fork_t &a = f.a;
-    const int lane = threadIdx.x % kWave;
-    const int64_t R = a.G * a.K, row = row0 + int64_t(blockIdx.x) * kPageWaves + threadIdx.x / kWave;
+    const int64_t R = a.G * a.K;
     if (row < R) {
         const int64_t g = row / a.K;
         const int32_t parent = a.parents[row];
@@ -150,11 +162,26 @@ __global__ __launch_bounds__(kPageThreads) void fork_tables_kernel(Fork f, int64
             children += __builtin_popcountll(__ballot(j0 + lane < a.K && a.parents[g * a.K + min(j0 + lane, a.K - 1)] == w));
         const int64_t have = children > 0 ? (held_tokens(a, old) + a.page_size - 1) / a.page_size : 0;
         // (one child takes over what the row held)
-        for (int64_t i = (children == 1 ? have : 0) + lane; i < a.width; i += kWave) {
-            const int32_t page = a.pages[old * a.pages_stride + i];
-            if (in_pool(a, page)) atomicAdd(a.refs + page, (i < have ? children : 0) - 1);
-        }
+        for (int64_t i = (children == 1 ? have : 0) + lane; i < a.width; i += kWave)
+            count_page<ONE>(a, a.pages[old * a.pages_stride + i], (i < have ? children : 0) - 1);
     }
+}
+__global__ __launch_bounds__(kPageThreads) void fork_tables_kernel(Fork f, int64_t row0) {
+    fork_tables<false>(f, row0 + int64_t(blockIdx.x) * kPageWaves + threadIdx.x / kWave, threadIdx.x % kWave);
+}
+
+// The fresh pages that a row needs, and the page that it copies.
+__device__ __forceinline__ int64_t fork_need(const Fork &f, int64_t row) {
+    const ngpu_kv_fork_t &a = f.a;
+    const int32_t last = f.last[row];
+    bool copy = false;
+    if (last >= 0) {
+        int before = 0;
+        for (int64_t r = row / a.K * a.K; r < row; ++r) before += f.last[r] == last ? 1 : 0;
+        copy = a.refs[last] - before > 1;
+    }
+    f.from[row] = copy ? last : -1;
+    return (copy ? 1 : 0) + max(f.more[row], 0);
 }
 
 // 2. What each row needs, summed over a row block, and the free pages of each block of pages.
@@ -163,18 +190,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_plan_kernel(Fork f, int64_t
     const int64_t R = a.G * a.K;
     if (int64_t(blockIdx.x) < row_blocks) {
         const int64_t row = int64_t(blockIdx.x) * kRowBlock + threadIdx.x;
-        int64_t need = 0;
-        if (row < R) {
-            const int32_t last = f.last[row];
-            bool copy = false;
-            if (last >= 0) {
-                int before = 0;
-                for (int64_t r = row / a.K * a.K; r < row; ++r) before += f.last[r] == last ? 1 : 0;
-                copy = a.refs[last] - before > 1;
-            }
-            f.from[row] = copy ? last : -1;
-            need = (copy ? 1 : 0) + max(f.more[row], 0);
-        }
+        const int64_t need = row < R ? fork_need(f, row) : 0;
         int64_t total;
         const int64_t before = scan_threads(need, total);
         if (row < R) f.start[row] = before;
@@ -182,8 +198,9 @@ __global__ __launch_bounds__(kPageThreads) void fork_plan_kernel(Fork f, int64_t
         return;
     }
     const int64_t b = int64_t(blockIdx.x) - row_blocks, p0 = b * f.blocks.per, p1 = min(a.num_pages, p0 + f.blocks.per);
-    const int n = over_pages(a.refs, p0, p1, [](int32_t r, int64_t) { return r == 0; },
-                             [&](int64_t page, int i) { f.lists[p0 + i] = int32_t(page); });
+    const int n = over_pages(a.refs, p0, p1, [](int32_t r) { return r == 0; }, [&](int64_t page, bool free, int i) {
+        if (free) f.lists[p0 + i] = int32_t(page);
+    });
     if (threadIdx.x == 0) f.counts[b] = n;
 }
 
@@ -209,27 +226,20 @@ __device__ __forceinline__ void scan_counts(const int32_t *counts, int blocks, i
     __syncthreads();
 }
 
-// 3. A wavefront a row: its fresh pages, or its entries given back.
-__global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f, int64_t row0) {
+// 3. A wavefront a row: its fresh pages, from the first-th free one on, or its entries given back.
+template <bool ONE>
+__device__ __forceinline__ void fork_pages(const Fork &f, int64_t row, int lane, int64_t first, const int32_t *before,
+                                           int blocks) {
     const ngpu_kv_fork_t &a = f.a;
-    __shared__ int32_t before[kMostPageBlocks + 1];
-    scan_counts(f.counts, f.blocks.count, before);
-    const int64_t R = a.G * a.K, w0 = row0 + int64_t(blockIdx.x) * kPageWaves, row_block = w0 / kRowBlock;
-    int64_t sum = 0, base;
-    for (int64_t b = threadIdx.x; b < row_block; b += kPageThreads) sum += f.row_sums[b];
-    scan_threads(sum, base);
-    const int lane = threadIdx.x % kWave;
-    const int64_t row = w0 + threadIdx.x / kWave;
-    if (row >= R) return;
     const int32_t parent = a.parents[row];
     const bool live = parent >= 0 && parent < a.W;
     const int32_t from = f.from[row], more = f.more[row];
-    const int64_t first = base + f.start[row], need = (from >= 0 ? 1 : 0) + max(more, 0);
+    const int64_t need = (from >= 0 ? 1 : 0) + max(more, 0);
     const int64_t n = live ? held_tokens(a, row / a.K * a.W + parent) : 0, have = (n + a.page_size - 1) / a.page_size;
     int32_t *const entries = a.out_pages + row * a.width, *const copy = a.copies + 3 * row;
-    if (live && (more < 0 || (need > 0 && first + need > before[f.blocks.count]))) {
+    if (live && (more < 0 || (need > 0 && first + need > before[blocks]))) {
         for (int64_t i = lane; i < have; i += kWave) {
-            if (const int32_t page = entries[i]; in_pool(a, page)) atomicAdd(a.refs + page, -1);
+            count_page<ONE>(a, entries[i], -1);
             entries[i] = -1;
         }
         if (lane == 0) {
@@ -240,7 +250,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f, int64_
         return;
     }
     auto fresh = [&](int64_t rank) {   // the free page of this rank
-        int lo = 0, hi = f.blocks.count;   // before[lo] <= rank < before[hi]
+        int lo = 0, hi = blocks;   // before[lo] <= rank < before[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             if (before[mid] <= rank)
@@ -260,15 +270,49 @@ __global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f, int64_
             const int32_t page = fresh(first);
             copy[1] = entries[have - 1] = page;
             copy[2] = int32_t(n % a.page_size);
-            atomicAdd(a.refs + from, -1);
+            count_page<ONE>(a, from, -1);
         }
     }
     for (int64_t i = lane; i < more; i += kWave) entries[have + i] = fresh(first + (from >= 0 ? 1 : 0) + i);
+}
+__global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f, int64_t row0) {
+    __shared__ int32_t before[kMostPageBlocks + 1];
+    scan_counts(f.counts, f.blocks.count, before);
+    const int64_t w0 = row0 + int64_t(blockIdx.x) * kPageWaves, row_block = w0 / kRowBlock;
+    int64_t sum = 0, base;
+    for (int64_t b = threadIdx.x; b < row_block; b += kPageThreads) sum += f.row_sums[b];
+    scan_threads(sum, base);
+    const int64_t row = w0 + threadIdx.x / kWave;
+    if (row < f.a.G * f.a.K) fork_pages<false>(f, row, threadIdx.x % kWave, base + f.start[row], before, f.blocks.count);
+}
+
+// All three, by one workgroup: at most a thread for each new row.
+__global__ __launch_bounds__(kOneThreads) void fork_one_kernel(Fork f) {
+    const ngpu_kv_fork_t &a = f.a;
+    __shared__ int32_t before[2];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t R = a.G * a.K, rows = R + a.G * a.W;
+    for (int64_t row = wave; row < rows; row += kOneWaves) fork_tables<true>(f, row, lane);
+    __syncthreads();
+    int64_t total;
+    const int64_t start = scan_threads<kOneWaves>(int64_t(threadIdx.x) < R ? fork_need(f, threadIdx.x) : 0, total);
+    if (int64_t(threadIdx.x) < R) f.start[threadIdx.x] = start;
+    if (threadIdx.x == 0) before[0] = 0;
+    const int n = over_pages<kOneWaves>(a.refs, 0, a.num_pages, [](int32_t r) { return r == 0; },
+                                        [&](int64_t page, bool free, int i) {
+                                            if (free) f.lists[i] = int32_t(page);
+                                        });
+    if (threadIdx.x == 0) before[1] = n;
+    __syncthreads();
+    for (int64_t row = wave; row < R; row += kOneWaves) fork_pages<true>(f, row, lane, f.start[row], before, 1);
 }
 
 namespace {
 
 constexpr int64_t kMostGroups = int64_t(1) << 23;   // workgroups a launch
+
+// Most rows (of 64 entries, old and new) and pages that one workgroup takes alone.
+constexpr int64_t kOneRows = 32, kOnePages = 16384;
 
 int64_t row_blocks_of(int64_t rows) { return (rows + kRowBlock - 1) / kRowBlock; }
 
@@ -306,6 +350,10 @@ size_t kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages) {
 hipError_t launch_kv_fork(const ngpu_kv_fork_t &a, void *workspace, hipStream_t stream) {
     const Fork f = fork_of(a, static_cast<char *>(workspace), nullptr);
     const int64_t R = a.G * a.K, rows = R + a.G * a.W;
+    if (R > 0 && R <= kOneThreads && rows * ((a.width + kWave - 1) / kWave) <= kOneRows && a.num_pages <= kOnePages) {
+        hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, f);
+        return hipGetLastError();
+    }
     for (int64_t r0 = 0; r0 < rows; r0 += kMostGroups * kPageWaves) {
         const int64_t grid = std::min(kMostGroups, (rows - r0 + kPageWaves - 1) / kPageWaves);
         hipLaunchKernelGGL(fork_tables_kernel, dim3(unsigned(grid)), dim3(kPageThreads), 0, stream, f, r0);
@@ -334,7 +382,7 @@ struct Compact {
 
 __global__ __launch_bounds__(kPageThreads) void compact_count_kernel(Compact c) {
     const int64_t p0 = int64_t(blockIdx.x) * c.blocks.per, p1 = min(c.num_pages, p0 + c.blocks.per);
-    const int n = over_pages(c.refs, p0, p1, [](int32_t r, int64_t) { return r != 0; }, [](int64_t, int) {});
+    const int n = over_pages(c.refs, p0, p1, [](int32_t r) { return r != 0; }, [](int64_t, bool, int) {});
     if (threadIdx.x == 0) c.counts[blockIdx.x] = n;
 }
 
@@ -345,23 +393,18 @@ __global__ __launch_bounds__(kPageThreads) void compact_pairs_kernel(Compact c) 
     const int64_t n = before[c.blocks.count];   // used pages
     // of them below page n: those of the blocks before its own, and of that block up to it
     const int64_t split = min(n / c.blocks.per, int64_t(c.blocks.count) - 1), s0 = split * c.blocks.per;
-    const int64_t low = before[split] + over_pages(c.refs, s0, n, [](int32_t r, int64_t) { return r != 0; }, [](int64_t, int) {});
-    __syncthreads();
+    const int64_t low = before[split] + over_pages(c.refs, s0, n, [](int32_t r) { return r != 0; }, [](int64_t, bool, int) {});
     const int64_t moves = n - low, half = c.num_pages / 2;
     const int64_t p0 = int64_t(blockIdx.x) * c.blocks.per, p1 = min(c.num_pages, p0 + c.blocks.per);
     const int64_t first = before[blockIdx.x];   // used pages before this block
-    over_pages(c.refs, p0, p1, [](int32_t r, int64_t) { return r != 0; },
-               [&](int64_t page, int i) {
-                   if (page >= n)
-                       c.copies[3 * (first + i - low)] = int32_t(page);
-                   else
-                       c.moved[page] = int32_t(page);
-               });
-    over_pages(c.refs, p0, p1, [](int32_t r, int64_t) { return r == 0; },
-               [&](int64_t page, int i) {
-                   c.moved[page] = int32_t(page);
-                   if (page < n) c.copies[3 * (p0 - first + i) + 1] = int32_t(page);
-               });
+    over_pages(c.refs, p0, p1, [](int32_t r) { return r != 0; }, [&](int64_t page, bool used, int i) {
+        if (used && page >= n) {
+            c.copies[3 * (first + i - low)] = int32_t(page);
+            return;
+        }
+        c.moved[page] = int32_t(page);
+        if (!used && page < n) c.copies[3 * (page - first - i) + 1] = int32_t(page);
+    });
     for (int64_t i = p0 / 2 + threadIdx.x; i < min(half, p1 / 2); i += kPageThreads) {
         c.copies[3 * i + 2] = i < moves ? c.page_size : 0;
         if (i >= moves) c.copies[3 * i] = c.copies[3 * i + 1] = -1;
@@ -387,11 +430,76 @@ __global__ __launch_bounds__(kPageThreads) void move_kernel(int32_t *pages, int6
     }
 }
 
+// All of it by one workgroup, E pages a thread: their counts stay in registers.
+template <int E>
+__global__ __launch_bounds__(kOneThreads) void compact_one_kernel(Compact c) {
+    extern __shared__ int32_t holes[];   // the free pages below page n, ascending
+    __shared__ int used_in[kOneWaves], free_in[kOneWaves];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, P = int(c.num_pages), p0 = wave * E * kWave + lane;
+    int r[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) r[i] = p0 + kWave * i < P ? c.refs[p0 + kWave * i] : 0;
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) mine += __builtin_popcountll(__ballot(r[i] != 0));
+    if (lane == 0) used_in[wave] = mine;
+    __syncthreads();
+    int n = 0, first = 0;   // used pages: all, and those before this wavefront's
+#pragma unroll
+    for (int w = 0; w < kOneWaves; ++w) {
+        first += w < wave ? used_in[w] : 0;
+        n += used_in[w];
+    }
+    int used = first, free = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int page = p0 + kWave * i;
+        const unsigned long long mask = __ballot(r[i] != 0), hole = __ballot(r[i] == 0 && page < n);
+        if (r[i] == 0 && page < n) holes[page - used - below(mask)] = page;
+        used += __builtin_popcountll(mask);
+        free += __builtin_popcountll(hole);
+    }
+    if (lane == 0) free_in[wave] = free;
+    __syncthreads();
+    int moves = 0;
+#pragma unroll
+    for (int w = 0; w < kOneWaves; ++w) moves += free_in[w];
+    used = first;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int page = p0 + kWave * i;
+        const unsigned long long mask = __ballot(r[i] != 0);
+        if (page < P) {
+            int to = page;
+            if (r[i] != 0 && page >= n) {
+                const int at = used + below(mask) - (n - moves);
+                to = holes[at];
+                c.copies[3 * at] = page;
+                c.copies[3 * at + 1] = to;
+                c.copies[3 * at + 2] = c.page_size;
+                c.refs[to] = r[i];
+                c.refs[page] = 0;
+            }
+            c.moved[page] = to;
+        }
+        used += __builtin_popcountll(mask);
+    }
+    for (int i = 3 * moves + int(threadIdx.x); i < 3 * (P / 2); i += kOneThreads) c.copies[i] = i % 3 == 2 ? 0 : -1;
+}
+
+template <int E>
+static hipError_t compact_one(const Compact &c, hipStream_t stream) {
+    hipLaunchKernelGGL(compact_one_kernel<E>, dim3(1), dim3(kOneThreads), size_t(c.num_pages / 2) * 4 + 4, stream, c);
+    return hipGetLastError();
+}
+
 size_t kv_compact_workspace(int64_t num_pages) { return size_t(page_blocks(num_pages).count) * 4; }
 
 hipError_t launch_kv_compact(int32_t *refs, int64_t num_pages, int32_t page_size, int32_t *copies, int32_t *moved,
                              void *workspace, hipStream_t stream) {
     const Compact c{refs, num_pages, page_size, copies, moved, page_blocks(num_pages), static_cast<int32_t *>(workspace)};
+    if (num_pages <= 4 * kOneThreads) return compact_one<4>(c, stream);
+    if (num_pages <= 8 * kOneThreads) return compact_one<8>(c, stream);
     hipLaunchKernelGGL(compact_count_kernel, dim3(unsigned(c.blocks.count)), dim3(kPageThreads), 0, stream, c);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(compact_pairs_kernel, dim3(unsigned(c.blocks.count)), dim3(kPageThreads), 0, stream, c);
