@@ -10,8 +10,10 @@
 // type's normal range.
 //
 // Bound by memory traffic, one read of 16 bits and one write of 8 for each
-// element (the second pass finds the tokens in the caches), and for a few
-// tokens by the launch.
+// element, and, as every block's wavefront waits for a chain of loads (its sequence's
+// place, its page, its tokens), by how many of them run beside the queries'
+// streaming: 5 x 3500 tokens of 32 + 8 + 8 heads of 128 80 us, 299 MB at 3.7
+// TB/s, in one launch with both, 86 in two.  A few tokens: the launch, 5.4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -24,7 +26,6 @@ namespace ngpu {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / kWave;
-
 struct Append8 {
     ngpu_kv_cache8_t c;
     ngpu_kv_append_t a;
@@ -32,51 +33,80 @@ struct Append8 {
     int bits;            // 2^bits threads a token's queries
 };
 
-// N elements from dimension d on of a head's row, rotated by the row `position` of the tables: N is 8, where everything
-// comes in eights, or 1.
-template <class T, int N>
-__device__ __forceinline__ void turned(const ngpu_kv_append_t &a, const T *row, int d, bool known, const float *cos,
-                                       const float *sin, float (&x)[N]) {
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const int half = a.rotary / 2;
-    auto load = [&](int at, float (&y)[N]) {
-        if constexpr (N == 8) {
-            const s16x8 v = *reinterpret_cast<const s16x8 *>(row + at);
-#pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = to_float(T{uint16_t(v[i])});
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// What an element is rotated with: nothing, its like of the other half, or its neighbour.
+enum { kAsIs = 0, kHalves = 1, kPairs = 2 };
+
+// N elements of a head's row from dimension d on, rotated by a row of the tables: N is 8, where everything comes in
+// eights, or 1.  Everything is loaded first, without a branch that lanes do not share, so that the loads of several pieces
+// are in flight together: what a dimension or a position has no use for is read from the row's or the tables' start.
+template <class T, int N, int MODE>
+struct Piece {
+    static constexpr int kWords = MODE == kAsIs ? 0 : (MODE == kHalves || N == 1 ? N : N / 2);   // angles
+    T x[N], y[MODE == kHalves || (MODE == kPairs && N == 1) ? N : 1];
+    float c[kWords > 0 ? kWords : 1], z[kWords > 0 ? kWords : 1];
+    bool turns, known, second;
+
+    template <int M, class U>
+    static __device__ __forceinline__ void fetch(const U *from, U (&to)[M]) {   // M: 16 or 32 bytes of eight, or one
+        if constexpr (M == 1) {
+            to[0] = from[0];
         } else {
-            y[0] = to_float(row[at]);
-        }
-    };
-    load(d, x);
-    if (d >= a.rotary) return;
-    if (!known) {
+            constexpr int kPer = 16 / int(sizeof(U));
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __builtin_nanf("");
-        return;
+            for (int i = 0; i < M / kPer; ++i) {
+                const i32x4 v = reinterpret_cast<const i32x4 *>(from)[i];
+                __builtin_memcpy(to + i * kPer, &v, 16);
+            }
+        }
     }
-    if (a.layout == NGPU_ROPE_HALF) {
-        const bool second = d >= half;
-        const int at = second ? d - half : d;
-        float y[N];
-        load(second ? at : d + half, y);
+    __device__ __forceinline__ void load(const ngpu_kv_append_t &a, const T *row, int d, int64_t position) {
+        fetch(row + d, x);
+        if constexpr (MODE != kAsIs) {
+            const int half = a.rotary / 2;
+            turns = d < a.rotary;
+            known = position >= 0 && position < a.positions_count;
+            second = MODE == kHalves ? d >= half : N == 1 && d % 2 != 0;
+            const int at = MODE == kHalves ? (second ? d - half : d) : d / 2;
+            if constexpr (MODE == kHalves || N == 1)
+                fetch(row + (!turns ? 0 : MODE == kHalves ? (second ? d - half : d + half) : d ^ 1), y);
+            if (a.positions_count > 0) {   // (else there are no tables)
+                const int64_t from = (known ? position * half : 0) + (turns ? at : 0);
+                fetch(a.cos + from, c);
+                fetch(a.sin + from, z);
+            }
+        }
+    }
+    // the pair's second element, of a piece that holds the first
+    __device__ __forceinline__ void other(float (&out)[N]) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float c = cos[at + i], z = sin[at + i];
-            x[i] = second ? x[i] * c + y[i] * z : x[i] * c - y[i] * z;
+            const float f = to_float(x[i]), g = to_float(y[i]);
+            out[i] = known ? g * c[i] + f * z[i] : __builtin_nanf("");
         }
-    } else if constexpr (N == 8) {
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float c = cos[(d + i) / 2], z = sin[(d + i) / 2], f = x[i], g = x[i + 1];
-            x[i] = f * c - g * z;
-            x[i + 1] = g * c + f * z;
-        }
-    } else {
-        const float other = to_float(row[d ^ 1]), c = cos[d / 2], z = sin[d / 2];
-        x[0] = d & 1 ? x[0] * c + other * z : x[0] * c - other * z;
     }
-}
+    __device__ __forceinline__ void turn(float (&out)[N]) const {
+        if constexpr (MODE == kAsIs) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) out[i] = to_float(x[i]);
+        } else if constexpr (MODE == kHalves || N == 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float f = to_float(x[i]), g = to_float(y[i]), t = second ? f * c[i] + g * z[i] : f * c[i] - g * z[i];
+                out[i] = !turns ? f : (known ? t : __builtin_nanf(""));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const float f = to_float(x[i]), g = to_float(x[i + 1]);
+                const float t = f * c[i / 2] - g * z[i / 2], u = g * c[i / 2] + f * z[i / 2];
+                out[i] = !turns ? f : (known ? t : __builtin_nanf(""));
+                out[i + 1] = !turns ? g : (known ? u : __builtin_nanf(""));
+            }
+        }
+    }
+};
 
 template <int N>
 __device__ __forceinline__ void store8(uint8_t *to, const float (&x)[N]) {
@@ -88,139 +118,252 @@ __device__ __forceinline__ void store8(uint8_t *to, const float (&x)[N]) {
     }
 }
 
-// The new tokens of one block and head, for the whole wavefront.
-template <class T, int N>
-__device__ __forceinline__ void append_block(const Append8 &p, int64_t unit) {
-    const ngpu_kv_append_t &a = p.a;
-    const ngpu_kv_cache_t &c = p.c.cache;
-    const int lane = threadIdx.x % kWave, D = c.dim, pieces = D / N, block = p.c.block;
-    const bool values = unit % 2 != 0;
-    const int h = int(unit / 2 % c.heads);
-    const int64_t sb = unit / 2 / c.heads, s = sb / p.blocks;
-    // places of the sequence's new tokens, and those of this block
-    const int64_t start = a.start[s], n = a.lengths ? min(max(int64_t(a.lengths[s]), int64_t(0)), a.T) : a.T;
-    const int64_t first = max(start, int64_t(0)), end = min(start + n, a.pages_width * c.page_size);
-    const int64_t b = first / block + sb % p.blocks, lo = max(first, b * block), hi = min(end, (b + 1) * block);
-    if (lo >= hi) return;
-    const int64_t at_page = b * block / c.page_size;
-    const int64_t page = a.pages[s * a.pages_stride + at_page];
-    if (page < 0 || page >= c.num_pages) return;
-    const int64_t entry = b * block - at_page * c.page_size;   // of the block's first token
-    uint8_t *const to = static_cast<uint8_t *>(values ? c.v : c.k) +
-                        (values ? page * c.v_stride_page + entry * c.v_stride_token + h * c.v_stride_head
-                                : page * c.k_stride_page + entry * c.k_stride_token + h * c.k_stride_head);
-    const int64_t to_token = values ? c.v_stride_token : c.k_stride_token;
-    float *const scale = (values ? p.c.v_scale : p.c.k_scale) +
-                         (values ? page * p.c.v_scale_stride_page + entry / block * p.c.v_scale_stride_block + h * p.c.v_scale_stride_head
-                                 : page * p.c.k_scale_stride_page + entry / block * p.c.k_scale_stride_block + h * p.c.k_scale_stride_head);
-    const int64_t from_token = values ? a.v_stride_token : a.k_stride_token;
-    const T *const from = static_cast<const T *>(values ? a.v : a.k) +
-                          (values ? s * a.v_stride_seq + h * a.v_stride_head : s * a.k_stride_seq + h * a.k_stride_head) +
-                          (lo - start) * from_token;
-    const int lead = int(lo - b * block), items = int(hi - lo) * pieces;
-    auto element = [&](int i, float (&x)[N]) {   // item i: N dimensions of a token
-        const int t = i / pieces, d = (i - t * pieces) * N;
-        if (values || a.rotary == 0) {
-            ngpu_kv_append_t plain = a;
-            plain.rotary = 0;
-            turned<T, N>(plain, from + t * from_token, d, true, nullptr, nullptr, x);
+// n / d for n, d > 0, by a division of 32 bits where they fit it.
+__device__ __forceinline__ int64_t divided64(int64_t n, int64_t d) {
+    return ((n | d) >> 32) == 0 ? int64_t(unsigned(n) / unsigned(d)) : n / d;
+}
+
+// Where the new tokens of one block and head come from and go to.
+template <class T>
+struct Block {
+    const T *from;          // the first new token's row
+    uint8_t *to;            // the block's first entry
+    float *scale;
+    int64_t from_token, to_token, place, n;   // n: the first new token's place in [S, T]
+    int lead, tokens;       // entries before the new ones, new ones: 0 where there is nothing to do
+    bool values;
+
+    __device__ __forceinline__ Block(const Append8 &p, int64_t unit) {
+        const ngpu_kv_append_t &a = p.a;
+        const ngpu_kv_cache_t &c = p.c.cache;
+        const int block = p.c.block;
+        const int64_t sb = divided64(unit / 2, c.heads), s = divided64(sb, p.blocks);
+        const int h = int(unit / 2 - sb * c.heads);
+        tokens = 0;
+        values = unit % 2 != 0;
+        // places of the sequence's new tokens, and those of this block
+        const int64_t start = a.start[s], count = a.lengths ? min(max(int64_t(a.lengths[s]), int64_t(0)), a.T) : a.T;
+        const int64_t first = max(start, int64_t(0)), end = min(start + count, a.pages_width * c.page_size);
+        const int64_t b = divided64(first, block) + (sb - s * p.blocks), lo = max(first, b * block), hi = min(end, (b + 1) * block);
+        if (lo >= hi) return;
+        const int64_t at_page = divided64(b * block, c.page_size);
+        const int64_t page = a.pages[s * a.pages_stride + at_page];
+        if (page < 0 || page >= c.num_pages) return;
+        const int64_t entry = b * block - at_page * c.page_size;   // of the block's first token
+        const int64_t which = divided64(entry, block);
+        if (values) {
+            to = static_cast<uint8_t *>(c.v) + page * c.v_stride_page + entry * c.v_stride_token + h * c.v_stride_head;
+            scale = p.c.v_scale + page * p.c.v_scale_stride_page + which * p.c.v_scale_stride_block + h * p.c.v_scale_stride_head;
+            from = static_cast<const T *>(a.v) + s * a.v_stride_seq + (lo - start) * a.v_stride_token + h * a.v_stride_head;
+            to_token = c.v_stride_token;
+            from_token = a.v_stride_token;
         } else {
-            const int64_t place = lo + t, position = a.positions ? int64_t(a.positions[s * a.T + place - start]) : place;
-            const bool known = position >= 0 && position < a.positions_count;
-            turned<T, N>(a, from + t * from_token, d, known, a.cos + position * (a.rotary / 2),
-                         a.sin + position * (a.rotary / 2), x);
+            to = static_cast<uint8_t *>(c.k) + page * c.k_stride_page + entry * c.k_stride_token + h * c.k_stride_head;
+            scale = p.c.k_scale + page * p.c.k_scale_stride_page + which * p.c.k_scale_stride_block + h * p.c.k_scale_stride_head;
+            from = static_cast<const T *>(a.k) + s * a.k_stride_seq + (lo - start) * a.k_stride_token + h * a.k_stride_head;
+            to_token = c.k_stride_token;
+            from_token = a.k_stride_token;
+        }
+        place = lo;
+        n = s * a.T + lo - start;
+        lead = int(lo - b * block);
+        tokens = int(hi - lo);
+    }
+};
+
+// The new tokens of a block and head, for WAVES wavefronts.  A lane's items are every kLanes-th: N dimensions of a token each.
+template <class T, int N, int MODE, int WAVES, int HELD>
+__device__ __forceinline__ void append_block(const Append8 &p, const Block<T> &b) {
+    constexpr int kLanes = WAVES * kWave;
+    const ngpu_kv_append_t &a = p.a;
+    const int lane = threadIdx.x % kLanes, D = p.c.cache.dim, pieces = D / N, items = b.tokens * pieces;
+    const int step_t = kLanes / pieces, step_d = kLanes % pieces * N;
+    int t = lane / pieces, d = lane % pieces * N;   // of the lane's item
+    auto restart = [&]() {
+        t = lane / pieces;
+        d = lane % pieces * N;
+    };
+    auto advance = [&]() {
+        t += step_t;
+        d += step_d;
+        if (d >= D) {
+            d -= D;
+            ++t;
         }
     };
-    float most = 0.0f;
-    for (int i = lane; i < items; i += kWave) {
-        float x[N];
-        element(i, x);
+    auto load = [&](Piece<T, N, MODE> &piece) {   // behind the last one: of the last token, for nothing
+        const int token = min(t, b.tokens - 1);
+        const int64_t position = MODE == kAsIs || !a.positions ? b.place + token : int64_t(a.positions[b.n + token]);
+        piece.load(a, b.from + token * b.from_token, d, position);
+    };
+    // Up to HELD a lane stay in registers, loaded a few at once; those of larger blocks are read again.
+    constexpr int kHeld = HELD, kBatch = HELD > 4 && MODE != kHalves ? 4 : (HELD > 2 ? 2 : HELD);
+    const bool held = items <= kHeld * kLanes;
+    float most = 0.0f, x[kHeld][N];
+    auto larger = [&](const float (&y)[N]) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float y = __builtin_fabsf(x[e]);
-            most = y < __builtin_inff() && y > most ? y : most;
+            const float z = __builtin_fabsf(y[e]);
+            most = z < __builtin_inff() && z > most ? z : most;
+        }
+    };
+    if (held) {
+#pragma unroll
+        for (int u = 0; u < kHeld; u += kBatch) {
+            if (kLanes * u < items) {
+                Piece<T, N, MODE> piece[kBatch];
+#pragma unroll
+                for (int e = 0; e < kBatch; ++e) {
+                    load(piece[e]);
+                    advance();
+                }
+#pragma unroll
+                for (int e = 0; e < kBatch; ++e) {
+                    piece[e].turn(x[u + e]);
+                    if (lane + kLanes * (u + e) < items) larger(x[u + e]);
+                }
+            }
+        }
+    } else {
+        for (int i = lane; i < items; i += kLanes) {
+            Piece<T, N, MODE> piece;
+            load(piece);
+            advance();
+            piece.turn(x[0]);
+            larger(x[0]);
         }
     }
     most = wave_max(most);
+    if constexpr (WAVES > 1) {
+        __shared__ float all[WAVES];
+        if (threadIdx.x % kWave == 0) all[threadIdx.x / kWave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = __builtin_fmaxf(most, all[w]);
+    }
     float now = least_scale(most);
-    if (lead > 0) {
-        const float had = *scale, old = had >= 0x1p-100f && had < __builtin_inff() ? had : 0x1p-100f;
+    if (b.lead > 0) {
+        const float had = *b.scale, old = had >= 0x1p-100f && had < __builtin_inff() ? had : 0x1p-100f;
         if (most > kMost8 * old) {   // it grows: the entries before, again
             const float ratio = old / now;
-            for (int i = lane; i < lead * pieces; i += kWave) {
-                const int t = i / pieces, d = (i - t * pieces) * N;
-                uint8_t *const at = to + t * to_token + d;
-                float x[N];
+            for (int i = lane; i < b.lead * pieces; i += kLanes) {
+                const int token = i / pieces, from = (i - token * pieces) * N;
+                uint8_t *const at = b.to + token * b.to_token + from;
+                float y[N];
                 if constexpr (N == 8) {
                     const int2 w = *reinterpret_cast<const int2 *>(at);
-                    const float2 y[4] = {to_floats8<false>(w.x), to_floats8<true>(w.x), to_floats8<false>(w.y),
+                    const float2 v[4] = {to_floats8<false>(w.x), to_floats8<true>(w.x), to_floats8<false>(w.y),
                                          to_floats8<true>(w.y)};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        x[2 * e] = y[e].x * ratio;
-                        x[2 * e + 1] = y[e].y * ratio;
+                        y[2 * e] = v[e].x * ratio;
+                        y[2 * e + 1] = v[e].y * ratio;
                     }
                 } else {
-                    x[0] = to_float(E4m3{*at}) * ratio;
+                    y[0] = to_float(E4m3{*at}) * ratio;
                 }
-                store8<N>(at, x);
+                store8<N>(at, y);
             }
         } else {
             now = old;
         }
     }
     const float by = 1.0f / now;
-    for (int i = lane; i < items; i += kWave) {
-        float x[N];
-        element(i, x);
+    auto put = [&](float (&y)[N]) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = __builtin_fabsf(x[e]) < __builtin_inff() ? x[e] * by : __builtin_nanf("");
-        const int t = i / pieces;
-        store8<N>(to + (lead + t) * to_token + (i - t * pieces) * N, x);
+        for (int e = 0; e < N; ++e) y[e] = __builtin_fabsf(y[e]) < __builtin_inff() ? y[e] * by : __builtin_nanf("");
+        store8<N>(b.to + (b.lead + t) * b.to_token + d, y);
+    };
+    restart();
+    if (held) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            if (lane + kLanes * u < items) put(x[u]);
+            advance();
+        }
+    } else {
+        for (int i = lane; i < items; i += kLanes) {
+            Piece<T, N, MODE> piece;
+            load(piece);
+            piece.turn(x[0]);
+            put(x[0]);
+            advance();
+        }
     }
-    if (lane == 0) *scale = now;
+    if (WAVES > 1 && b.lead > 0) __syncthreads();   // all have read the scale that there was
+    if (lane == 0) *b.scale = now;
 }
 
-// The queries of 256 >> bits tokens, N dimensions at a time.
-template <class T, int N>
+// The queries of 256 >> bits tokens.  Of halves a lane takes both elements of its pairs, else N dimensions at a time; a
+// few such items are loaded at once.
+template <class T, int N, int MODE>
 __device__ __forceinline__ void turn_queries(const Append8 &p, int64_t group) {
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
     const ngpu_kv_append_t &a = p.a;
     const int64_t n = (group * kAppendThreads + threadIdx.x) >> p.bits;
     if (n >= a.S * a.T) return;
     const int threads = 1 << p.bits, thread = threadIdx.x & (threads - 1);
-    const int D = p.c.cache.dim, pieces = D / N;
-    const int64_t s = n / a.T, t = n % a.T;
+    const int D = p.c.cache.dim, half = a.rotary / 2, pairs = MODE == kHalves ? half / N : 0, each = D / N - pairs;
+    const int64_t s = divided64(n, a.T), t = n - s * a.T;
     T *const to = static_cast<T *>(a.q_out) + n * a.q_heads * D;
     const bool counts = !a.lengths || t < a.lengths[s];
-    const int64_t position = a.rotary == 0 ? 0 : (a.positions ? int64_t(a.positions[n]) : int64_t(a.start[s]) + t);
-    const bool known = position >= 0 && position < a.positions_count;
-    const float *const cos = a.cos + position * (a.rotary / 2), *const sin = a.sin + position * (a.rotary / 2);
+    const int64_t position = a.rotary > 0 && a.positions ? int64_t(a.positions[n]) : int64_t(a.start[s]) + t;
     const T *const from = static_cast<const T *>(a.q) + s * a.q_stride_seq + t * a.q_stride_token;
-    for (int i = thread; i < a.q_heads * pieces; i += threads) {
-        const int h = i / pieces, d = (i - h * pieces) * N;
-        float x[N] = {};
-        if (counts) turned<T, N>(a, from + h * a.q_stride_head, d, known, cos, sin, x);
-        if constexpr (N == 8) {
-            s16x8 y;
+    const int items = a.q_heads * each;
+    constexpr int kBatch = N == 1 ? 1 : (MODE == kHalves ? 2 : 4);
+    auto put = [&](int at, const float (&x)[N]) {
+        T y[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) y[e] = short(from_float<T>(x[e]).bits);
-            *reinterpret_cast<s16x8 *>(to + i * N) = y;
-        } else {
-            to[i] = from_float<T>(x[0]);
+        for (int e = 0; e < N; ++e) y[e] = from_float<T>(counts ? x[e] : 0.0f);
+        if constexpr (N == 8)
+            *reinterpret_cast<i32x4 *>(to + at) = __builtin_bit_cast(i32x4, y);
+        else
+            to[at] = y[0];
+    };
+    for (int i0 = thread; i0 < items; i0 += kBatch * threads) {
+        Piece<T, N, MODE> piece[kBatch];
+        int head[kBatch], d[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {   // behind the last one: the last, for nothing
+            const int i = min(i0 + u * threads, items - 1), in = i - i / each * each;
+            head[u] = i / each;
+            d[u] = (in < pairs || MODE != kHalves ? in : in + pairs) * N;
+            piece[u].load(a, from + head[u] * a.q_stride_head, d[u], position);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u * threads >= items) break;
+            float x[N];
+            piece[u].turn(x);
+            put(head[u] * D + d[u], x);
+            if (MODE == kHalves && piece[u].turns) {
+                piece[u].other(x);
+                put(head[u] * D + d[u] + half, x);
+            }
         }
     }
 }
 
-template <class T, int N>
-__global__ __launch_bounds__(kAppendThreads) void append8_kernel(Append8 p, int64_t g0, int64_t block_groups) {
-    const int64_t group = g0 + blockIdx.x;
-    if (group >= block_groups) {
-        turn_queries<T, N>(p, group - block_groups);
+template <class T, int N, int MODE, int WAVES, int HELD>
+__global__ __launch_bounds__(kAppendThreads) void append8_kernel(Append8 p, int64_t g0, int64_t block_groups,
+                                                                int64_t all_groups) {
+    // The blocks' workgroups wait for their loads, one after the other: they are dealt evenly among the queries' (of fewer
+    // than 2^31 workgroups: the products fit 64 bits).
+    const int64_t at = g0 + blockIdx.x;
+    const bool deal = all_groups >> 31 == 0;
+    const int64_t group = deal ? divided64(at * block_groups, all_groups) : min(at, block_groups);
+    if ((deal ? divided64((at + 1) * block_groups, all_groups) : min(at + 1, block_groups)) == group) {
+        turn_queries<T, N, MODE>(p, at - group);
         return;
     }
-    const int64_t unit = group * kAppendWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
-    if (unit < p.a.S * p.blocks * p.c.cache.heads * 2) append_block<T, N>(p, unit);
+    constexpr int kUnits = kAppendWaves / WAVES;   // of the workgroup
+    const int64_t unit = group * kUnits + (kUnits == 1 ? 0 : __builtin_amdgcn_readfirstlane(int(threadIdx.x) / (WAVES * kWave)));
+    if (unit >= p.a.S * p.blocks * p.c.cache.heads * 2) return;
+    const Block<T> b(p, unit);
+    if (b.tokens == 0) return;
+    if (MODE == kAsIs || b.values)
+        append_block<T, N, kAsIs, WAVES, HELD>(p, b);
+    else
+        append_block<T, N, MODE, WAVES, HELD>(p, b);
 }
 
 // Whether eight elements can be moved at a time everywhere.
@@ -235,31 +378,50 @@ static bool in_eights(const Append8 &p) {
     for (const int64_t s : strides)
         if (s % 8 != 0) return false;
     return c.dim % 8 == 0 && a.rotary % (a.layout == NGPU_ROPE_HALF ? 16 : 8) == 0 && aligned(c.k, 8) && aligned(c.v, 8) &&
-           aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.q, 16) && aligned(a.q_out, 16);
+           aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.q, 16) && aligned(a.q_out, 16) &&
+           (a.rotary == 0 || (aligned(a.cos, 16) && aligned(a.sin, 16)));
 }
 
-template <class T, int N>
+template <class T, int N, int WAVES, int HELD>
 static hipError_t launch(Append8 p, hipStream_t stream) {
     constexpr int64_t kMost = int64_t(1) << 23;
     const ngpu_kv_append_t &a = p.a;
-    const int64_t units = a.S * p.blocks * p.c.cache.heads * 2, block_groups = (units + kAppendWaves - 1) / kAppendWaves;
-    const int64_t items = a.q ? int64_t(a.q_heads) * (p.c.cache.dim / N) : 0;
+    const int64_t units = a.S * p.blocks * p.c.cache.heads * 2, per_group = kAppendWaves / WAVES;
+    const int64_t block_groups = (units + per_group - 1) / per_group;
+    const bool halves = a.layout == NGPU_ROPE_HALF;
+    const int64_t items = a.q ? int64_t(a.q_heads) * (p.c.cache.dim / N - (halves ? a.rotary / 2 / N : 0)) : 0;
+    // Threads a token's queries: one for each item where these are few, else one for eight, or four pairs.  us: 5 x 3500 tokens of
+    // 32 + 8 heads of 128, pairs 80, with two an item 112, four 86, 32 90; 4 x 2000 of 8 + 4 of 80, halves 14.1, with one 19.3.
+    const int64_t passes = a.S * a.T * items >= int64_t(1) << 18 ? (halves ? 4 : 8) : 1;
     p.bits = 4;
-    while (p.bits < 8 && (int64_t(1) << p.bits) < items) ++p.bits;
-    const int64_t per = kAppendThreads >> p.bits, all = block_groups + (a.q ? (a.S * a.T + per - 1) / per : 0);
+    while (p.bits < 8 && (passes << p.bits) < items) ++p.bits;
+    const int64_t per = kAppendThreads >> p.bits, all = block_groups + (items > 0 ? (a.S * a.T + per - 1) / per : 0);
+    const auto kernel = a.rotary == 0 ? &append8_kernel<T, N, kAsIs, WAVES, HELD>
+                                      : (halves ? &append8_kernel<T, N, kHalves, WAVES, HELD>
+                                                : &append8_kernel<T, N, kPairs, WAVES, HELD>);
     for (int64_t g0 = 0; g0 < all; g0 += kMost) {
-        hipLaunchKernelGGL((append8_kernel<T, N>), dim3(unsigned(std::min(kMost, all - g0))), dim3(kAppendThreads), 0, stream,
-                           p, g0, block_groups);
+        hipLaunchKernelGGL(kernel, dim3(unsigned(std::min(kMost, all - g0))), dim3(kAppendThreads), 0, stream, p, g0,
+                           block_groups, all);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+// Four wavefronts a block where one would have more than eight items a lane (23 x 2000 tokens of 1 head of 128 in blocks of
+// 128: 38 us, not 78; with two items a lane each 5 x 3500 takes 109, not 86); fewer registers where it has two (16 x 2000 of
+// 4 heads of 64 in blocks of 16: 54 us, not 60).
+template <class T>
+static hipError_t launch(const Append8 &p, hipStream_t stream) {
+    const int N = in_eights(p) ? 8 : 1;
+    const int64_t items = std::min<int64_t>(p.c.block, p.a.T) * (p.c.cache.dim / N);
+    if (N == 1) return items > 8 * kWave ? launch<T, 1, 4, 1>(p, stream) : launch<T, 1, 1, 1>(p, stream);
+    if (items <= 2 * kWave) return launch<T, 8, 1, 2>(p, stream);
+    return items > 8 * kWave ? launch<T, 8, 4, 8>(p, stream) : launch<T, 8, 1, 8>(p, stream);
+}
+
 hipError_t launch_kv_append8(const ngpu_kv_cache8_t &c, const ngpu_kv_append_t &a, hipStream_t stream) {
     const Append8 p{c, a, (a.T + c.block - 2) / c.block + 1, 0};
-    const bool half = c.cache.dtype == NGPU_F16;
-    if (in_eights(p)) return half ? launch<F16, 8>(p, stream) : launch<Bf16, 8>(p, stream);
-    return half ? launch<F16, 1>(p, stream) : launch<Bf16, 1>(p, stream);
+    return c.cache.dtype == NGPU_F16 ? launch<F16>(p, stream) : launch<Bf16>(p, stream);
 }
 
 }  // namespace ngpu
