@@ -332,6 +332,33 @@ struct AttendTile {
     }
 };
 
+// The kernel's arguments for what follows its loop.  Of a cache in 8 bits they are read again: beside what the loop needs
+// they do not fit the scalar registers.
+template <class C>
+struct LastArgs {
+    const AttendOf<C> &p;
+    const AttendPlan &plan;
+    __device__ __forceinline__ LastArgs(const AttendOf<C> &p, const AttendPlan &plan) : p(p), plan(plan) {}
+};
+template <>
+struct LastArgs<E4m3> {
+    struct Args {   // as they lie in memory
+        Attend8 p;
+        AttendPlan plan;
+    };
+    const Attend8 &p;
+    const AttendPlan &plan;
+    __device__ __forceinline__ LastArgs(const Attend8 &, const AttendPlan &) : LastArgs(*read()) {}
+
+private:
+    __device__ __forceinline__ explicit LastArgs(const Args &a) : p(a.p), plan(a.plan) {}
+    static __device__ __forceinline__ const Args *read() {
+        const Args *args = (const Args *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(args));
+        return args;
+    }
+};
+
 // Work `w` of the plan, for WR wavefronts with LDS from `lds0` on.
 template <class T, class C, int DK, int RT, int WR>
 __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendPlan &plan, unsigned w, unsigned lds0) {
@@ -479,6 +506,16 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
         if (WR > 1) asm volatile("s_barrier" ::: "memory");
     }
     const bool whole_rows = (A::kEight || whole_head) && k_token < (1u << 21) && v_token < (1u << 21);
+    // (in 8 bits) the scales that this lane loads: its key's, or that key's value's; strides in vector registers
+    const float *scales = nullptr;
+    uint64_t scales_page = 0, scales_block = 0;
+    if constexpr (A::kEight) {
+        const bool values = lane >= A::kLoad;
+        scales = values ? p.v_scale + h * p.v_scale_head : p.k_scale + h * p.k_scale_head;
+        scales_page = uint64_t(values ? p.v_scale_page : p.k_scale_page);
+        scales_block = uint64_t(values ? p.v_scale_block : p.k_scale_block);
+        asm volatile("" : "+v"(scales), "+v"(scales_page), "+v"(scales_block));
+    }
     const char *no_data = reinterpret_cast<const char *>(kNoData);
     asm volatile("" : "+s"(no_data));   // its address is loaded once
     unsigned valid = 0;   // keys that exist among those this wavefront loaded last
@@ -502,12 +539,9 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
             }
         };
         // the scales of this wavefront's keys, then values, a lane each; 1 where there is no key
-        auto load_scales = [&](int64_t page, unsigned entry, bool there) {
+        auto load_scales = [&](unsigned page, unsigned entry, bool there) {
             if constexpr (A::kEight) {
-                const bool values = lane >= A::kLoad;
-                const int64_t block = divided(entry, p.block, p.block_magic);
-                const float *from = values ? p.v_scale + page * p.v_scale_page + block * p.v_scale_block + h * p.v_scale_head
-                                           : p.k_scale + page * p.k_scale_page + block * p.k_scale_block + h * p.k_scale_head;
+                const float *from = scales + uint64_t(page) * scales_page + uint64_t(divided(entry, p.block, p.block_magic)) * scales_block;
                 if (lane < 2 * A::kLoad)
                     load_word_to_lds(there ? from : &kNoScale, lds0 + unsigned(stage * A::kStage + 2 * A::kKeys * A::kPitch +
                                                                               wave * 8 * A::kLoad));
@@ -526,7 +560,7 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
             const uint64_t entry = is ? j - page_index(j) * page_size : 0u, pg = is ? unsigned(p0) : 0u;
             const char *kb = k_head + (pg * k_page + entry * k_token) * 16;
             const char *vb = v_head + (pg * v_page + entry * v_token) * 16;
-            load_scales(int64_t(pg), unsigned(entry) + unsigned(lane % A::kLoad), is && lane % A::kLoad < left);
+            load_scales(unsigned(pg), unsigned(entry) + unsigned(lane % A::kLoad), is && lane % A::kLoad < left);
             if (valid == kAll && whole_rows) {
 #pragma unroll
                 for (int u = 0; u < A::kLoads; ++u) load_whole(u, kb, vb);
@@ -555,7 +589,7 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
         const bool is = page >= 0 && page < p.c.num_pages;
         valid = unsigned(__ballot(is)) & kAll;
         put_mask();
-        load_scales(is ? page : 0, entry, is);
+        load_scales(is ? unsigned(page) : 0u, entry, is);
         if (valid == kAll && whole_rows && page_size % A::kPerLoad == 0) {   // a load's keys lie in one page
             unsigned e = j - page_index(j) * page_size;
             const char *kb = nullptr, *vb = nullptr;   // of the page's entry 0, for this load's offsets
@@ -866,29 +900,30 @@ if constexpr (A::kEight) {
         stage = 1 - stage;
     }
 
+    const LastArgs<C> last(p, plan);
     float total[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) total[r] = row_sum(sum[r]);
-    const int64_t all_rows = a.S * a.T * a.q_heads;
-    const int part = (own ? plan.prefix.parts : 0) + split;
+    const int64_t all_rows = last.p.a.S * last.p.a.T * last.p.a.q_heads;
+    const int part = (own ? last.plan.prefix.parts : 0) + split;
     if (one_by_one) {
         for (unsigned i = 0; i < 16 * RT; ++i) {
             const unsigned row = unsigned(block) * A::kRows + unsigned(wave) * 16 * RT + i;
             if (row >= rows) break;
             const int t = int(row / unsigned(rep)), head = h * rep + int(row % unsigned(rep));   // (own: one sequence)
-            const int nq = int(query_length(a, s0)), seen = max(0, min(count, count - nq + t + 1));
+            const int nq = int(query_length(last.p.a, s0)), seen = max(0, min(count, count - nq + t + 1));
             RowPart<T, C> r;
-            r.load(p, s0, t, head, lane);
+            r.load(last.p, s0, t, head, lane);
             const unsigned end = min(unsigned(tile1) * A::kKeys, unsigned(seen));
-            for (unsigned j = unsigned(tile0) * A::kKeys; j < end; ++j) r.take(p, table, j, h, lane);
-            const int64_t out = (int64_t(s0) * T_ + t) * a.q_heads + head;
-            if (plan.parts > 1) {
-                if (lane == 0) plan.stats[part * all_rows + out] = make_float2(r.m, r.sum);
+            for (unsigned j = unsigned(tile0) * A::kKeys; j < end; ++j) r.take(last.p, table, j, h, lane);
+            const int64_t out = (int64_t(s0) * T_ + t) * last.p.a.q_heads + head;
+            if (last.plan.parts > 1) {
+                if (lane == 0) last.plan.stats[part * all_rows + out] = make_float2(r.m, r.sum);
 #pragma unroll
                 for (int e = 0; e < r.kDims; ++e)
-                    if (const int d = lane + kWave * e; d < D) plan.sums[(part * all_rows + out) * D + d] = r.o[e];
+                    if (const int d = lane + kWave * e; d < D) last.plan.sums[(part * all_rows + out) * D + d] = r.o[e];
             } else {
-                r.finish(p, out, lane, t < nq);
+                r.finish(last.p, out, lane, t < nq);
             }
         }
         return;
@@ -898,20 +933,20 @@ if constexpr (A::kEight) {
         const unsigned i = unsigned(block) * A::kRows + (wave * RT + r) * 16 + col, token = i / unsigned(rep);
         if (i >= rows) continue;
         const int s = s0 + int(token / unsigned(T_)), t = int(token % unsigned(T_));
-        const int64_t row = int64_t(s * T_ + t) * a.q_heads + h * rep + int(i - token * unsigned(rep));
-        if (plan.parts > 1) {
-            if (quad == 0) plan.stats[part * all_rows + row] = make_float2(m[r], total[r]);
+        const int64_t row = int64_t(s * T_ + t) * last.p.a.q_heads + h * rep + int(i - token * unsigned(rep));
+        if (last.plan.parts > 1) {
+            if (quad == 0) last.plan.stats[part * all_rows + row] = make_float2(m[r], total[r]);
             if (total[r] == 0.0f) continue;
-            float *dst = plan.sums + (part * all_rows + row) * D;
+            float *dst = last.plan.sums + (part * all_rows + row) * D;
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d)
                 if (const int at = 16 * d + 4 * quad; at < D) *reinterpret_cast<f32x4 *>(dst + at) = o[r][d];
         } else {
-            const bool any = t < query_length(a, s) && total[r] != 0.0f;   // (a NaN sum too)
-            if (a.lse && quad == 0)
-                a.lse[row] = any ? (m[r] == -__builtin_inff() ? total[r] : m[r] * 0.69314718056f + logf(total[r]))
+            const bool any = t < query_length(last.p.a, s) && total[r] != 0.0f;   // (a NaN sum too)
+            if (last.p.a.lse && quad == 0)
+                last.p.a.lse[row] = any ? (m[r] == -__builtin_inff() ? total[r] : m[r] * 0.69314718056f + logf(total[r]))
                                         : -__builtin_inff();
-            T *dst = static_cast<T *>(a.out) + row * D;
+            T *dst = static_cast<T *>(last.p.a.out) + row * D;
             const float f = 1.0f / total[r];
 #pragma unroll
             for (int d = 0; d < A::kTiles; ++d) {
