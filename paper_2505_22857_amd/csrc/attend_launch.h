@@ -223,11 +223,12 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
         // Workgroups: 2 a CU, not 4, where several wavefronts share the keys (us: 4 sequences of 500 tokens that see 3500,
         // 32 / 8 heads of 128 129, not 164; one of 64 that sees 8000 31, not 49), and beside prefixes whose rows
         // take several, where own tokens wait for memory while those compute (64 sequences of one token that see 300, 2048
-        // of prefix 60, not 68).
+        // of prefix 60, not 68).  In 8 bits 8, whose tiles are computed as long and read half as long (16 sequences of one token
+        // that see 4000, 32 / 8 heads of 128: 27 us, 30 with 6, 36 with 4).
         cut_rows(prefix_rows, r.steps, r.prefix_tiles, r.prefix_waves, r.plan.prefix.blocks);
         cut_rows(a.T * rep, r.steps, r.own_tiles, r.own_waves, r.plan.own.blocks);
         const int64_t keys = a.pages_width * c.page_size, have = a.S * c.heads * r.plan.own.blocks;
-        r.plan.own = cut(a.S * c.heads, a.T * rep, keys, (r.prefix_waves > 1 || r.own_waves == 4 ? 2 : 4) * kCus,
+        r.plan.own = cut(a.S * c.heads, a.T * rep, keys, (r.prefix_waves > 1 || r.own_waves == 4 ? 2 : kEight ? 8 : 4) * kCus,
                          r.own_tiles, r.own_waves);
         // One workgroup a block of rows would have the last block's be twice as long as the mean: one sequence of
         // 8192 tokens that see each other, 8 heads of 64: 280 us, in two splits 178.
@@ -237,7 +238,7 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     if (a.G > 0) {
         const int64_t left = per_cu * kCus - r.plan.own.works();
         r.plan.prefix = cut(a.G * c.heads, prefix_rows, a.prefix_width * c.page_size,
-                            std::max<int64_t>(left, 2 * kCus), r.prefix_tiles, r.prefix_waves);
+                            std::max<int64_t>(left, (kEight ? 3 : 2) * kCus), r.prefix_tiles, r.prefix_waves);
         if (r.prefix_waves == 4)
             r.plan.prefix = cut(a.G * c.heads, prefix_rows, a.prefix_width * c.page_size, 2 * kCus,
                                 r.prefix_tiles, r.prefix_waves);

@@ -116,9 +116,8 @@ struct AttendPlan {
     float2 *stats;       // [parts, rows] {maximum in log2, sum of weights}
 };
 
-// 16 bytes of zeros, which stand for keys and dimensions that do not exist.
+// 16 bytes of zeros, which stand for keys and dimensions that do not exist, and for such keys' scales.
 static __device__ __attribute__((aligned(16))) unsigned kNoData[4];
-static __device__ float kNoScale = 1.0f;
 
 // One row's running maximum (in log2) and sums, a wavefront's lanes holding every
 // 64th dimension: for what the matrix instructions do not take.
@@ -538,12 +537,12 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
                 if (value_piece(u) < used) load_to_lds<A::kOnce>(vb, v_off[u], v_to);
             }
         };
-        // the scales of this wavefront's keys, then values, a lane each; 1 where there is no key
+        // the scales of this wavefront's keys, then values, a lane each; 0 where there is no key
         auto load_scales = [&](unsigned page, unsigned entry, bool there) {
             if constexpr (A::kEight) {
                 const float *from = scales + uint64_t(page) * scales_page + uint64_t(divided(entry, p.block, p.block_magic)) * scales_block;
                 if (lane < 2 * A::kLoad)
-                    load_word_to_lds(there ? from : &kNoScale, lds0 + unsigned(stage * A::kStage + 2 * A::kKeys * A::kPitch +
+                    load_word_to_lds(there ? static_cast<const void *>(from) : no_data, lds0 + unsigned(stage * A::kStage + 2 * A::kKeys * A::kPitch +
                                                                               wave * 8 * A::kLoad));
             }
         };
