@@ -95,6 +95,29 @@ def test_all_alike():
             assert got[0][0].tolist() == list(range(64)) and not got[1].any()
 
 
+@pytest.mark.parametrize("V,W", [(256, 16), (250, 9), (512, 8), (300, 5), (1024, 4), (1000, 3), (2048, 2), (1900, 1)])
+def test_one_launch(V, W):
+    """All that one launch takes, up to its most wavefronts: sums that differ, that are few, and that are one."""
+    m = model(V, 3, True)
+    for k in (1, W, 64):
+        check(*m, *inputs(m[0], 5, W, "aed", seed=k, ended=0.15, empty=0.1), k, "aed")
+    check(*m, *inputs(m[0], 4, W, "aed", seed=3, ended=0.1, coarse=True), 40, "aed", lam=0.0)
+    asr, states = np.full((2, W, V + 1), -2.0, np.float32), uniform_states(m[0], 2 * W, seed=1).reshape(2, W)
+    scores, last = np.full((2, W), -7.0, np.float32), np.zeros((2, W), np.int32)
+    check(*m, asr, states, scores, last, 64, "aed", lam=0.0)
+    scores[:, 0], asr[0, W - 1, 17:19], asr[1, 0, V] = -9.0, -1.5, 3.0   # a few above those that are alike
+    check(*m, asr, states, scores, last, 64, "aed", lam=0.0)
+    last[0] = V                                                         # nothing but ended ones
+    check(*m, asr, states, scores, last, 64, "aed", lam=0.0)
+
+
+@pytest.mark.parametrize("V,W", [(200, 8), (200, 9), (500, 4), (500, 5), (1000, 2), (1000, 3), (1500, 1), (1500, 2)])
+def test_more_utterances_than_compute_units(V, W):
+    m = model(V)
+    for B in (256, 257):
+        check(*m, *inputs(m[0], B, W, "transducer", seed=B), W, "transducer")
+
+
 def test_infinities_and_nan():
     m = model(300, 3, True)
     asr, states, scores, last = inputs(m[0], 6, 4, "aed", seed=2, ended=0.2)
