@@ -9,6 +9,7 @@
 #include <atomic>
 
 #include "attend_tile.h"
+#include "launch.h"
 
 namespace ngpu {
 
@@ -251,19 +252,6 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     r.plan.sums = reinterpret_cast<float *>(workspace);
     r.plan.stats = reinterpret_cast<float2 *>(workspace + size_t(r.plan.parts) * size_t(rows) * c.dim * 4);
     return r;
-}
-
-// More LDS than a launch has by default, asked for once a device (bits of `devices`).
-template <class K>
-hipError_t allow_lds(K *kernel, int bytes, std::atomic<uint64_t> &devices) {
-    int device;
-    if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
-    const uint64_t bit = uint64_t(1) << device % 64;
-    if (device < 64 && (devices.load(std::memory_order_relaxed) & bit)) return hipSuccess;
-    const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == hipSuccess && device < 64) devices.fetch_or(bit, std::memory_order_relaxed);
-    return e;
 }
 
 template <class T, class C, int DK, int RT, int WR>

@@ -29,6 +29,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "launch.h"
 #include "reduce.h"
 
 namespace ngpu {
@@ -571,14 +572,19 @@ __global__ __launch_bounds__(kWholeWaves * kWave) void beam_whole_kernel(DevTrie
     }
 }
 
-template <int HW>
+template <int HW, int NT>
 static hipError_t whole(const DevTrie &t, const Beam &p, hipStream_t stream) {
-    constexpr int NT = 4;
     constexpr int64_t kMost = int64_t(1) << 22;
     const int waves = p.a.W * HW;
     const size_t lds = sizeof(WholeMeet) + std::max(size_t(kWholeList) * 12, size_t(waves) * kWave * NT * sizeof(i32x2));
-    static_assert(sizeof(WholeMeet) + kWholeWaves * kWave * NT * sizeof(i32x2) <= 65536, "a launch's LDS");
+    constexpr int kMostLds = sizeof(WholeMeet) + kWholeWaves * kWave * NT * sizeof(i32x2);
     const bool full = t.vocab_size == HW * kWave * NT;
+    if (lds > 65536) {
+        static std::atomic<uint64_t> devices[2];
+        const hipError_t e = full ? allow_lds(&beam_whole_kernel<HW, NT, true>, kMostLds, devices[1])
+                                  : allow_lds(&beam_whole_kernel<HW, NT, false>, kMostLds, devices[0]);
+        if (e != hipSuccess) return e;
+    }
     for (int64_t b0 = 0; b0 < p.a.B; b0 += kMost) {
         const dim3 grid(unsigned(std::min(kMost, p.a.B - b0))), block(waves * kWave);
         if (full)
@@ -619,18 +625,19 @@ static hipError_t select(const Beam &p, hipStream_t stream) {
 
 // Whether one launch takes the call: where each lane has four tokens of at most 16 wavefronts.  64 utterances take 5.0
 // against 7.4 us in two launches (4 hypotheses, 128 tokens), 6.4 against 8.6 (8, 512) and 6.3 against 8.0 (4, 1024); with
-// eight tokens a lane, 16 hypotheses of 512 or 8 of 1024 gain nothing (11.3 against 9.5, 9.4 against 8.8).  Past a workgroup
-// a CU small ones still gain, 600 utterances of 4 hypotheses 6.0 against 8.9 (128 tokens) and 7.8 against 9.5 (512), larger
+// eight tokens a lane, 16 hypotheses of 512 gain nothing (11.3 against 9.5), while 8 of 1024 are even on the card
+// (9.4 against 8.8; 128 utterances 9.7 against 10.1) and spare the caller a launch, 2 us.  Past a workgroup a CU
+// small ones still gain, 600 utterances of 4 hypotheses 6.0 against 8.9 (128 tokens) and 7.8 against 9.5 (512), larger
 // ones do not: 8 hypotheses of 512 tokens 17.8 against 12.0.
 static bool takes_whole(int64_t B, int W, int V) {
     const int range = V <= 256 ? 1 : V <= 512 ? 2 : V <= 1024 ? 4 : 8;   // wavefronts a hypothesis, of 256 tokens
-    return V <= 2048 && W * range <= (B <= 256 ? kWholeWaves : 8);
+    return V <= 2048 && (W * range <= (B <= 256 ? kWholeWaves : 8) || (B <= 256 && W <= 8 && V <= 1024));
 }
 static hipError_t whole(const DevTrie &t, const Beam &p, int V, hipStream_t stream) {
-    if (V <= 256) return whole<1>(t, p, stream);
-    if (V <= 512) return whole<2>(t, p, stream);
-    if (V <= 1024) return whole<4>(t, p, stream);
-    return whole<8>(t, p, stream);
+    if (V <= 256) return whole<1, 4>(t, p, stream);
+    if (V <= 512) return whole<2, 4>(t, p, stream);
+    if (V <= 1024) return p.a.W <= 4 ? whole<4, 4>(t, p, stream) : whole<2, 8>(t, p, stream);
+    return whole<8, 4>(t, p, stream);
 }
 
 // Wavefronts and tokens per lane of a hypothesis: the top-k kernel's rules for k up to 64.

@@ -95,7 +95,8 @@ def test_all_alike():
             assert got[0][0].tolist() == list(range(64)) and not got[1].any()
 
 
-@pytest.mark.parametrize("V,W", [(256, 16), (250, 9), (512, 8), (300, 5), (1024, 4), (1000, 3), (2048, 2), (1900, 1)])
+@pytest.mark.parametrize("V,W", [(256, 16), (250, 9), (512, 8), (300, 5), (1024, 4), (1000, 3), (2048, 2), (1900, 1),
+                                 (1024, 8), (900, 7), (1000, 5)])
 def test_one_launch(V, W):
     """All that one launch takes, up to its most wavefronts: sums that differ, that are few, and that are one."""
     m = model(V, 3, True)
@@ -111,7 +112,8 @@ def test_one_launch(V, W):
     check(*m, asr, states, scores, last, 64, "aed", lam=0.0)
 
 
-@pytest.mark.parametrize("V,W", [(200, 8), (200, 9), (500, 4), (500, 5), (1000, 2), (1000, 3), (1500, 1), (1500, 2)])
+@pytest.mark.parametrize("V,W", [(200, 8), (200, 9), (500, 4), (500, 5), (1000, 2), (1000, 3), (1000, 8), (1500, 1),
+                                 (1500, 2)])
 def test_more_utterances_than_compute_units(V, W):
     m = model(V)
     for B in (256, 257):
