@@ -350,7 +350,8 @@ size_t kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages) {
 hipError_t launch_kv_fork(const ngpu_kv_fork_t &a, void *workspace, hipStream_t stream) {
     const Fork f = fork_of(a, static_cast<char *>(workspace), nullptr);
     const int64_t R = a.G * a.K, rows = R + a.G * a.W;
-    if (R > 0 && R <= kOneThreads && rows * ((a.width + kWave - 1) / kWave) <= kOneRows && a.num_pages <= kOnePages) {
+    const int64_t steps = std::max<int64_t>((a.width + kWave - 1) / kWave, 1);   // of a wavefront over a row
+    if (R > 0 && R <= kOneThreads && rows * steps <= kOneRows && a.num_pages <= kOnePages) {
         hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, f);
         return hipGetLastError();
     }

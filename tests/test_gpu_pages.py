@@ -154,6 +154,14 @@ def test_large_pools(P):
     assert after[1].tolist() == [0, 0, 0, -1 if len(free) <= 302 else 0, 0]
 
 
+def test_tables_without_entries():
+    pages, lengths, refs = np.zeros((6400, 0), np.int32), np.arange(6400, dtype=np.int32), np.zeros(9, np.int32)
+    parents = np.arange(40, dtype=np.int32).repeat(100).reshape(100, 40)
+    for tokens in (0, 1):
+        after = check_fork(pages, lengths, parents, refs, 4, tokens)
+        assert (after[1] == -tokens).all()
+
+
 def test_many_rows():
     """More rows than a block of them, in groups that span two."""
     rng = np.random.default_rng(5)
