@@ -495,7 +495,7 @@ class NgpuLM:
                     _check(r)
                 return r
         import torch
-        from .serving import _need, _on
+        from .serving import _need, _on, _untracked
         if not hasattr(asr, "is_cuda") or not asr.is_cuda or asr.dtype is not torch.float32:
             raise TypeError("asr must be a float32 device tensor")
         if asr.dim() != 3:
@@ -512,6 +512,7 @@ class NgpuLM:
                       _need(states, "states", dev, torch.int32, (B, W)),
                       _need(scores, "scores", dev, torch.float32, (B, W)),
                       _need(last, "last", dev, torch.int32, (B, W)))
+        _untracked(asr=asr, scores=scores)
         with _on(dev, stream) as handle:
             tokens, parents, after = (torch.empty((B, k), dtype=torch.int32, device=dev) for _ in range(3))
             best = torch.empty((B, k), dtype=torch.float32, device=dev)

@@ -501,7 +501,7 @@ PyObject *beam_step(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     if (a[6] != Py_None && (!whole(a[6], k) || k < 1 || k > NGPU_LM_MAX_BEAMS)) return none();
     Input states, scores, last;
     if (!states.set(a[4], at::kInt, {B, W}, *asr, false) || !scores.set(a[5], at::kFloat, {B, W}, *asr, false) ||
-        !last.set(a[7], at::kInt, {B, W}, *asr, false, true))
+        !last.set(a[7], at::kInt, {B, W}, *asr, false, true) || tracked(asr) || tracked(scores.t))
         return none();
     const auto ints = states.t->options();
     const at::Tensor tokens = at::empty({B, k}, ints), parents = at::empty({B, k}, ints), after = at::empty({B, k}, ints),

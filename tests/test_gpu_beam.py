@@ -208,6 +208,12 @@ def test_empty_batch_and_refusals():
         lm.beam_step(asr, 0.5, st.long(), sc)
     with pytest.raises(TypeError):
         lm.beam_step(asr.half(), 0.5, st, sc)
+    for tracked in ((asr.clone().requires_grad_(), sc), (asr, sc.clone().requires_grad_())):
+        for stream in (None, torch.cuda.current_stream()):
+            with pytest.raises(TypeError, match="gradient"):
+                lm.beam_step(tracked[0], 0.5, st, tracked[1], stream=stream)
+        with torch.no_grad():
+            lm.beam_step(tracked[0], 0.5, st, tracked[1])
     with pytest.raises(TypeError, match="stride"):
         lm.beam_step(z(2, 3, 202, device="cuda")[:, :, ::2], 0.5, st, sc)
     with pytest.raises(TypeError):
