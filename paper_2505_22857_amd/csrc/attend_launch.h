@@ -229,8 +229,13 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
         cut_rows(prefix_rows, r.steps, r.prefix_tiles, r.prefix_waves, r.plan.prefix.blocks);
         cut_rows(a.T * rep, r.steps, r.own_tiles, r.own_waves, r.plan.own.blocks);
         const int64_t keys = a.pages_width * c.page_size, have = a.S * c.heads * r.plan.own.blocks;
-        r.plan.own = cut(a.S * c.heads, a.T * rep, keys, (r.prefix_waves > 1 || r.own_waves == 4 ? 2 : kEight ? 8 : 4) * kCus,
-                         r.own_tiles, r.own_waves);
+        const int per = r.prefix_waves > 1 || r.own_waves == 4 ? (kEight && r.prefix_waves == 4 ? 4 : 2) : kEight ? 8 : 4;
+        r.plan.own = cut(a.S * c.heads, a.T * rep, keys, per * kCus, r.own_tiles, r.own_waves);
+        // In 8 bits also one for 512 tokens beside such prefixes, as one wavefront would take longer over more than those do:
+        // 4 x 12 sequences of one token that see up to 3000 of their own 55 us, not 148; 32 x 10 that see 1500 and 1500 of
+        // prefix 111, not 122; with one for 256 126.
+        if (kEight && r.prefix_waves > 1 && r.own_waves == 1)
+            r.plan.own.splits = int(std::max<int64_t>(r.plan.own.splits, std::min<int64_t>((keys + 511) / 512, 128)));
         // One workgroup a block of rows would have the last block's be twice as long as the mean: one sequence of
         // 8192 tokens that see each other, 8 heads of 64: 280 us, in two splits 178.
         if (r.own_waves == 4 && 2 * a.T > keys && have <= 2 * kCus) r.plan.own.splits = std::max(r.plan.own.splits, 2);
@@ -279,15 +284,14 @@ hipError_t launch_tile(const AttendOf<C> &p, const AttendPlan &plan, int tiles, 
 template <class T, class C, int DK, int WR>
 hipError_t launch_both(const AttendOf<C> &p, const AttendPlan &plan, hipStream_t stream) {
     constexpr int RT = DK <= 4 ? 2 : 1;
-    using A = AttendTile<T, C, DK, RT, WR>;
     constexpr int64_t kMost = int64_t(1) << 23;   // workgroups a launch
     static std::atomic<uint64_t> devices;
-    if (const hipError_t e = allow_lds(&attend_both_kernel<T, C, DK, RT, WR>, A::kLds, devices); e != hipSuccess) return e;
-    constexpr int kWaves = kOwnWaves<T, C, DK, RT, WR>;
+    constexpr int kLds = kBothLds<T, C, DK, RT, WR>, kWaves = kOwnWaves<T, C, DK, RT, WR>;
+    if (const hipError_t e = allow_lds(&attend_both_kernel<T, C, DK, RT, WR>, kLds, devices); e != hipSuccess) return e;
     const int64_t own = (plan.own.works() + kWaves - 1) / kWaves, all = own + plan.prefix.works();
     for (int64_t b0 = 0; b0 < all; b0 += kMost) {
         hipLaunchKernelGGL((attend_both_kernel<T, C, DK, RT, WR>), dim3(unsigned(std::min(kMost, all - b0))),
-                           dim3(64 * WR), A::kLds, stream, p, plan, unsigned(b0), unsigned(own));
+                           dim3(64 * WR), kLds, stream, p, plan, unsigned(b0), unsigned(own));
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -721,22 +721,22 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
                 }
         } else {
 #pragma unroll
-        for (int i = 0; i < kKeysAhead; ++i) load_keys(i);
+            for (int i = 0; i < kKeysAhead; ++i) load_keys(i);
 #pragma unroll
-        for (int i = 0; i < N * DK; ++i) {
-            if (i + kKeysAhead < N * DK) load_keys(i + kKeysAhead);
-            if (i + 1 == N * DK) {
+            for (int i = 0; i < N * DK; ++i) {
+                if (i + kKeysAhead < N * DK) load_keys(i + kKeysAhead);
+                if (i + 1 == N * DK) {
 #pragma unroll
-                for (int j = 0; j < kValuesAhead; ++j) load_values(j);
+                    for (int j = 0; j < kValuesAhead; ++j) load_values(j);
+                }
+                const int c = i / DK, k = i % DK;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        x[r][2 * c + u] = M::mul(kx[i % (kKeysAhead + 1)][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const int c = i / DK, k = i % DK;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    x[r][2 * c + u] = M::mul(kx[i % (kKeysAhead + 1)][u], q[r][k], k == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : x[r][2 * c + u]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
         }
         const bool some_rows = own && key0 > least - A::kKeys;   // some rows do not see some of the keys
         bool all = !some_rows;
@@ -758,7 +758,7 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
                     __builtin_amdgcn_sched_barrier(0);
                 }
             if (some_rows) {
-if constexpr (A::kEight) {
+                if constexpr (A::kEight) {
                     unsigned nan = 0;   // a byte whose lower bits are all set
                     for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
                         const u32x4 v = *lds_at<u32x4>(tile_at + A::kKeys * A::kPitch + 16 * i) & 0x7f7f7f7fu;
@@ -776,17 +776,17 @@ if constexpr (A::kEight) {
                         }
                     if (__ballot(odd)) one_by_one = true;
                 } else {
-                                u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
-                for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
-                    // (the places of pieces that a head does not have hold what was in LDS before)
-                    if (A::kUsed != A::kPieces && (i % A::kPieces ^ A::value_swizzle(i / A::kPieces)) >= A::kUsed) continue;
-                    most = __builtin_elementwise_max(
-                        most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
-                }
-                bool odd = false;
+                    u16x8 most = {};   // the largest bits of a value: from those of infinity on, one is not finite
+                    for (int i = lane; i < A::kKeys * A::kPieces; i += kWave) {
+                        // (the places of pieces that a head does not have hold what was in LDS before)
+                        if (A::kUsed != A::kPieces && (i % A::kPieces ^ A::value_swizzle(i / A::kPieces)) >= A::kUsed) continue;
+                        most = __builtin_elementwise_max(
+                            most, *lds_at<u16x8>(tile_at + A::kKeys * A::kPitch + 16 * i) & (unsigned short)(0x7fff));
+                    }
+                    bool odd = false;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) odd |= most[e] >= M::kInfinity;
-                if (__ballot(odd)) one_by_one = true;
+                    for (int e = 0; e < 8; ++e) odd |= most[e] >= M::kInfinity;
+                    if (__ballot(odd)) one_by_one = true;
                 }
             }
         }
@@ -976,16 +976,27 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
 // Prefixes whose rows take WR wavefronts, and own tokens whose rows take one, in
 // one launch: the second wait for memory while the first compute.  A workgroup
 // is either WR wavefronts at one work of a prefix or, first, as many as have
-// room in the same LDS at a work of own tokens each.
+// room in the same LDS at a work of own tokens each.  In 8 bits all WR are (there
+// is LDS for it), and own tokens come last behind prefixes of four wavefronts, whose works are the longer ones: 4
+// x 12 sequences of 5 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128: 80 us, 88 before both (and
+// four splits of own tokens a CU); but with prefixes of two wavefronts 16 x 16 of one token 82, not 71.
 template <class T, class C, int DK, int RT, int WR>
-constexpr int kOwnWaves = AttendTile<T, C, DK, RT, WR>::kLds / AttendTile<T, C, DK, RT, 1>::kLds;
+constexpr int kOwnWaves = AttendTile<T, C, DK, RT, WR>::kEight
+                              ? WR
+                              : AttendTile<T, C, DK, RT, WR>::kLds / AttendTile<T, C, DK, RT, 1>::kLds;
+template <class T, class C, int DK, int RT, int WR>
+constexpr int kBothLds = AttendTile<T, C, DK, RT, WR>::kEight && WR * AttendTile<T, C, DK, RT, 1>::kLds > AttendTile<T, C, DK, RT, WR>::kLds
+                             ? WR * AttendTile<T, C, DK, RT, 1>::kLds
+                             : AttendTile<T, C, DK, RT, WR>::kLds;
 template <class T, class C, int DK, int RT, int WR>
 __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_both_kernel(AttendOf<C> p, AttendPlan plan,
                                                                               unsigned block0, unsigned own_blocks) {
     constexpr int kWaves = kOwnWaves<T, C, DK, RT, WR>;
-    const unsigned lds0 = tile_lds(), block = block0 + blockIdx.x;
-    if (block >= own_blocks) {
-        attend_tiles<T, C, DK, RT, WR>(p, plan, block - own_blocks, lds0);
+    constexpr bool kOwnLast = AttendTile<T, C, DK, RT, WR>::kEight && WR == 4;
+    const unsigned lds0 = tile_lds(), at = block0 + blockIdx.x;
+    const unsigned own0 = kOwnLast ? unsigned(plan.prefix.works()) : 0u, block = at - own0;   // among those of own tokens
+    if (kOwnLast ? at < own0 : at >= own_blocks) {
+        attend_tiles<T, C, DK, RT, WR>(p, plan, kOwnLast ? at : at - own_blocks, lds0);
         return;
     }
     const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), w = block * kWaves + wave;
