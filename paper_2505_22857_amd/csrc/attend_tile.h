@@ -31,6 +31,18 @@
 // wavefronts (4 x 384 rows: 7.4 us per 1024 tokens of prefix, 870 TFLOP/s, behind 24 us
 // for launches, first loads, partial sums and their join; 32768 tokens ran at 630 to 710 in
 // all).  Short ones: the chain of page table, first tile and join.
+//
+// A cache in 8 bits (Attend8).  An element stands for e s, s the scale of its block of tokens and its head, so
+// that S = (q . e_k) s_k and O = sum_k (w_k s_k) e_v: the scales are numbers of a key, which a lane has four
+// of, and no product of theirs reaches the elements.  These go to LDS as they are; a key's 16 bytes are a lane's
+// dimensions of two steps and are widened after the load, which is exact, values by the transposing load of
+// bytes.  Scales go to LDS beside their tile, one a key.  w s is split into two bfloat16 (2^-17 of it is lost):
+// with one the result's error was 1.35 to 1.58 times that of fp32 weights, which it now equals, for 4 %
+// of the time of many rows; halves would need one, but not every s leaves w s in their range.
+// Reading is bound as above at half the bytes (4 prefixes of 120000 tokens for 2 x 4 rows, 8 heads of 128: 170 us, 988 MB at
+// 5.8 TB/s); many rows by vector instructions, 620 a tile of 64 keys and 32 rows beside 96 of the matrix
+// cores, with two wavefronts a SIMD (4 groups of 60 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128:
+// 69 us; 585 TFLOP/s behind 20 us for launches, first tiles, partial sums and join; one group of 128 that sees 20000: 464 in all).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -815,9 +827,8 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
 #pragma unroll
         for (int r = 0; r < RT; ++r) base[r] = m[r] == -__builtin_inff() ? 0.0f : m[r];
         u32x4 weights[RT][N];   // of chunk c: pairs of rounded ones
-        // In 8 bits a weight takes its value's scale along, in bfloat16, whose exponents have room for both; where the
-        // output is half, in two parts, the second what the first's rounding has left.
-        constexpr bool kParts = A::kEight;
+        // In 8 bits a weight takes its value's scale along, in bfloat16, whose exponents have room for both, and in two
+        // parts, the second what the first's rounding has left.
         u32x4 rests[RT][N];
         f32x4 v_scales[N][2];
         if constexpr (A::kEight) {
@@ -836,8 +847,8 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
                 const float y0 = z0 * v_scales[c][e / 4][e % 4], y1 = z1 * v_scales[c][e / 4][e % 4 + 1];
                 const unsigned both = Matrix<Bf16>::round(y0, y1);
                 weights[r][c][pair % 4] = both;
-                if constexpr (kParts)
-                    rests[r][c][pair % 4] = Matrix<Bf16>::round(y0 - __uint_as_float(both << 16), y1 - __uint_as_float(both & 0xffff0000u));
+                rests[r][c][pair % 4] =
+                    Matrix<Bf16>::round(y0 - __uint_as_float(both << 16), y1 - __uint_as_float(both & 0xffff0000u));
                 return;
             }
             const float z0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][2 * c + e / 4][e % 4], to_log2, -base[r]));
@@ -864,7 +875,7 @@ __device__ __forceinline__ void attend_tiles(const AttendOf<C> &p, const AttendP
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     o[r][d] = Matrix<Bf16>::mul(value, __builtin_bit_cast(s16x8, weights[r][c]), o[r][d]);
-                    if constexpr (kParts) o[r][d] = Matrix<Bf16>::mul(value, __builtin_bit_cast(s16x8, rests[r][c]), o[r][d]);
+                    o[r][d] = Matrix<Bf16>::mul(value, __builtin_bit_cast(s16x8, rests[r][c]), o[r][d]);
                 }
             } else {
 #pragma unroll

@@ -1,10 +1,9 @@
 """Attention over a cache in 8 bits against its definition in 64 bits, from the values that elements and scales stand for.
 
 With u half an ulp of the output's type (2^-8 bfloat16, 2^-11 half) and A = sum of softmax |v|: the output is rounded once
-(u A) and the weights, times their values' scales, to bfloat16 (2^-8 A), where the output is half to two of them
-(2^-16 A); scores and sums are fp32: a score is off by at most 2^-24 (D + 4) sum |q k| scale, which is below
-2e-4 here and moves a weight by as much of its size.  So |out - exact| <= (u + w + 5e-4) A + 2^-25, w = 2^-8 or 2^-16,
-and the log of the sum is off by at most 1e-3.
+(u A) and the weights, times their values' scales, to a sum of two bfloat16 (2^-16 A); scores and sums are fp32: a score is
+off by at most 2^-24 (D + 4) sum |q k| scale, which is below 2e-4 here and moves a weight by as much of its size.  So
+|out - exact| <= (u + 2^-16 + 5e-4) A + 2^-25, and the log of the sum is off by at most 1e-3.
 """
 
 import math
@@ -20,7 +19,7 @@ import paper_2505_22857_amd as ng  # noqa: E402
 import serving_reference as ref  # noqa: E402
 
 F16, BF16, E4M3 = torch.float16, torch.bfloat16, torch.float8_e4m3fn
-BOUND = {F16: 2.0 ** -11 + 2.0 ** -16 + 5e-4, BF16: 2.0 ** -7 + 5e-4}
+BOUND = {F16: 2.0 ** -11 + 2.0 ** -16 + 5e-4, BF16: 2.0 ** -8 + 2.0 ** -16 + 5e-4}
 VALUES = beam_reference.e4m3_values()
 
 
