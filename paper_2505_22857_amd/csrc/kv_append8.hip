@@ -12,7 +12,7 @@
 // Bound by memory traffic, one read of 16 bits and one write of 8 for each
 // element, and, as every block's wavefront waits for a chain of loads (its sequence's
 // place, its page, its tokens), by how many of them run beside the queries'
-// streaming: 5 x 3500 tokens of 32 + 8 + 8 heads of 128 80 us, 299 MB at 3.7
+// streaming: 5 x 3500 tokens of 32 + 8 + 8 heads of 128 79 us, 299 MB at 3.8
 // TB/s, in one launch with both, 86 in two.  A few tokens: the launch, 5.4 us.
 #include <hip/hip_runtime.h>
 
@@ -307,7 +307,9 @@ __device__ __forceinline__ void turn_queries(const Append8 &p, int64_t group) {
     T *const to = static_cast<T *>(a.q_out) + n * a.q_heads * D;
     const bool counts = !a.lengths || t < a.lengths[s];
     const int64_t position = a.rotary > 0 && a.positions ? int64_t(a.positions[n]) : int64_t(a.start[s]) + t;
-    const T *const from = static_cast<const T *>(a.q) + s * a.q_stride_seq + t * a.q_stride_token;
+    // a token that does not count reads the sequence's first, for nothing (5 x 3500, a quarter of which do
+    not: 78.9 us, 80.7 with its own)
+    const T *const from = static_cast<const T *>(a.q) + s * a.q_stride_seq + (counts ? t : 0) * a.q_stride_token;
     const int items = a.q_heads * each;
     constexpr int kBatch = N == 1 ? 1 : (MODE == kHalves ? 2 : 4);
     auto put = [&](int at, const float (&x)[N]) {
