@@ -308,7 +308,7 @@ __device__ __forceinline__ void turn_queries(const Append8 &p, int64_t group) {
     const bool counts = !a.lengths || t < a.lengths[s];
     const int64_t position = a.rotary > 0 && a.positions ? int64_t(a.positions[n]) : int64_t(a.start[s]) + t;
     // a token that does not count reads the sequence's first, for nothing (5 x 3500, a quarter of which do
-    not: 78.9 us, 80.7 with its own)
+    // not: 78.9 us, 80.7 with its own)
     const T *const from = static_cast<const T *>(a.q) + s * a.q_stride_seq + (counts ? t : 0) * a.q_stride_token;
     const int items = a.q_heads * each;
     constexpr int kBatch = N == 1 ? 1 : (MODE == kHalves ? 2 : 4);
