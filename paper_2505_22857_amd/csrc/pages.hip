@@ -10,8 +10,9 @@
 //
 // Three steps, as each needs the one before whole: tables and counts; what every
 // row needs and what is free; the pages.  A few rows of a small pool are taken
-// by one workgroup in one launch, others by a launch a step; bound by these launches until
-// tables and pool are large.
+// by one workgroup in one launch, others by a launch a step; bound by these launches and a few
+// dependent round trips each until tables and pool are large: a fork of 64 x 16 rows of 114 entries over 29408 pages takes
+// 14.3 us, 8.8 MB of tables and counts, a compaction of 200 pages 2.1 us, of 8000 4.4, of 200000 10.1.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -311,8 +312,10 @@ namespace {
 
 constexpr int64_t kMostGroups = int64_t(1) << 23;   // workgroups a launch
 
-// Most rows (of 64 entries, old and new) and pages that one workgroup takes alone.
-constexpr int64_t kOneRows = 32, kOnePages = 16384;
+// Most rows (of 64 entries, old and new) and pages that one workgroup takes alone.  us, against three launches: 16 rows and
+// 70 pages 4.7 and 6.7, 24 rows 7.8 and 8.3, 48 rows and 416 pages 10.5 and 8.7, 128 rows 18 and 9; 16 rows and 4030 pages 7.5
+// and 8.6, 8030 pages 9.1 and 8.8, 16030 pages 13.2 and 9.4.
+constexpr int64_t kOneRows = 32, kOnePages = 4096;
 
 int64_t row_blocks_of(int64_t rows) { return (rows + kRowBlock - 1) / kRowBlock; }
 
@@ -431,7 +434,8 @@ __global__ __launch_bounds__(kPageThreads) void move_kernel(int32_t *pages, int6
     }
 }
 
-// All of it by one workgroup, E pages a thread: their counts stay in registers.
+// All of it by one workgroup, E pages a thread: their counts stay in registers.  us, against three launches: 200 pages 2.1
+// and 6.4, 2000 2.4 and 8.5, 8000 4.4 and 9.4.
 template <int E>
 __global__ __launch_bounds__(kOneThreads) void compact_one_kernel(Compact c) {
     extern __shared__ int32_t holes[];   // the free pages below page n, ascending
