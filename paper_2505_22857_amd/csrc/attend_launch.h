@@ -73,14 +73,13 @@ static hipError_t launch_rows(const AttendOf<C> &p, hipStream_t stream) {
 }
 
 // A row's parts joined: `lanes` threads take 4 dimensions each, and `groups` such
-// sets of threads every groups-th part, eight parts at a time so that their
+// sets of threads every groups-th part, kBatch parts at a time so that their
 // loads are in flight together; the sets then meet in LDS.  Bound by reading the
 // parts: 12288 rows of 5 or 6 of 128 dimensions (35 MB) 10 us, 160 rows of 33 6 us.
 constexpr int kJoinThreads = 256;
-template <class T>
+template <class T, int kBatch>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(Attend p, AttendPlan plan, int64_t rows, int lanes,
                                                                    int groups, int64_t row0) {
-    constexpr int kBatch = 8;
     const ngpu_attend_t &a = p.a;
     const int D = p.c.dim, d = int(threadIdx.x) % lanes * 4, group = int(threadIdx.x) / lanes % groups;
     const int64_t row = row0 + int64_t(blockIdx.x) * (kJoinThreads / (lanes * groups)) + int(threadIdx.x) / (lanes * groups);
@@ -323,18 +322,24 @@ hipError_t launch_tile(const AttendOf<C> &p, const Choice &r, int tiles, int wav
     }
 }
 
-template <class T>
+template <class T, class C>
 hipError_t join(const Attend &p, const Choice &r, hipStream_t stream) {
+    // In 8 bits four parts at a time, whose fewer registers leave more wavefronts room, and 16 a set of threads where
+    // these are many: 4 x 12 x 5 tokens of 32 heads, 10 parts, 73 us in all, with eight 77, with eight a set 74; four
+    // tokens of 8 heads, 6 parts, 10.3, with 16 a set 11.3.
+    constexpr bool kEight = std::is_same_v<C, E4m3>;
     const ngpu_attend_t &a = p.a;
     if (r.plan.parts == 1) return hipSuccess;
+    const int64_t rows = a.S * a.T * a.q_heads;
     int lanes = 2;   // threads a row
     while (4 * lanes < p.c.dim) lanes *= 2;
-    int groups = 1;   // sets of them, eight parts each
-    while (8 * groups < r.plan.prefix.splits + r.plan.own.splits && 2 * groups * lanes <= kJoinThreads) groups *= 2;
-    const int64_t rows = a.S * a.T * a.q_heads, per = kJoinThreads / (lanes * groups), kMost = int64_t(1) << 23;
+    const int each = kEight && rows >= 4096 ? 16 : 8;
+    int groups = 1;   // sets of them, `each` parts each
+    while (each * groups < r.plan.prefix.splits + r.plan.own.splits && 2 * groups * lanes <= kJoinThreads) groups *= 2;
+    const int64_t per = kJoinThreads / (lanes * groups), kMost = int64_t(1) << 23;
     for (int64_t r0 = 0; r0 < rows; r0 += kMost * per) {
         const int64_t grid = std::min(kMost, (rows - r0 + per - 1) / per);
-        hipLaunchKernelGGL((attend_join_kernel<T>), dim3(unsigned(grid)), dim3(kJoinThreads), 0, stream, p, r.plan,
+        hipLaunchKernelGGL((attend_join_kernel<T, kEight ? 4 : 8>), dim3(unsigned(grid)), dim3(kJoinThreads), 0, stream, p, r.plan,
                            rows, lanes, groups, r0);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
@@ -354,7 +359,7 @@ hipError_t launch(const AttendOf<C> &p, void *workspace, hipStream_t stream) {
             r.prefix_waves == r.own_waves
                 ? launch_tile<T, C>(p, r, std::max(r.prefix_tiles, r.own_tiles), r.own_waves, 0, all, stream)
                 : launch_both<T, C>(p, r, stream);
-        return e != hipSuccess ? e : join<T>(p, r, stream);
+        return e != hipSuccess ? e : join<T, C>(p, r, stream);
     }
     if (prefix > 0)
         if (const hipError_t e = launch_tile<T, C>(p, r, r.prefix_tiles, r.prefix_waves, 0, prefix, stream);
@@ -363,7 +368,7 @@ hipError_t launch(const AttendOf<C> &p, void *workspace, hipStream_t stream) {
     if (all > prefix)
         if (const hipError_t e = launch_tile<T, C>(p, r, r.own_tiles, r.own_waves, prefix, all, stream); e != hipSuccess)
             return e;
-    return join<T>(p, r, stream);
+    return join<T, C>(p, r, stream);
 }
 
 // Bytes of a call's workspace.
