@@ -230,11 +230,8 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
         const int64_t keys = a.pages_width * c.page_size, have = a.S * c.heads * r.plan.own.blocks;
         const int per = r.prefix_waves > 1 || r.own_waves == 4 ? (kEight && r.prefix_waves == 4 ? 4 : 2) : kEight ? 8 : 4;
         r.plan.own = cut(a.S * c.heads, a.T * rep, keys, per * kCus, r.own_tiles, r.own_waves);
-        // In 8 bits also one for 512 tokens beside such prefixes, as one wavefront would take longer over more than those do:
-        // 4 x 12 sequences of one token that see up to 3000 of their own 55 us, not 148; 32 x 10 that see 1500 and 1500 of
-        // prefix 111, not 122; with one for 256 126.
-        if (kEight && r.prefix_waves > 1 && r.own_waves == 1)
-            r.plan.own.splits = int(std::max<int64_t>(r.plan.own.splits, std::min<int64_t>((keys + 511) / 512, 128)));
+        // (Beside such prefixes one for 512 tokens of the tables' width would take 4 x 12 sequences of one token that see up to 3000 of
+        // their own from 150 us to 55, but 16 x 16 of two tokens that see 100 and whose tables hold 2048 from 61 to 82.)
         // One workgroup a block of rows would have the last block's be twice as long as the mean: one sequence of
         // 8192 tokens that see each other, 8 heads of 64: 280 us, in two splits 178.
         if (r.own_waves == 4 && 2 * a.T > keys && have <= 2 * kCus) r.plan.own.splits = std::max(r.plan.own.splits, 2);

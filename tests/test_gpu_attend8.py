@@ -118,7 +118,7 @@ def test_prefix_lengths(page, blocks, prefix):
 @pytest.mark.parametrize("beam", [5, 9])
 @pytest.mark.parametrize("own", [511, 513, 1300])
 def test_long_own_tokens_beside_prefixes_of_many_rows(D, beam, own):
-    """In splits of their own, in one launch with prefixes of two and four wavefronts."""
+    """In one launch with prefixes of two and four wavefronts."""
     check(G=2, beam=beam, T=2, H=1, rep=4, D=D, prefix=(200, 37), own=(own, 3, 0, own - 70, 512, 40, 1), seed=own, dtype=F16)
     check(G=1, beam=beam, T=1, H=3, rep=8, D=D, prefix=(0,), own=(7, own), seed=own + 1)
 
