@@ -42,7 +42,8 @@
 // Reading is bound as above at half the bytes (4 prefixes of 120000 tokens for 2 x 4 rows, 8 heads of 128: 170 us, 988 MB at
 // 5.8 TB/s); many rows by vector instructions, 620 a tile of 64 keys and 32 rows beside 96 of the matrix
 // cores, with two wavefronts a SIMD (4 groups of 60 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128:
-// 65 to 68 us; 585 TFLOP/s behind 17 us for launches, first tiles, partial sums and join; one group of 128 that sees 20000: 480 in all).
+// 65 to 68 us; 585 TFLOP/s behind 17 us for launches, first tiles, partial sums and join; one group of 128 that sees
+// 20000: 480 in all).
 #pragma once
 
 #include <hip/hip_runtime.h>
