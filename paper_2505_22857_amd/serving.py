@@ -260,7 +260,7 @@ def _table(t, name, dev, rows):
 
 
 def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, sin=None,
-              layout: int = NGPU_ROPE_HALF, q=None, lengths=None, k_scale=None, v_scale=None, stream=None):
+              layout: int = NGPU_ROPE_HALF, q=None, lengths=None, stream=None, k_scale=None, v_scale=None):
     """Store new keys and values in a paged cache, rotating keys and queries on the way.
 
     ``k``, ``v`` [S, T, heads, dim] go to places ``start[s] + t`` of the sequences' own tokens, entry
@@ -322,7 +322,7 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
 
 
 def attend(q, k_cache, v_cache, pages=None, lengths=None, prefix_pages=None, prefix_lengths=None, q_lengths=None,
-           scale=None, return_lse: bool = False, k_scale=None, v_scale=None, stream=None):
+           scale=None, return_lse: bool = False, stream=None, k_scale=None, v_scale=None):
     """Attention of ``q`` [S, T, q heads, dim] over a paged cache [pages, page size, heads, dim].
 
     With ``prefix_pages`` [G, width] and ``prefix_lengths`` [G], consecutive sequences in G groups of
