@@ -440,7 +440,7 @@ typedef struct {
  * a block whose entries before the first new one are kept (that one is not its entry 0) keeps its scale where that holds the
  * new tokens, and else takes the new one, and the entries before are rounded again to it.  What lies behind the last
  * new token of a block is no longer meaningful.  Elements that are not finite become NaN.  No two sequences of a call
- * may append to one block. */
+ * may append to one block.  Scales that overlap, as with a stride of 0 or one array for keys and values, are refused. */
 int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *args, void *hip_stream);
 
 /* ngpu_lm_attend over a cache in 8 bits: keys and values are the elements times their scales, in fp32.
@@ -538,7 +538,8 @@ int ngpu_lm_kv_fork(const ngpu_kv_fork_t *args, void *d_workspace, size_t worksp
  * nothing.  No page may be the `to` of two rows, or one row's `to` and another's `from`. */
 int ngpu_lm_kv_copy(const ngpu_kv_cache_t *cache, const int32_t *copies, int64_t n, void *hip_stream);
 
-/* The same for a cache in 8 bits; all scales of the page are copied with the entries. */
+/* The same for a cache in 8 bits; all scales of the page are copied with the entries.  A stride of 0, and one array of scales
+ * for keys and values, are taken; scales that overlap otherwise are refused. */
 int ngpu_lm_kv_copy8(const ngpu_kv_cache8_t *cache, const int32_t *copies, int64_t n, void *hip_stream);
 
 /* Device memory a compaction needs, 16-byte aligned, not initialised. */

@@ -2,6 +2,7 @@
 // verification, the paged cache and its pages, and attention.  Argument checks and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -94,6 +95,54 @@ int check_cache8(const ngpu_kv_cache8_t *c) {
         c->v_scale_stride_page < 0 || c->v_scale_stride_block < 0 || c->v_scale_stride_head < 0)
         return refuse("negative strides of the scales");
     if (c->cache.num_pages > 0 && (!c->k_scale || !c->v_scale)) return refuse("null device pointer of the scales");
+    return NGPU_OK;
+}
+
+// Dimensions of a strided tensor: entries, and the elements from one to the next.
+struct Axes {
+    struct {
+        int64_t size, stride;
+    } at[4];
+    int count = 0;
+};
+
+// Whether no two indexes share an element, for tensors whose dimensions are nested in any order, with gaps or not: from the
+// smallest stride on, each passes what the dimensions before span.
+bool apart(Axes axes) {
+    std::sort(axes.at, axes.at + axes.count, [](const auto &a, const auto &b) { return a.stride < b.stride; });
+    __int128 span = 0;
+    for (int i = 0; i < axes.count; ++i) {
+        if (axes.at[i].size <= 1) continue;
+        if (axes.at[i].stride <= span) return false;
+        span += __int128(axes.at[i].size - 1) * axes.at[i].stride;
+    }
+    return true;
+}
+
+// Scales that a call writes: each needs its own element, among keys', among values' and between the two.  With `same`, writers
+// of one element write one value, so a stride of 0, and one tensor for both, do no harm.
+int check_scales_apart(const ngpu_kv_cache8_t &c, bool same) {
+    if (c.cache.num_pages == 0) return NGPU_OK;
+    const int64_t sizes[] = {c.cache.num_pages, c.cache.page_size / c.block, c.cache.heads};
+    const int64_t strides[2][3] = {{c.k_scale_stride_page, c.k_scale_stride_block, c.k_scale_stride_head},
+                                   {c.v_scale_stride_page, c.v_scale_stride_block, c.v_scale_stride_head}};
+    Axes axes[2];
+    __int128 bytes[2] = {4, 4};   // from the first scale to behind the last
+    bool alike = true;
+    for (int i = 0; i < 3; ++i) {
+        alike = alike && (sizes[i] <= 1 || strides[0][i] == strides[1][i]);
+        for (int t = 0; t < 2; ++t) {
+            if (!same || strides[t][i] > 0) axes[t].at[axes[t].count++] = {sizes[i], strides[t][i]};
+            bytes[t] += __int128(sizes[i] - 1) * strides[t][i] * 4;
+        }
+    }
+    for (int t = 0; t < 2; ++t)
+        if (!apart(axes[t])) return refuse("%s_scale is written and must not overlap itself", t == 0 ? "k" : "v");
+    const uintptr_t k = reinterpret_cast<uintptr_t>(c.k_scale), v = reinterpret_cast<uintptr_t>(c.v_scale);
+    const uintptr_t between = k < v ? v - k : k - v;
+    if (between >= bytes[k < v ? 0 : 1] || (same && alike && between == 0)) return NGPU_OK;
+    axes[0].at[axes[0].count++] = {2, int64_t(between / 4)};
+    if (!alike || between % 4 != 0 || !apart(axes[0])) return refuse("k_scale and v_scale are written and must not overlap");
     return NGPU_OK;
 }
 
@@ -218,6 +267,7 @@ int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *ar
     bool empty;
     if (const int rc = check_append(cache->cache, args, a, empty)) return rc;
     if (empty) return done(hipSuccess, "");
+    if (const int rc = check_scales_apart(*cache, false)) return rc;
     return done(ngpu::launch_kv_append8(*cache, a, static_cast<hipStream_t>(hip_stream)), "append launch");
 }
 
@@ -286,6 +336,7 @@ int ngpu_lm_kv_copy8(const ngpu_kv_cache8_t *cache, const int32_t *copies, int64
     if (n < 0 || n > NGPU_LM_MAX_PAGES) return refuse("n = %lld out of range", (long long)n);
     if (n == 0 || cache->cache.num_pages == 0) return done(hipSuccess, "");
     if (!copies) return refuse("null device pointer");
+    if (const int rc = check_scales_apart(*cache, true)) return rc;
     return done(ngpu::launch_kv_copy8(*cache, copies, n, static_cast<hipStream_t>(hip_stream)), "copy launch");
 }
 

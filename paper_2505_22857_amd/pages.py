@@ -115,7 +115,8 @@ def kv_copy(k_cache, v_cache, copies, k_scale=None, v_scale=None, stream=None):
 
     ``copies`` [n, 3] int32 of ``kv_fork`` or ``kv_compact``: {from, to, entries} a row; rows with a page outside
     the cache are skipped.  No page may be written by two rows, or written by one and read by another.  Of an
-    8-bit cache all scales of a page, ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32, go with it."""
+    8-bit cache all scales of a page, ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32, go with it; they may be
+    expanded, or one tensor for both, and must not overlap otherwise."""
     native = _native()
     eight = k_scale is not None or v_scale is not None
     if stream is None and native:
