@@ -438,7 +438,8 @@ typedef struct {
 /* ngpu_lm_kv_append for a cache in 8 bits.  The rotated keys, in fp32, and the values are rounded once to e4m3.  A block's
  * scale for a head is the least power of two s (2^-100 at least) with 448 s no smaller than the new tokens' finite elements;
  * a block whose entries before the first new one are kept (that one is not its entry 0) keeps its scale where that holds the
- * new tokens, and else takes the new one, and the entries before are rounded again to it.  What lies behind the last
+ * new tokens and is 2^-100 at least, and else takes the new one, and the entries before are rounded again to it.  A scale there that is
+ * not finite and positive counts as 2^-100.  What lies behind the last
  * new token of a block is no longer meaningful.  Elements that are not finite become NaN.  No two sequences of a call
  * may append to one block.  Scales that overlap, as with a stride of 0 or one array for keys and values, are refused. */
 int ngpu_lm_kv_append8(const ngpu_kv_cache8_t *cache, const ngpu_kv_append_t *args, void *hip_stream);

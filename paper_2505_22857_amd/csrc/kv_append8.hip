@@ -243,8 +243,9 @@ __device__ __forceinline__ void append_block(const Append8 &p, const Block<T> &b
     }
     float now = least_scale(most);
     if (b.lead > 0) {
-        const float had = *b.scale, old = had >= 0x1p-100f && had < __builtin_inff() ? had : 0x1p-100f;
-        if (most > kMost8 * old) {   // it grows: the entries before, again
+        // (no number above 0 is none: 2^-100; one below that is raised to it, so that its inverse is finite)
+        const float had = *b.scale, old = had > 0.0f && had < __builtin_inff() ? had : 0x1p-100f;
+        if (most > kMost8 * old || old < 0x1p-100f) {   // it grows: the entries before, again
             const float ratio = old / now;
             for (int i = lane; i < b.lead * pieces; i += kLanes) {
                 const int token = i / pieces, from = (i - token * pieces) * N;

@@ -271,8 +271,8 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
 
     With ``k_scale`` and ``v_scale`` [pages, blocks, heads] float32 the caches are float8_e4m3fn, a value being the
     element times the scale of its block of page size / blocks tokens and its head.  A block's scale is the least power of
-    two that holds its tokens; where tokens before the new ones are in the block it grows when it has to, and they
-    are rounded again; entries behind the new ones are not kept.  No two sequences may append to one block, and the
+    two, 2^-100 at least, that holds its tokens; where tokens before the new ones are in the block it grows when it has to,
+    and they are rounded again; entries behind the new ones are not kept.  No two sequences may append to one block, and the
     scales must not overlap (an expanded tensor, one for keys and values): ``attend`` alone takes such ones.
     Returns the rotated queries (zero where a token does not count), None without ``q``."""
     native = _native()
