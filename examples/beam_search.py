@@ -59,16 +59,19 @@ class Network8(Network):
 
 
 def search(net: Network8, lm: "ng.NgpuLM", frames, frame_lengths, beam: int, tokens: int, weight: float = 0.3,
-           first: int = 0, compact_every: int = 0):
+           first: int = 0, compact_every: int = 0, pool: int = None):
     """At most ``tokens`` classes for the ``beam`` best hypotheses of each utterance of ``frames`` [G, L, width].
 
+    ``pool``: pages for the hypotheses' tokens, as many as they could need unless given; one that finds none is given up.
     Returns the classes [G, beam, tokens] (the vocabulary's size: ended; -1 behind it, or no hypothesis), the sums [G, beam]
     and the most pages that were in use."""
     s, dev = net.shape, net.device
     G, L = frames.shape[:2]
     i32 = torch.int32
     prefix_width, width = -(-L // s.page), -(-tokens // s.page)
-    P = G * (prefix_width + beam * width)   # enough where hypotheses share nothing
+    if pool is None:
+        pool = G * beam * width   # enough where hypotheses share nothing
+    P = G * prefix_width + pool
     refs = torch.zeros(P, dtype=i32, device=dev)
     cache = net.make_cache(P)
     tables = ng.rope_table(L + tokens, s.rotary, device=dev)
@@ -93,6 +96,8 @@ def search(net: Network8, lm: "ng.NgpuLM", frames, frame_lengths, beam: int, tok
     for t in range(tokens):
         new = ((classes >= 0) & (classes < s.vocab)).to(i32)
         pages, lengths, copies = ng.kv_fork(pages, lengths, parents, refs, s.page, tokens=new)
+        gone = (lengths < 0).view(G, beam)   # dropped for want of pages
+        scores, new = scores.masked_fill(gone, -torch.inf), new.masked_fill(gone, 0)
         for kc, vc, ks, vs in cache:
             ng.kv_copy(kc, vc, copies, k_scale=ks, v_scale=vs)
         most = torch.maximum(most, (refs > 0).sum())

@@ -528,8 +528,8 @@ size_t ngpu_lm_kv_fork_workspace(int64_t G, int64_t K, int64_t num_pages);
  *  3. It takes fresh pages for the places of its new tokens behind.
  * Fresh pages are the free ones of after step 1, the lowest to the first row (its copy first), each with refs 1.  A row
  * whose pages, with those of the rows before, are not there, or whose tokens would not fit the table, is dropped: its
- * entries are given back and -1, its length -1, no copy.  out_lengths: the parent's (without the new tokens), 0 without
- * parent.  The lengths are counted in tokens the table holds, so rejected tokens are given up by passing shorter ones.
+ * entries are given back and -1, its length -1, no copy; the caller has to end that hypothesis, as a later call takes a length
+ * below 0 for 0.  out_lengths: the parent's (without the new tokens), 0 without parent.  The lengths are counted in tokens the table holds, so rejected tokens are given up by passing shorter ones.
  * Freeing is a fork without children: K = 0, or parents of -1.  A new sequence is a row of -1 entries and length 0 that
  * is forked with as many tokens as its prompt has.  G = 0 is a no-op. */
 int ngpu_lm_kv_fork(const ngpu_kv_fork_t *args, void *d_workspace, size_t workspace_bytes, void *hip_stream);

@@ -68,7 +68,9 @@ def kv_fork(pages, lengths, parents, refs, page_size: int, tokens=0, stream=None
     A new row shares its parent's pages.  Where it is going to append into a page that is filled in part and that
     others hold too, it gets a fresh page, to which ``kv_copy`` has to copy what is filled, in each layer's
     cache, before the append; and fresh pages for the tokens behind.  Fresh pages are the lowest free ones, in
-    the rows' order.  A row that finds too few, or whose tokens do not fit the table, is dropped (length -1).
+    the rows' order.  A row that finds too few, or whose tokens do not fit the table, is dropped: it holds no pages
+    and its length is -1.  The caller has to end that hypothesis (a score of -inf in ``beam_step``, nothing to append),
+    as a length below 0 counts as 0 in the next call.
     Entries of the old tables are given up: pages that no new row holds are free.  So ``parents`` of
     -1 free a group's pages, a shorter length gives up rejected tokens, and a new sequence is a row of -1 entries
     and length 0 that is forked with its prompt's tokens.
