@@ -495,7 +495,7 @@ class NgpuLM:
                     _check(r)
                 return r
         import torch
-        from .serving import _need, _on, _untracked
+        from .serving import _need, _on, _untracked, _whole
         if not hasattr(asr, "is_cuda") or not asr.is_cuda or asr.dtype is not torch.float32:
             raise TypeError("asr must be a float32 device tensor")
         if asr.dim() != 3:
@@ -505,10 +505,10 @@ class NgpuLM:
             raise ValueError(f"asr rows must hold {self._classes(mode)} classes for mode {mode}")
         if C > 1 and asr.stride(2) != 1 and asr.numel() > 0:
             raise TypeError("asr must have unit stride in the last dimension")
-        dev, k = asr.device, W if k is None else int(k)
+        dev, k = asr.device, W if k is None else _whole(k, "k")
         if not 1 <= W <= MAX_BEAMS or not 1 <= k <= MAX_BEAMS:
             raise ValueError(f"hypotheses before and after a step must lie in [1, {MAX_BEAMS}]")
-        a = _BeamStep(B, W, k, int(mode), float(lam), asr.data_ptr(), asr.stride(0), asr.stride(1),
+        a = _BeamStep(B, W, k, _whole(mode, "mode"), float(lam), asr.data_ptr(), asr.stride(0), asr.stride(1),
                       _need(states, "states", dev, torch.int32, (B, W)),
                       _need(scores, "scores", dev, torch.float32, (B, W)),
                       _need(last, "last", dev, torch.int32, (B, W)))

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes
 
 from . import _check, _torch_mod, load_library
-from .serving import _cache, _Cache, _cache8, _Cache8, _device_of, _native, _need, _on, _table, _untracked
+from .serving import _cache, _Cache, _cache8, _Cache8, _device_of, _native, _need, _on, _table, _untracked, _whole
 
 MAX_FORK = 4096                  # NGPU_LM_MAX_FORK
 MAX_PAGES = 1 << 28              # NGPU_LM_MAX_PAGES
@@ -92,14 +92,14 @@ def kv_fork(pages, lengths, parents, refs, page_size: int, tokens=0, stream=None
     if pages.dim() != 2 or (G > 0 and pages.shape[0] % G != 0) or (G == 0 and pages.shape[0] > 0):
         raise ValueError("pages must be a [G * W, width] tensor")
     rows = pages.shape[0]
-    a = _Fork(G, rows // G if G else 0, K, page_size=int(page_size), num_pages=P, refs=refs_at)
+    a = _Fork(G, rows // G if G else 0, K, page_size=_whole(page_size, "page_size"), num_pages=P, refs=refs_at)
     a.pages, a.width, a.pages_stride = _table(pages, "pages", dev, rows)
     a.lengths = _need(lengths, "lengths", dev, i32, (rows,))
     a.parents = _need(parents, "parents", dev, i32, (G, K))
     if hasattr(tokens, "dim"):
         a.tokens = _need(tokens, "tokens", dev, i32, (G, K))
     else:
-        a.T = int(tokens)
+        a.T = _whole(tokens, "tokens", 64)
     lib = _library()
     with _on(dev, stream) as handle:
         new = torch.empty((G * K, a.width), dtype=i32, device=dev)
@@ -162,13 +162,13 @@ def kv_compact(refs, page_size: int, tables=(), stream=None):
     starts = [f[0] for f, t in zip(found, tables) if t.numel() > 0]
     if len(set(starts)) < len(starts):
         raise ValueError("a table must not be listed twice")
-    lib = _library()
+    page_size, lib = _whole(page_size, "page_size"), _library()
     with _on(dev, stream) as handle:
         copies = torch.empty((P // 2, 3), dtype=torch.int32, device=dev)
         moved = torch.empty(P, dtype=torch.int32, device=dev)
         size = lib.ngpu_lm_kv_compact_workspace(P)
         workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-        _check(lib.ngpu_lm_kv_compact(refs_at, P, int(page_size), copies.data_ptr(), moved.data_ptr(),
+        _check(lib.ngpu_lm_kv_compact(refs_at, P, page_size, copies.data_ptr(), moved.data_ptr(),
                                       workspace.data_ptr(), size, handle))
         for (at, width, stride), t in zip(found, tables):
             _check(lib.ngpu_lm_kv_move(at, t.shape[0], width, stride, moved.data_ptr(), P, handle))

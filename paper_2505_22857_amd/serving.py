@@ -134,6 +134,14 @@ def _need(t, name, device, dtype, shape, rows=False):
     return t.data_ptr()
 
 
+def _whole(x, name, bits=32):
+    """A whole number as a signed one of so many bits: ctypes would drop what is above them, and int() a fraction."""
+    n = int(x)
+    if n != x or not -(1 << bits - 1) <= n < 1 << bits - 1:
+        raise ValueError(f"{name} must be a whole number of {bits} bits, not {x}")
+    return n
+
+
 def _temperature(t):
     """A float as the library is to check it: what fp32 would round to 0, which is greedy, stays one that is refused."""
     t = float(t)
@@ -222,7 +230,7 @@ def _cache(k_cache, v_cache):
 def _layout(k_cache, v_cache, dev, code):
     if k_cache.dim() != 4:
         raise ValueError("the cache must be a [pages, page size, heads, dim] tensor")
-    pages, page_size, heads, dim = k_cache.shape
+    pages, page_size, heads, dim = (_whole(n, "each dimension of the cache") for n in k_cache.shape)
     return _Cache(code, heads, dim, page_size, pages,
                   _need(k_cache, "k_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
                   _need(v_cache, "v_cache", dev, k_cache.dtype, k_cache.shape, rows=True),
@@ -297,7 +305,7 @@ def kv_append(k, v, k_cache, v_cache, pages, start, positions=None, cos=None, si
     a.pages, a.pages_width, a.pages_stride = _table(pages, "pages", dev, S)
     a.start = _need(start, "start", dev, i32, (S,))
     a.lengths = _need(lengths, "lengths", dev, i32, (S,))
-    a.layout = int(layout)
+    a.layout = _whole(layout, "layout")
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin come together")
     if cos is not None:
