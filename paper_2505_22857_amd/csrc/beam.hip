@@ -599,11 +599,18 @@ static hipError_t whole(const DevTrie &t, const Beam &p, hipStream_t stream) {
 template <int W, int NT>
 static hipError_t expand(const DevTrie &t, const Beam &p, hipStream_t stream) {
     constexpr int64_t kMost = int64_t(1) << 22;   // workgroups a launch
-    const size_t lds = sizeof(BeamMeet) + std::max(size_t(beam_list<W>()) * 12, size_t(W) * kWave * NT * sizeof(i32x2));
+    constexpr size_t lds = sizeof(BeamMeet) + std::max(size_t(beam_list<W>()) * 12, size_t(W) * kWave * NT * sizeof(i32x2));
     const int64_t all = p.a.B * p.a.W;
+    const bool full = t.vocab_size == W * kWave * NT;
+    if constexpr (lds > 65536) {
+        static std::atomic<uint64_t> devices[2];
+        const hipError_t e = full ? allow_lds(&beam_expand_kernel<W, NT, true>, int(lds), devices[1])
+                                  : allow_lds(&beam_expand_kernel<W, NT, false>, int(lds), devices[0]);
+        if (e != hipSuccess) return e;
+    }
     for (int64_t n0 = 0; n0 < all; n0 += kMost) {
         const dim3 grid(unsigned(std::min(kMost, all - n0))), block(W * kWave);
-        if (t.vocab_size == W * kWave * NT)
+        if (full)
             hipLaunchKernelGGL((beam_expand_kernel<W, NT, true>), grid, block, lds, stream, t, p, n0);
         else
             hipLaunchKernelGGL((beam_expand_kernel<W, NT, false>), grid, block, lds, stream, t, p, n0);

@@ -8,7 +8,8 @@
 
 namespace ngpu {
 
-// More LDS than a launch has by default, asked for once a device (bits of `devices`).
+// More LDS than the 64 KB of a launch by default, asked for once a device (bits of `devices`), as HIP's documentation has it.
+// (The runtime of ROCm 7 launches without being asked: step, decode and top-k rely on that with 65 KB.)
 template <class K>
 hipError_t allow_lds(K *kernel, int bytes, std::atomic<uint64_t> &devices) {
     int device;
