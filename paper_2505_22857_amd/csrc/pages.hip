@@ -167,8 +167,8 @@ __device__ __forceinline__ void fork_tables(const Fork &f, int64_t row, int lane
             count_page<ONE>(a, a.pages[old * a.pages_stride + i], (i < have ? children : 0) - 1);
     }
 }
-__global__ __launch_bounds__(kPageThreads) void fork_tables_kernel(Fork f, int64_t row0) {
-    fork_tables<false>(f, row0 + int64_t(blockIdx.x) * kPageWaves + threadIdx.x / kWave, threadIdx.x % kWave);
+__global__ __launch_bounds__(kPageThreads) void fork_tables_kernel(Fork f) {
+    fork_tables<false>(f, int64_t(blockIdx.x) * kPageWaves + threadIdx.x / kWave, threadIdx.x % kWave);
 }
 
 // The fresh pages that a row needs, and the page that it copies.
@@ -276,10 +276,10 @@ __device__ __forceinline__ void fork_pages(const Fork &f, int64_t row, int lane,
     }
     for (int64_t i = lane; i < more; i += kWave) entries[have + i] = fresh(first + (from >= 0 ? 1 : 0) + i);
 }
-__global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f, int64_t row0) {
+__global__ __launch_bounds__(kPageThreads) void fork_pages_kernel(Fork f) {
     __shared__ int32_t before[kMostPageBlocks + 1];
     scan_counts(f.counts, f.blocks.count, before);
-    const int64_t w0 = row0 + int64_t(blockIdx.x) * kPageWaves, row_block = w0 / kRowBlock;
+    const int64_t w0 = int64_t(blockIdx.x) * kPageWaves, row_block = w0 / kRowBlock;
     int64_t sum = 0, base;
     for (int64_t b = threadIdx.x; b < row_block; b += kPageThreads) sum += f.row_sums[b];
     scan_threads(sum, base);
@@ -310,7 +310,8 @@ __global__ __launch_bounds__(kOneThreads) void fork_one_kernel(Fork f) {
 
 namespace {
 
-constexpr int64_t kMostGroups = int64_t(1) << 23;   // workgroups a launch
+// Old and new rows, a wavefront each, fit a launch (of less than 2^32 work-items).
+static_assert(2 * int64_t(NGPU_LM_MAX_SEQUENCES) * kWave <= int64_t(1) << 31, "rows of a launch");
 
 // Most rows (of 64 entries, old and new) and pages that one workgroup takes alone.  us, against three launches: 16 rows and
 // 70 pages 4.7 and 6.7, 24 rows 7.8 and 8.3, 48 rows and 416 pages 10.5 and 8.7, 128 rows 18 and 9; 16 rows and 4030 pages 7.5
@@ -358,18 +359,16 @@ hipError_t launch_kv_fork(const ngpu_kv_fork_t &a, void *workspace, hipStream_t 
         hipLaunchKernelGGL(fork_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, f);
         return hipGetLastError();
     }
-    for (int64_t r0 = 0; r0 < rows; r0 += kMostGroups * kPageWaves) {
-        const int64_t grid = std::min(kMostGroups, (rows - r0 + kPageWaves - 1) / kPageWaves);
-        hipLaunchKernelGGL(fork_tables_kernel, dim3(unsigned(grid)), dim3(kPageThreads), 0, stream, f, r0);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
+    hipLaunchKernelGGL(fork_tables_kernel, dim3(unsigned((rows + kPageWaves - 1) / kPageWaves)), dim3(kPageThreads), 0, stream,
+                       f);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (R == 0) return hipSuccess;
     const int64_t row_blocks = row_blocks_of(R);
     hipLaunchKernelGGL(fork_plan_kernel, dim3(unsigned(row_blocks + f.blocks.count)), dim3(kPageThreads), 0, stream, f,
                        row_blocks);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(fork_pages_kernel, dim3(unsigned((R + kPageWaves - 1) / kPageWaves)), dim3(kPageThreads), 0, stream,
-                       f, int64_t(0));
+                       f);
     return hipGetLastError();
 }
 
