@@ -554,7 +554,7 @@ int ngpu_lm_kv_compact(int32_t *refs, int64_t num_pages, int32_t page_size, int3
                        void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* pages[r][i] = moved[pages[r][i]] for the entries in [0, num_pages) of a table [rows, width], row stride pages_stride
- * (at least width where rows > 1). */
+ * (at least width where rows > 1).  A second time changes nothing: each new place was free, and moved has it stay. */
 int ngpu_lm_kv_move(int32_t *pages, int64_t rows, int64_t width, int64_t pages_stride, const int32_t *moved,
                     int64_t num_pages, void *hip_stream);
 

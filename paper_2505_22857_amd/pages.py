@@ -143,7 +143,8 @@ def kv_compact(refs, page_size: int, tables=(), stream=None):
 
     With n pages in use (``refs`` other than 0), those from page n on move to the free ones below, in ascending
     order.  ``refs`` and the page ``tables`` (int32 [rows, width] each, all that hold the pool's pages) are
-    updated in place; ``kv_copy`` then has to move the pages of each layer's cache.
+    updated in place; ``kv_copy`` then has to move the pages of each layer's cache.  Tables may be views that share rows:
+    an entry that is put through ``moved`` twice stays where the first time put it.
 
     Returns (copies [pages // 2, 3] int32, moved [pages] int32: each page's new number)."""
     native, tables = _native(), tuple(tables)
@@ -159,6 +160,7 @@ def kv_compact(refs, page_size: int, tables=(), stream=None):
     for i, t in enumerate(tables):
         if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
             raise ValueError(f"the rows of tables[{i}] must not overlap")
+    # (views that share entries otherwise do no harm: a page's new place was free, and a free page's number stays)
     starts = [f[0] for f, t in zip(found, tables) if t.numel() > 0]
     if len(set(starts)) < len(starts):
         raise ValueError("a table must not be listed twice")
