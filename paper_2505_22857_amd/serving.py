@@ -248,12 +248,13 @@ def _cache8(k_cache, v_cache, k_scale, v_scale, dtype):
     if code not in (NGPU_F16, NGPU_BF16):
         raise TypeError("an 8-bit cache goes with float16 or bfloat16")
     c = _layout(k_cache, v_cache, dev, code)
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if not hasattr(t, "is_cuda") or t.device != dev or t.dtype is not torch.float32:
+            raise TypeError(f"{name} must be a torch.float32 tensor on {dev}")
     if k_scale.dim() != 3 or k_scale.shape[1] < 1 or c.page_size % k_scale.shape[1] != 0:
         raise ValueError("the scales must be [pages, blocks of a page, heads] tensors whose blocks divide a page")
     shape = (c.num_pages, k_scale.shape[1], c.heads)
     for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-        if not hasattr(t, "is_cuda") or t.device != dev or t.dtype is not torch.float32:
-            raise TypeError(f"{name} must be a torch.float32 tensor on {dev}")
         if tuple(t.shape) != shape:
             raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
     return dev, _Cache8(c, c.page_size // k_scale.shape[1], k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride(),
