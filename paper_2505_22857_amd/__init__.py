@@ -42,10 +42,9 @@ EXPORTED = [
     "ngpu_lm_check_states", "ngpu_lm_sync_check",
     "ngpu_lm_query_bytes", "ngpu_lm_host_image", "ngpu_lm_last_error",
     "ngpu_lm_draft", "ngpu_lm_verify_workspace", "ngpu_lm_verify", "ngpu_lm_kv_append", "ngpu_lm_attend_workspace",
-    "ngpu_lm_attend", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork", "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_append8", "ngpu_lm_attend8_workspace", "ngpu_lm_attend8",
-    "ngpu_lm_beam_step_workspace",
-    "ngpu_lm_beam_step",
-        "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
+    "ngpu_lm_attend", "ngpu_lm_kv_append8", "ngpu_lm_attend8_workspace", "ngpu_lm_attend8",
+    "ngpu_lm_beam_step_workspace", "ngpu_lm_beam_step", "ngpu_lm_kv_fork_workspace", "ngpu_lm_kv_fork",
+    "ngpu_lm_kv_copy", "ngpu_lm_kv_copy8", "ngpu_lm_kv_compact_workspace", "ngpu_lm_kv_compact", "ngpu_lm_kv_move",
     "ngpu_arpa_parse", "ngpu_arpa_list", "ngpu_arpa_free",
 ]
 
@@ -553,7 +552,10 @@ from .serving import (MAX_DRAFT, MAX_HEAD_DIM, NGPU_BF16, NGPU_F16, NGPU_F32, NG
                       NGPU_ROPE_INTERLEAVED, attend, kv_append, rope_table, verify)
 from .pages import MAX_FORK, MAX_PAGES, kv_compact, kv_copy, kv_fork  # noqa: E402
 
-__all__ = ["MAX_BEAMS", "verify", "kv_append", "attend", "kv_fork", "kv_copy", "kv_compact", "MAX_FORK", "MAX_PAGES", "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16",
-           "NGPU_BF16", "NGPU_ROPE_HALF", "NGPU_ROPE_INTERLEAVED", "NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED", "NGPU_BUILD_BOS_EOS",
-           "NGPU_BUILD_REPAIR_CLOSURE",
-           "NGPU_FUSION_PLAIN", "NGPU_FUSION_CTC", "NGPU_FUSION_TRANSDUCER", "NGPU_FUSION_AED"]
+__all__ = [
+    "MAX_BEAMS", "verify", "kv_append", "attend", "kv_fork", "kv_copy", "kv_compact", "MAX_FORK", "MAX_PAGES",
+    "rope_table", "MAX_DRAFT", "MAX_HEAD_DIM", "NGPU_F32", "NGPU_F16", "NGPU_BF16", "NGPU_ROPE_HALF",
+    "NGPU_ROPE_INTERLEAVED", "NgpuLM", "NgpuError", "load_library", "parse_arpa", "LIB_PATH", "EXPORTED",
+    "NGPU_BUILD_BOS_EOS", "NGPU_BUILD_REPAIR_CLOSURE", "NGPU_FUSION_PLAIN", "NGPU_FUSION_CTC",
+    "NGPU_FUSION_TRANSDUCER", "NGPU_FUSION_AED",
+]

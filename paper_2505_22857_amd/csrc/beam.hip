@@ -43,10 +43,6 @@ struct Beam {
     int32_t *next;       // [B, W, k + 1] their states
 };
 
-__device__ __forceinline__ int lanes_below(u64 mask) {   // bits of the lanes before this one
-    return int(__builtin_amdgcn_mbcnt_hi(unsigned(mask >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(mask), 0u)));
-}
-
 // Sum over 16 lanes, in each of them.
 __device__ __forceinline__ int row_sum(int x) {
     auto moved = [](int v, auto ctrl) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, 0xf, 0xf, true); };

@@ -78,10 +78,6 @@ __device__ __forceinline__ int64_t scan_threads(int64_t x, int64_t &total) {
     return before + upto - x;
 }
 
-__device__ __forceinline__ int below(unsigned long long mask) {   // bits of the lanes before this one
-    return int(__builtin_amdgcn_mbcnt_hi(unsigned(mask >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(mask), 0u)));
-}
-
 // The pages of a block in ascending order, a tile of coalesced loads at a time: visit(page, whether its count meets `is`, how
 // many of the block before it do).  Returns how many do; for the whole workgroup.
 template <int WAVES = kPageWaves, class Is, class Visit>
@@ -112,7 +108,7 @@ __device__ __forceinline__ int over_pages(const int32_t *refs, int64_t p0, int64
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            if (w0 + kWave * i < p1) visit(w0 + kWave * i, (masks[i] >> lane & 1) != 0, at + below(masks[i]));
+            if (w0 + kWave * i < p1) visit(w0 + kWave * i, (masks[i] >> lane & 1) != 0, at + lanes_below(masks[i]));
             at += __builtin_popcountll(masks[i]);
         }
     }
@@ -459,7 +455,7 @@ __global__ __launch_bounds__(kOneThreads) void compact_one_kernel(Compact c) {
     for (int i = 0; i < E; ++i) {
         const int page = p0 + kWave * i;
         const unsigned long long mask = __ballot(r[i] != 0), hole = __ballot(r[i] == 0 && page < n);
-        if (r[i] == 0 && page < n) holes[page - used - below(mask)] = page;
+        if (r[i] == 0 && page < n) holes[page - used - lanes_below(mask)] = page;
         used += __builtin_popcountll(mask);
         free += __builtin_popcountll(hole);
     }
@@ -476,7 +472,7 @@ __global__ __launch_bounds__(kOneThreads) void compact_one_kernel(Compact c) {
         if (page < P) {
             int to = page;
             if (r[i] != 0 && page >= n) {
-                const int at = used + below(mask) - (n - moves);
+                const int at = used + lanes_below(mask) - (n - moves);
                 to = holes[at];
                 c.copies[3 * at] = page;
                 c.copies[3 * at + 1] = to;

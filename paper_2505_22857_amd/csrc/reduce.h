@@ -1,4 +1,4 @@
-// Reductions of floats over a wavefront and over a few wavefronts' results.
+// Reductions of floats over a wavefront and over a few wavefronts' results, and a lane's rank in a mask.
 #pragma once
 
 #include <type_traits>
@@ -6,6 +6,11 @@
 #include "group.h"
 
 namespace ngpu {
+
+// Bits of a wavefront's mask that belong to the lanes before this one.
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+    return int(__builtin_amdgcn_mbcnt_hi(unsigned(mask >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(mask), 0u)));
+}
 
 // The inverse of float_key.
 __device__ __forceinline__ float key_float(unsigned k) {
