@@ -200,7 +200,9 @@ Choice choose(const ngpu_kv_cache_t &c, const ngpu_attend_t &a, char *workspace)
     Choice r{};
     r.tiles = takes_tiles(c, a, 16 / int64_t(sizeof(C)));
     if (!r.tiles) return r;
-    r.steps = c.dim <= 64 ? 2 : (c.dim <= 96 && !kEight ? 3 : (c.dim <= 128 ? 4 : 8));   // (two steps at a time in 8 bits)
+    // (two steps at a time in 8 bits, so heads of 65 to 96 dimensions are computed as 128: 4 x 12 x 5 tokens that see 7000 take 68
+    // us in a graph with heads of 96, 67 with 80, 72 with 128)
+    r.steps = c.dim <= 64 ? 2 : (c.dim <= 96 && !kEight ? 3 : (c.dim <= 128 ? 4 : 8));
     const int64_t rep = a.q_heads / c.heads;
     auto cut = [&](int64_t problems, int64_t rows, int64_t most_keys, int64_t wanted, int &tiles, int &waves) {
         Cut u{problems, 0, 0, 0};
@@ -322,8 +324,9 @@ hipError_t launch_tile(const AttendOf<C> &p, const Choice &r, int tiles, int wav
 template <class T, class C>
 hipError_t join(const Attend &p, const Choice &r, hipStream_t stream) {
     // In 8 bits four parts at a time, whose fewer registers leave more wavefronts room, and 16 a set of threads where
-    // these are many: 4 x 12 x 5 tokens of 32 heads, 10 parts, 73 us in all, with eight 77, with eight a set 74; four
-    // tokens of 8 heads, 6 parts, 10.3, with 16 a set 11.3.
+    // rows are many.  us in all, calls in a graph, 4 x 12 x 5 tokens of 32 heads, 7680 rows: 72 to 73, with eight at a time
+    // 73.5, with eight a set 76; 2 x 16 x 8 of 64 dimensions, 8192 rows, 33.5, 34.5, 35; 8 x 16 x 8, 32768 rows, 126, 132, 127.  With 16
+    // a set for fewer rows: 4096 even (80), 2048 34.7 (8 x 8 x 1) not 33.9 but 56.1 (2 x 8 x 4) not 57.4, 1024 15.9 not 14.9, 32 11.3 not 10.3.
     constexpr bool kEight = std::is_same_v<C, E4m3>;
     const ngpu_attend_t &a = p.a;
     if (r.plan.parts == 1) return hipSuccess;

@@ -42,7 +42,7 @@
 // Reading is bound as above at half the bytes (4 prefixes of 120000 tokens for 2 x 4 rows, 8 heads of 128: 170 us, 988 MB at
 // 5.8 TB/s); many rows by vector instructions, 620 a tile of 64 keys and 32 rows beside 96 of the matrix
 // cores, with two wavefronts a SIMD (4 groups of 60 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128:
-// 65 to 68 us; 585 TFLOP/s behind 17 us for launches, first tiles, partial sums and join; one group of 128 that sees
+// 65 to 68 us a call among others, 72 to 73 in a graph; 585 TFLOP/s behind 17 us for launches, first tiles, partial sums and join; one group of 128 that sees
 // 20000: 480 in all).
 #pragma once
 
@@ -990,8 +990,9 @@ __global__ __launch_bounds__(64 * WR, DK <= 4 ? 2 : 1) void attend_tile_kernel(A
 // is either WR wavefronts at one work of a prefix or, first, as many as have
 // room in the same LDS at a work of own tokens each.  In 8 bits all WR are (there
 // is LDS for it), and own tokens come last behind prefixes of four wavefronts, whose works are the longer ones: 4
-// x 12 sequences of 5 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128: 80 us, 88 without either and with
-// half the splits of own tokens; but with prefixes of two wavefronts 16 x 16 of one token 82, not 71.
+// x 12 sequences of 5 tokens that see up to 7000 of prefix and 300, 32 / 8 heads of 128, calls in a graph: 72 to 73 us, with own
+// tokens first 78, without either and with half the splits of own tokens 81.  With prefixes of two wavefronts it depends: 16 x 16
+// of one token that see 100 gain (49.5, not 51.8), 4 x 12 of one that see 3000 lose (181, not 157).
 template <class T, class C, int DK, int RT, int WR>
 constexpr int kOwnWaves = AttendTile<T, C, DK, RT, WR>::kEight
                               ? WR

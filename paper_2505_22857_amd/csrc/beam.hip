@@ -20,10 +20,12 @@
 // states (8 bytes a token, from L2 where hypotheses share them): the smallest
 // calls are bound by the latency of the chain state, record, arcs, selection
 // (1 x 4 hypotheses of 128 tokens: 4.7 us, an empty launch 3.9), the largest by
-// instructions: 592 hypotheses of 8192 tokens take 16.5 + 3.5 us, 450 vector
-// and 440 scalar instructions a wavefront of 1024 tokens, 1.2 TB/s of scores.
-// The bound matters: with the smallest of enough parts' maxima instead of the
-// k-th largest of 64, two or three more halvings, it was 19.6 us.
+// the same chain with two workgroups a CU, whose slots fill LDS: 592 hypotheses
+// of 8192 tokens take 16.5 + 3.5 us and fetch 52 MB, 19 of scores and the rest of
+// dense rows (10 us at a copy's rate), while their wavefronts wait for 53 % of
+// their cycles and issue 450 vector and 440 scalar instructions each.  The
+// selection's bound matters too: with the smallest of enough parts' maxima instead
+// of the k-th largest of 64, two or three more halvings, it was 19.6 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -628,8 +630,9 @@ static hipError_t select(const Beam &p, hipStream_t stream) {
 
 // Whether one launch takes the call: where each lane has four tokens of at most 16 wavefronts.  64 utterances take 5.0
 // against 7.4 us in two launches (4 hypotheses, 128 tokens), 6.4 against 8.6 (8, 512) and 6.3 against 8.0 (4, 1024); with
-// eight tokens a lane, 16 hypotheses of 512 gain nothing (11.3 against 9.5), while 8 of 1024 are even on the card
-// (9.4 against 8.8; 128 utterances 9.7 against 10.1) and spare the caller a launch, 2 us.  Past a workgroup a CU
+// eight tokens a lane, 16 hypotheses of 512 gain nothing (11.3 against 9.5), while 5 to 8 of 513 to 1024 do: of 1024, 6-grams,
+// calls in a graph, 1 / 64 / 256 utterances take 6.5 / 6.8 / 7.1 us with 5 hypotheses (two launches 7.9 / 9.1 / 10.5) and
+// 7.1 / 7.8 / 8.1 with 8 (7.9 / 9.4 / 11.5), and calls that the host paces 8.1, not 10.9.  Past a workgroup a CU
 // small ones still gain, 600 utterances of 4 hypotheses 6.0 against 8.9 (128 tokens) and 7.8 against 9.5 (512), larger
 // ones do not: 8 hypotheses of 512 tokens 17.8 against 12.0.
 static bool takes_whole(int64_t B, int W, int V) {

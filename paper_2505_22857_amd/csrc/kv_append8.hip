@@ -12,8 +12,9 @@
 // Bound by memory traffic, one read of 16 bits and one write of 8 for each
 // element, and, as every block's wavefront waits for a chain of loads (its sequence's
 // place, its page, its tokens), by how many of them run beside the queries'
-// streaming: 5 x 3500 tokens of 32 + 8 + 8 heads of 128 79 us, 299 MB at 3.8
-// TB/s, in one launch with both, 86 in two.  A few tokens: the launch, 5.4 us.
+// streaming: 5 x 3500 tokens of 32 + 8 + 8 heads of 128 take 72 us a call among
+// others, 299 MB at 4.1 TB/s, and 79 in a graph of calls on the same tokens, as all
+// figures below are; in two launches 85.  A few tokens: the launch, 5.4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -309,7 +310,7 @@ __device__ __forceinline__ void turn_queries(const Append8 &p, int64_t group) {
     const bool counts = !a.lengths || t < a.lengths[s];
     const int64_t position = a.rotary > 0 && a.positions ? int64_t(a.positions[n]) : int64_t(a.start[s]) + t;
     // a token that does not count reads the sequence's first, for nothing (5 x 3500, a quarter of which do
-    // not: 78.9 us, 80.7 with its own)
+    // not: 79 us, 80.5 with its own)
     const T *const from = static_cast<const T *>(a.q) + s * a.q_stride_seq + (counts ? t : 0) * a.q_stride_token;
     const int items = a.q_heads * each;
     constexpr int kBatch = N == 1 ? 1 : (MODE == kHalves ? 2 : 4);
@@ -394,7 +395,7 @@ static hipError_t launch(Append8 p, hipStream_t stream) {
     const bool halves = a.layout == NGPU_ROPE_HALF;
     const int64_t items = a.q ? int64_t(a.q_heads) * (p.c.cache.dim / N - (halves ? a.rotary / 2 / N : 0)) : 0;
     // Threads a token's queries: one for each item where these are few, else one for eight, or four pairs.  us: 5 x 3500 tokens of
-    // 32 + 8 heads of 128, pairs 80, with two an item 112, four 86, 32 90; 4 x 2000 of 8 + 4 of 80, halves 14.1, with one 19.3.
+    // 32 + 8 heads of 128, pairs 79, four 86, two 108, one 108; 4 x 2000 of 8 + 4 of 80, halves 14.0, two 16.5, one 19.3.
     const int64_t passes = a.S * a.T * items >= int64_t(1) << 18 ? (halves ? 4 : 8) : 1;
     p.bits = 4;
     while (p.bits < 8 && (passes << p.bits) < items) ++p.bits;
@@ -411,8 +412,8 @@ static hipError_t launch(Append8 p, hipStream_t stream) {
 }
 
 // Four wavefronts a block where one would have more than eight items a lane (23 x 2000 tokens of 1 head of 128 in blocks of
-// 128: 38 us, not 78; with two items a lane each 5 x 3500 takes 109, not 86); fewer registers where it has two (16 x 2000 of
-// 4 heads of 64 in blocks of 16: 54 us, not 60).
+// 128: 31.5 us, not 74.5; with four from two items a lane on, 5 x 3500 takes 94, not 79); fewer registers where it has two
+// (16 x 2000 of 4 heads of 64 in blocks of 16: 46 us, not 50).
 template <class T>
 static hipError_t launch(const Append8 &p, hipStream_t stream) {
     const int N = in_eights(p) ? 8 : 1;

@@ -12,7 +12,9 @@
 // row needs and what is free; the pages.  A few rows of a small pool are taken
 // by one workgroup in one launch, others by a launch a step; bound by these launches and a few
 // dependent round trips each until tables and pool are large: a fork of 64 x 16 rows of 114 entries over 29408 pages takes
-// 14.3 us, 8.8 MB of tables and counts, a compaction of 200 pages 2.1 us, of 8000 4.4, of 200000 10.1.
+// 14.3 us, 8.8 MB of tables and counts, a compaction of 200 pages 2.1 us, of 8000 4.4, of 200000 10.1.  A row that appends into
+// a page filled in part looks at the rows before it in its group: 1 x K rows that do take 10 us with K = 16, 31 with 256, 99
+// with 1024 and 370 with 4096.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
